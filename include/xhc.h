@@ -404,6 +404,80 @@ xhc_status xhc_flash_pre_bwd(const xhc_dims* d, int32_t Q, const void* X, const 
 xhc_status xhc_stream_sum(const xhc_dims* d, const void* X, void* out, void* stream);
 xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int32_t accumulate, void* stream);
 
+/* ------------------------------------------------------------ the sublayer's own function
+ * What runs between xhc_pre and xhc_post of an MLP-type sublayer: the norm of
+ * its input and a gated feed-forward block, forward and backward.  Only T, C,
+ * state_dtype and (norm) eps of d are used.  Tensor pointers are 16-byte
+ * aligned; an output may not be one of the other tensors of its call.
+ *
+ * xhc_rmsnorm: y [T,C] = x r gain with r_t = 1 / sqrt(mean_c x[t,c]^2 + eps),
+ *   rounded once.  x, y in the state dtype, gain [C] fp32; rstd [T] fp32 or
+ *   NULL receives r, as xhc_rmsnorm_bwd needs it.
+ * xhc_rmsnorm_bwd: dx [T,C] = r v - x r^3 mean_c(v x), v = dy gain, in the
+ *   state dtype; dgain [C] fp32 = sum_t dy x r (zero for T = 0), summed in a
+ *   fixed order.  workspace: xhc_rmsnorm_workspace_bytes(d) bytes.           */
+size_t xhc_rmsnorm_workspace_bytes(const xhc_dims* d);
+xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void* y, float* rstd, void* stream);
+xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, const float* rstd, const void* dy,
+                           void* dx, float* dgain, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gated feed-forward block with H hidden columns (1 <= H <= 2^20, any; C <= 2^20):
+ *   h = act(input W_gate) * (input W_up),  F = h W_down
+ * act: SILU z sigma(z), GELU z Phi(z) (the error function, not its tanh form).
+ *
+ * xhc_pack_ffn rounds W_gate, W_up [C,H] and W_down [H,C] (fp32) to bf16
+ *   (nearest even) into an opaque layout of xhc_packed_ffn_bytes; with_bwd = 1
+ *   also lays them out for xhc_ffn_bwd (twice the bytes; without it
+ *   xhc_ffn_bwd must not be called on them).  To be called again whenever the
+ *   weights have changed.
+ * xhc_ffn: F [T,C] from input [T,C].  saved: NULL, or xhc_ffn_saved_bytes(d, H)
+ *   bytes that receive input W_gate and input W_up for xhc_ffn_bwd.
+ * xhc_ffn_bwd: given dF [T,C] and the forward's input, packed and saved,
+ *   d_input [T,C] and dW_gate, dW_up [C,H], dW_down [H,C] in the state dtype
+ *   (overwritten; zero for T = 0).  Weights receive the gradient of their bf16
+ *   values.
+ * workspace: xhc_ffn_workspace_bytes(d, H, backward) bytes, backward = 0 for
+ *   xhc_ffn and 1 for xhc_ffn_bwd.
+ *
+ * Sums are fp32 (matrix cores), in an order fixed by the sizes.  bf16 state:
+ * h, the saved projections and the gradients of the projections are rounded to
+ * bf16, everything else once, as output.  fp32 state: activations enter the
+ * products as three bf16 parts that add up to them exactly, so that results
+ * have fp32 accuracy (for the bf16 weights).                                */
+typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1 } xhc_act;
+size_t xhc_packed_ffn_bytes(const xhc_dims* d, int32_t H, int32_t with_bwd);
+size_t xhc_ffn_saved_bytes(const xhc_dims* d, int32_t H);
+size_t xhc_ffn_workspace_bytes(const xhc_dims* d, int32_t H, int32_t backward);
+xhc_status xhc_pack_ffn(const xhc_dims* d, int32_t H, const float* W_gate, const float* W_up, const float* W_down,
+                        int32_t with_bwd, void* packed, void* stream);
+xhc_status xhc_ffn(const xhc_dims* d, int32_t H, int32_t act, const void* input, const void* packed, void* F,
+                   void* saved, void* workspace, size_t workspace_bytes, void* stream);
+xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* input, const void* packed,
+                       const void* saved, const void* dF, void* d_input, void* dW_gate, void* dW_up, void* dW_down,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------ gradient norm and clip
+ * Over n tensors (0 <= n <= 4096) of any sizes: grads, counts, dtypes (and
+ * outs) are HOST arrays, read before the call returns: device pointer, number
+ * of elements (0: not looked at; at most 2^40 in all) and xhc_dtype of each.
+ * Pointers are aligned to their element; where they are to 16 bytes the
+ * tensor is read and written fastest.
+ *
+ * xhc_grad_norm: norm [1] fp32 = sqrt(sum of the squares of all elements).
+ * xhc_grad_clip: that norm, and out_i = c grads_i in the tensor's dtype with
+ *   c = min(1, max_norm / (norm + 1e-6)); outs[i] may be grads[i] (in place).
+ *   Where norm is not finite (an element is not, or the norm is above the
+ *   largest float) out_i = grads_i: the caller sees it from norm.  max_norm >= 0.
+ *   XHC_EINVAL where an output overlaps another tensor of the call.
+ * Squares and sums are fp64, added in a fixed order.  workspace:
+ * xhc_grad_workspace_bytes(n) bytes.                                        */
+size_t xhc_grad_workspace_bytes(int32_t n);
+xhc_status xhc_grad_norm(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                         float* norm, void* workspace, size_t workspace_bytes, void* stream);
+xhc_status xhc_grad_clip(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                         float max_norm, void* const* outs, float* norm, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
 #ifdef __cplusplus
 }
 #endif

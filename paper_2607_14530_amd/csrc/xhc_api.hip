@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <new>
 
 #include "xhc.h"
 #include "xhc_launch.h"
@@ -998,6 +999,204 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
   XHC_STEP("stream_sum_bwd", launch_stream_bcast(d->state_dtype, dout, d->T, d->N, d->C, accumulate, dX,
                                                  reinterpret_cast<hipStream_t>(stream)));
   return hip_status(e);
+}
+
+size_t xhc_rmsnorm_workspace_bytes(const xhc_dims* d) {
+  return check_dims(d) == XHC_OK ? rmsnorm_bwd_ws_bytes(d->T, d->C) : 0;
+}
+
+xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void* y, float* rstd, void* stream) {
+  xhc_status st = check_dims(d);
+  if (st != XHC_OK) return st;
+  if (d->T == 0) return XHC_OK;
+  if (!x || !gain || !y || x == y || gain == y || (rstd && (rstd == x || rstd == y || rstd == gain)))
+    return XHC_EINVAL;
+  if (!aligned16(x) || !aligned16(gain) || !aligned16(y) || !aligned16(rstd)) return XHC_EUNSUPPORTED;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("rmsnorm", launch_rmsnorm(d->state_dtype, x, gain, d->T, d->C, d->eps, y, rstd,
+                                     reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, const float* rstd, const void* dy,
+                           void* dx, float* dgain, void* workspace, size_t workspace_bytes, void* stream) {
+  xhc_status st = check_dims(d);
+  if (st != XHC_OK) return st;
+  if (!dgain) return XHC_EINVAL;
+  if (d->T > 0) {
+    if (!x || !gain || !rstd || !dy || !dx || !workspace) return XHC_EINVAL;
+    for (const void* in : {x, (const void*)gain, (const void*)rstd, dy})
+      if (in == dx || in == dgain) return XHC_EINVAL;
+    if (dx == dgain) return XHC_EINVAL;
+  }
+  for (const void* p : {x, (const void*)gain, (const void*)rstd, dy, (const void*)dx, (const void*)dgain,
+                        (const void*)workspace})
+    if (!aligned16(p)) return XHC_EUNSUPPORTED;
+  if (workspace_bytes < rmsnorm_bwd_ws_bytes(d->T, d->C)) return XHC_EWORKSPACE;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("rmsnorm_bwd", launch_rmsnorm_bwd(d->state_dtype, x, gain, rstd, dy, d->T, d->C, dx, dgain,
+                                             reinterpret_cast<float*>(workspace),
+                                             reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+static xhc_status check_ffn(const xhc_dims* d, int32_t H) {
+  xhc_status st = check_dims(d);
+  if (st != XHC_OK) return st;
+  if (H < 1) return XHC_EINVAL;
+  return H > kMaxFfn || d->C > kMaxFfn ? XHC_EUNSUPPORTED : XHC_OK;
+}
+
+size_t xhc_packed_ffn_bytes(const xhc_dims* d, int32_t H, int32_t with_bwd) {
+  return check_ffn(d, H) == XHC_OK ? ffn_packed_bytes(d->C, H, with_bwd != 0) : 0;
+}
+
+size_t xhc_ffn_saved_bytes(const xhc_dims* d, int32_t H) {
+  return check_ffn(d, H) == XHC_OK ? ffn_saved_bytes(d->state_dtype, d->T, H) : 0;
+}
+
+size_t xhc_ffn_workspace_bytes(const xhc_dims* d, int32_t H, int32_t backward) {
+  return check_ffn(d, H) == XHC_OK ? ffn_ws_bytes(d->state_dtype, d->T, d->C, H, backward != 0) : 0;
+}
+
+xhc_status xhc_pack_ffn(const xhc_dims* d, int32_t H, const float* W_gate, const float* W_up, const float* W_down,
+                        int32_t with_bwd, void* packed, void* stream) {
+  xhc_status st = check_ffn(d, H);
+  if (st != XHC_OK) return st;
+  if (!W_gate || !W_up || !W_down || !packed || packed == W_gate || packed == W_up || packed == W_down ||
+      (with_bwd != 0 && with_bwd != 1))
+    return XHC_EINVAL;
+  if (!aligned16(W_gate) || !aligned16(W_up) || !aligned16(W_down) || !aligned16(packed)) return XHC_EUNSUPPORTED;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("ffn_pack", launch_ffn_pack(d->C, H, W_gate, W_up, W_down, with_bwd != 0, packed,
+                                       reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_ffn(const xhc_dims* d, int32_t H, int32_t act, const void* input, const void* packed, void* F,
+                   void* saved, void* workspace, size_t workspace_bytes, void* stream) {
+  xhc_status st = check_ffn(d, H);
+  if (st != XHC_OK) return st;
+  if (act != XHC_ACT_SILU && act != XHC_ACT_GELU) return XHC_EINVAL;
+  if (d->T == 0) return XHC_OK;
+  if (!input || !packed || !F || !workspace || F == input || F == packed || saved == input || saved == packed ||
+      saved == F)
+    return XHC_EINVAL;
+  if (!aligned16(input) || !aligned16(packed) || !aligned16(F) || !aligned16(saved) || !aligned16(workspace))
+    return XHC_EUNSUPPORTED;
+  if (workspace_bytes < ffn_ws_bytes(d->state_dtype, d->T, d->C, H, false)) return XHC_EWORKSPACE;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("ffn", launch_ffn(d->state_dtype, d->T, d->C, H, act, input, packed, F, saved, workspace,
+                             reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* input, const void* packed,
+                       const void* saved, const void* dF, void* d_input, void* dW_gate, void* dW_up, void* dW_down,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  xhc_status st = check_ffn(d, H);
+  if (st != XHC_OK) return st;
+  if (act != XHC_ACT_SILU && act != XHC_ACT_GELU) return XHC_EINVAL;
+  if (!dW_gate || !dW_up || !dW_down || !workspace) return XHC_EINVAL;
+  if (d->T > 0 && (!input || !packed || !saved || !dF || !d_input)) return XHC_EINVAL;
+  const void* outs[4] = {dW_gate, dW_up, dW_down, d_input};
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i]) continue;
+    for (const void* in : {input, packed, saved, dF})
+      if (in == outs[i]) return XHC_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (outs[j] == outs[i]) return XHC_EINVAL;
+  }
+  for (const void* p : {input, packed, saved, dF, (const void*)d_input, (const void*)dW_gate, (const void*)dW_up,
+                        (const void*)dW_down, (const void*)workspace})
+    if (!aligned16(p)) return XHC_EUNSUPPORTED;
+  if (workspace_bytes < ffn_ws_bytes(d->state_dtype, d->T, d->C, H, true)) return XHC_EWORKSPACE;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("ffn_bwd", launch_ffn_bwd(d->state_dtype, d->T, d->C, H, act, input, packed, saved, dF, d_input, dW_gate,
+                                     dW_up, dW_down, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+// Whether every output is apart from all else of the call (but its own
+// gradient, in place).  Sorted by start, a range overlaps an earlier one if it
+// starts before the furthest end so far.
+static xhc_status check_apart(int n, const void* const* grads, void* const* outs, const int64_t* counts,
+                              const int32_t* dtypes, const float* norm) {
+  struct Range {
+    uintptr_t at, end;
+    bool out;
+  };
+  Range* r = new (std::nothrow) Range[2 * (size_t)n + 1];
+  if (!r) return XHC_EUNSUPPORTED;
+  int m = 0;
+  for (int i = 0; i < n; ++i) {
+    if (counts[i] == 0) continue;
+    const uintptr_t bytes = (uintptr_t)counts[i] * (dtypes[i] == XHC_F32 ? 4 : 2);
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]), o = reinterpret_cast<uintptr_t>(outs[i]);
+    r[m++] = Range{o, o + bytes, true};
+    if (g != o) r[m++] = Range{g, g + bytes, false};
+  }
+  const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
+  r[m++] = Range{at, at + sizeof(float), true};
+  std::sort(r, r + m, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t all = 0, written = 0;
+  bool apart = true;
+  for (int i = 0; i < m; ++i) {
+    if (r[i].at < (r[i].out ? all : written)) apart = false;
+    all = std::max(all, r[i].end);
+    if (r[i].out) written = std::max(written, r[i].end);
+  }
+  delete[] r;
+  return apart ? XHC_OK : XHC_EINVAL;
+}
+
+static xhc_status grad_call(const char* step, int32_t n, const void* const* grads, const int64_t* counts,
+                            const int32_t* dtypes, float max_norm, void* const* outs, float* norm, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (n < 0 || !norm || !workspace || (n > 0 && (!grads || !counts || !dtypes))) return XHC_EINVAL;
+  if (n > kMaxGrads) return XHC_EUNSUPPORTED;
+  int64_t total = 0;
+  for (int i = 0; i < n; ++i) {
+    if (counts[i] < 0 || (dtypes[i] != XHC_BF16 && dtypes[i] != XHC_F32)) return XHC_EINVAL;
+    if (counts[i] == 0) continue;
+    if (!grads[i] || (outs && !outs[i])) return XHC_EINVAL;
+    if (counts[i] > kMaxGradElems || (total += counts[i]) > kMaxGradElems) return XHC_EUNSUPPORTED;
+    const uintptr_t low = dtypes[i] == XHC_F32 ? 3 : 1;
+    if ((reinterpret_cast<uintptr_t>(grads[i]) | (outs ? reinterpret_cast<uintptr_t>(outs[i]) : 0)) & low)
+      return XHC_EUNSUPPORTED;
+  }
+  if ((reinterpret_cast<uintptr_t>(norm) & 3) || !aligned16(workspace)) return XHC_EUNSUPPORTED;
+  if (workspace_bytes < grad_ws_bytes(n)) return XHC_EWORKSPACE;
+  if (outs) {
+    const xhc_status st = check_apart(n, grads, outs, counts, dtypes, norm);
+    if (st != XHC_OK) return st;
+  }
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP(step, launch_grad_clip(n, grads, counts, dtypes, max_norm, outs, norm, workspace,
+                                  reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+size_t xhc_grad_workspace_bytes(int32_t n) { return n < 0 || n > kMaxGrads ? 0 : grad_ws_bytes(n); }
+
+xhc_status xhc_grad_norm(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                         float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  return grad_call("grad_norm", n, grads, counts, dtypes, 0.f, nullptr, norm, workspace, workspace_bytes, stream);
+}
+
+xhc_status xhc_grad_clip(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                         float max_norm, void* const* outs, float* norm, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (!(max_norm >= 0.f) || (n > 0 && !outs)) return XHC_EINVAL;
+  static void* const none[1] = {nullptr};
+  return grad_call("grad_clip", n, grads, counts, dtypes, max_norm, outs ? outs : none, norm, workspace,
+                   workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -292,6 +292,33 @@ hipError_t launch_fbwd_scatter(int state_dtype, int64_t T, int N, int k, int C, 
 hipError_t launch_fbwd_finish(int state_dtype, int64_t T, int k, int C, const float* da_rev, const float* Hsel,
                               const void* din, float* da, hipStream_t s);
 
+// ---- the sublayer's own function: norm, gated feed-forward block; gradient clip
+hipError_t launch_rmsnorm(int state_dtype, const void* x, const float* gain, int64_t T, int C, float eps, void* y,
+                          float* rstd, hipStream_t s);
+size_t rmsnorm_bwd_ws_bytes(int64_t T, int C);
+hipError_t launch_rmsnorm_bwd(int state_dtype, const void* x, const float* gain, const float* rstd, const void* dy,
+                              int64_t T, int C, void* dx, float* dgain, float* part, hipStream_t s);
+
+constexpr int kMaxFfn = 1 << 20;   // C and H: a tile's rows stay below 2 GiB
+size_t ffn_packed_bytes(int64_t C, int64_t H, bool with_bwd);
+size_t ffn_saved_bytes(int state_dtype, int64_t T, int64_t H);
+size_t ffn_ws_bytes(int state_dtype, int64_t T, int64_t C, int64_t H, bool bwd);
+hipError_t launch_ffn_pack(int64_t C, int64_t H, const float* W_gate, const float* W_up, const float* W_down,
+                           bool with_bwd, void* packed, hipStream_t s);
+hipError_t launch_ffn(int state_dtype, int64_t T, int64_t C, int64_t H, int act, const void* input,
+                      const void* packed, void* F, void* saved, void* workspace, hipStream_t s);
+hipError_t launch_ffn_bwd(int state_dtype, int64_t T, int64_t C, int64_t H, int act, const void* input,
+                          const void* packed, const void* saved, const void* dF, void* d_input, void* dW_gate,
+                          void* dW_up, void* dW_down, void* workspace, hipStream_t s);
+
+constexpr int kGradBatch = 128;    // tensors of one launch
+constexpr int kMaxGrads = 4096;    // tensors of one call
+constexpr int64_t kMaxGradElems = (int64_t)1 << 40;   // their elements
+size_t grad_ws_bytes(int n);
+// outs null: the norm alone
+hipError_t launch_grad_clip(int n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                            float max_norm, void* const* outs, float* norm, void* ws, hipStream_t s);
+
 // per-token values xhc_pre saves for the backward: [z_r (N) | z_pre (N) |
 // z_post, z_res (k*Kr + k*k) | mu | nu | nu_a | pad], z = normalised logits
 __host__ __device__ inline int saved_floats(int N, int k, int Kr) { return 2 * N + k * Kr + k * k + 4; }

@@ -7,11 +7,15 @@ runs in the library's HIP kernels.  There is no CPU fallback: if the library
 is missing or no GPU is present, calls raise.
 
 ``Sublayer`` / ``FlashGroup`` bundle packing, output allocation and the calls
-for convenience; they add no arithmetic.
+for convenience; they add no arithmetic.  ``RMSNorm`` and ``FeedForward`` (and
+their trainable forms, whose forward and backward ``Stack`` takes as a
+sublayer's functions) do the same for an MLP-type sublayer's own function, and
+``clip_grad_norm`` for the clip of the gradients that a backward has given.
 """
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -27,6 +31,7 @@ STATUS_NAMES = {0: "XHC_OK", 1: "XHC_EINVAL", 2: "XHC_EUNSUPPORTED", 3: "XHC_EWO
 XHC_BF16, XHC_F32 = 0, 1
 XHC_IMPL_AUTO, XHC_IMPL_MULTI, XHC_IMPL_FUSED = 0, 1, 2
 XHC_ROUTER_SIGMOID, XHC_ROUTER_SOFTMAX = 0, 1
+XHC_ACT_SILU, XHC_ACT_GELU = 0, 1
 (XHC_OP_PRE, XHC_OP_POST, XHC_OP_FLASH_PRE, XHC_OP_FLASH_POST, XHC_OP_POST_BWD, XHC_OP_PRE_BWD,
  XHC_OP_FLASH_POST_BWD, XHC_OP_FLASH_PRE_BWD) = range(8)
 
@@ -95,6 +100,18 @@ _SIGS = {
     "xhc_stream_sum": (ctypes.c_int, [_D, _P, _P, _P]),
     "xhc_stream_sum_bwd": (ctypes.c_int, [_D, _P, _P, ctypes.c_int32, _P]),
     "xhc_pre_failures": (ctypes.c_int, [_P, _P, _P]),
+    "xhc_rmsnorm_workspace_bytes": (ctypes.c_size_t, [_D]),
+    "xhc_rmsnorm": (ctypes.c_int, [_D] + [_P] * 5),
+    "xhc_rmsnorm_bwd": (ctypes.c_int, [_D] + [_P] * 7 + [ctypes.c_size_t, _P]),
+    "xhc_packed_ffn_bytes": (ctypes.c_size_t, [_D, ctypes.c_int32, ctypes.c_int32]),
+    "xhc_ffn_saved_bytes": (ctypes.c_size_t, [_D, ctypes.c_int32]),
+    "xhc_ffn_workspace_bytes": (ctypes.c_size_t, [_D, ctypes.c_int32, ctypes.c_int32]),
+    "xhc_pack_ffn": (ctypes.c_int, [_D, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P, _P]),
+    "xhc_ffn": (ctypes.c_int, [_D, ctypes.c_int32, ctypes.c_int32] + [_P] * 5 + [ctypes.c_size_t, _P]),
+    "xhc_ffn_bwd": (ctypes.c_int, [_D, ctypes.c_int32, ctypes.c_int32] + [_P] * 9 + [ctypes.c_size_t, _P]),
+    "xhc_grad_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32]),
+    "xhc_grad_norm": (ctypes.c_int, [ctypes.c_int32] + [_P] * 5 + [ctypes.c_size_t, _P]),
+    "xhc_grad_clip": (ctypes.c_int, [ctypes.c_int32] + [_P] * 3 + [ctypes.c_float] + [_P] * 3 + [ctypes.c_size_t, _P]),
     "xhc_status_string": (ctypes.c_char_p, [ctypes.c_int32]),
     "xhc_last_hip_error": (ctypes.c_char_p, []),
 }
@@ -271,6 +288,78 @@ def xhc_stream_sum(d, X, out, stream=None):
 
 def xhc_stream_sum_bwd(d, dout, dX, accumulate=False, stream=None):
     _call("xhc_stream_sum_bwd", ctypes.byref(d), _ptr(dout), _ptr(dX), int(bool(accumulate)), _stream(stream))
+
+
+def xhc_rmsnorm_workspace_bytes(d):
+    return lib().xhc_rmsnorm_workspace_bytes(ctypes.byref(d))
+
+
+def xhc_rmsnorm(d, x, gain, y, rstd, stream=None):
+    _call("xhc_rmsnorm", ctypes.byref(d), _ptr(x), _ptr(gain), _ptr(y), _ptr(rstd), _stream(stream))
+
+
+def xhc_rmsnorm_bwd(d, x, gain, rstd, dy, dx, dgain, workspace, stream=None):
+    _call("xhc_rmsnorm_bwd", ctypes.byref(d), _ptr(x), _ptr(gain), _ptr(rstd), _ptr(dy), _ptr(dx), _ptr(dgain),
+          _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def xhc_packed_ffn_bytes(d, H, with_bwd):
+    return lib().xhc_packed_ffn_bytes(ctypes.byref(d), H, int(with_bwd))
+
+
+def xhc_ffn_saved_bytes(d, H):
+    return lib().xhc_ffn_saved_bytes(ctypes.byref(d), H)
+
+
+def xhc_ffn_workspace_bytes(d, H, backward):
+    return lib().xhc_ffn_workspace_bytes(ctypes.byref(d), H, int(backward))
+
+
+def xhc_pack_ffn(d, H, W_gate, W_up, W_down, with_bwd, packed, stream=None):
+    _call("xhc_pack_ffn", ctypes.byref(d), H, _ptr(W_gate), _ptr(W_up), _ptr(W_down), int(with_bwd), _ptr(packed),
+          _stream(stream))
+
+
+def xhc_ffn(d, H, act, input, packed, F, saved, workspace, stream=None):
+    _call("xhc_ffn", ctypes.byref(d), H, act, _ptr(input), _ptr(packed), _ptr(F), _ptr(saved), _ptr(workspace),
+          _nbytes(workspace), _stream(stream))
+
+
+def xhc_ffn_bwd(d, H, act, input, packed, saved, dF, d_input, dW_gate, dW_up, dW_down, workspace, stream=None):
+    _call("xhc_ffn_bwd", ctypes.byref(d), H, act, _ptr(input), _ptr(packed), _ptr(saved), _ptr(dF), _ptr(d_input),
+          _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def _grad_arrays(grads):
+    """Host arrays of the tensors' addresses, counts and dtypes."""
+    n = len(grads)
+    for g in grads:
+        if g.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"gradients are bf16 or fp32, got {g.dtype}")
+    return ((_P * n)(*[_ptr(g) for g in grads]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
+            (ctypes.c_int32 * n)(*[XHC_BF16 if g.dtype == torch.bfloat16 else XHC_F32 for g in grads]))
+
+
+def xhc_grad_workspace_bytes(n):
+    return lib().xhc_grad_workspace_bytes(n)
+
+
+def xhc_grad_norm(grads, norm, workspace, stream=None):
+    ptrs, counts, dtypes = _grad_arrays(grads)
+    _call("xhc_grad_norm", len(grads), ptrs, counts, dtypes, _ptr(norm), _ptr(workspace), _nbytes(workspace),
+          _stream(stream))
+
+
+def xhc_grad_clip(grads, max_norm, outs, norm, workspace, stream=None):
+    """outs: a list of the gradients' shapes and dtypes (the gradients themselves for in place)."""
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
+    for g, o in zip(grads, outs):
+        _expect(o, g.dtype, g.shape, "output of a gradient")
+    ptrs, counts, dtypes = _grad_arrays(grads)
+    to = ptrs if outs is grads else (_P * len(outs))(*[_ptr(o) for o in outs])
+    _call("xhc_grad_clip", len(grads), ptrs, counts, dtypes, max_norm, to, _ptr(norm), _ptr(workspace),
+          _nbytes(workspace), _stream(stream))
 
 
 # ---------------------------------------------------------------- convenience bundle
@@ -600,3 +689,174 @@ class Stack:
             dX = g["X"]
         return grads, dX
 
+
+# ---------------------------------------------------------------- the sublayer's own function
+
+def _on(t, dev, name):
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+
+
+def _here(device):
+    """The device of a bundle: the current one, where its calls enqueue."""
+    dev = torch.device(device)
+    cur = torch.device("cuda", torch.cuda.current_device())
+    if dev.type != "cuda" or (dev.index is not None and dev != cur):
+        raise ValueError(f"{dev} is not the current device {cur}")
+    return cur
+
+
+def _within(stream):
+    """The context in which temporaries of work on `stream` are made: their
+    memory then belongs to that stream."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+def _state_dtype(d):
+    return torch.bfloat16 if d.state_dtype == XHC_BF16 else torch.float32
+
+
+class RMSNorm:
+    """RMS norm of [T, C] rows with a gain (fp32 [C]); eps is d.eps.  Outputs
+    go to a buffer of this object, overwritten by its next forward."""
+
+    def __init__(self, d: Dims, gain, device="cuda"):
+        self.d, self.device = d, _here(device)
+        _expect(gain, torch.float32, (d.C,), "gain")
+        self.gain = gain.to(self.device).contiguous()
+        self.y = torch.empty(d.T, d.C, dtype=_state_dtype(d), device=self.device)
+        self.rstd = None
+
+    def forward(self, x, stream=None):
+        _expect(x, self.y.dtype, self.y.shape, "x")
+        _on(x, self.device, "x")
+        xhc_rmsnorm(self.d, x, self.gain, self.y, self.rstd, stream)
+        return self.y
+
+
+class TrainableRMSNorm(RMSNorm):
+    """An RMSNorm that keeps what the backward needs and runs it: backward(dy)
+    returns dL/dx of the last forward's x (read again: it must still hold its
+    values) and leaves dL/dgain in grads["gain"]."""
+
+    def __init__(self, d: Dims, gain, device="cuda"):
+        super().__init__(d, gain, device)
+        self.rstd = torch.empty(d.T, dtype=torch.float32, device=self.device)
+        self.dx = torch.empty_like(self.y)
+        self.grads = {"gain": torch.empty_like(self.gain)}
+        self.ws = _bytes(xhc_rmsnorm_workspace_bytes(d), self.device)
+        self.x = None
+
+    def forward(self, x, stream=None):
+        self.x = x
+        return super().forward(x, stream)
+
+    def backward(self, dy, stream=None):
+        if self.x is None:
+            raise ValueError("backward without a forward")
+        _expect(dy, self.y.dtype, self.y.shape, "dy")
+        _on(dy, self.device, "dy")
+        xhc_rmsnorm_bwd(self.d, self.x, self.gain, self.rstd, dy, self.dx, self.grads["gain"], self.ws, stream)
+        return self.dx
+
+
+class FeedForward:
+    """Gated feed-forward block F = (act(x W_gate) * (x W_up)) W_down of [T, C]
+    rows: packed weights and buffers.  ``weights`` holds W_gate, W_up [C, H]
+    and W_down [H, C], fp32; act is "silu" or "gelu".  pack(weights) takes new
+    values of them.  Outputs go to a buffer of this object, overwritten by its
+    next forward."""
+
+    with_bwd = 0
+
+    def __init__(self, d: Dims, H: int, weights, act="silu", device="cuda"):
+        if act not in ("silu", "gelu"):
+            raise ValueError(f"act is 'silu' or 'gelu', got {act!r}")
+        self.d, self.H, self.device = d, H, _here(device)
+        self.act = XHC_ACT_SILU if act == "silu" else XHC_ACT_GELU
+        self.F = torch.empty(d.T, d.C, dtype=_state_dtype(d), device=self.device)
+        self.packed = _bytes(xhc_packed_ffn_bytes(d, H, self.with_bwd), self.device)
+        self.ws = _bytes(xhc_ffn_workspace_bytes(d, H, 0), self.device)
+        self.saved = None
+        self.pack(weights)
+
+    def pack(self, weights, stream=None):
+        w = [weights[n] for n in ("W_gate", "W_up", "W_down")]
+        for t, n in zip(w, ("W_gate", "W_up", "W_down")):
+            _expect(t, torch.float32, (self.H, self.d.C) if n == "W_down" else (self.d.C, self.H), n)
+        with _within(stream):
+            w = [t.to(self.device).contiguous() for t in w]
+        xhc_pack_ffn(self.d, self.H, *w, self.with_bwd, self.packed, stream)
+
+    def forward(self, x, stream=None):
+        _expect(x, self.F.dtype, self.F.shape, "x")
+        _on(x, self.device, "x")
+        xhc_ffn(self.d, self.H, self.act, x, self.packed, self.F, self.saved, self.ws, stream)
+        return self.F
+
+
+class TrainableFeedForward(FeedForward):
+    """A FeedForward that keeps what the backward needs and runs it:
+    backward(dF) returns dL/dx of the last forward's x (read again: it must
+    still hold its values, as the input buffer of a sublayer does) and leaves
+    dL/dW_gate, dL/dW_up and dL/dW_down in grads, in the state dtype."""
+
+    with_bwd = 1
+
+    def __init__(self, d: Dims, H: int, weights, act="silu", device="cuda"):
+        super().__init__(d, H, weights, act, device)
+        self.saved = _bytes(xhc_ffn_saved_bytes(d, H), self.device)
+        self.ws_bwd = _bytes(xhc_ffn_workspace_bytes(d, H, 1), self.device)
+        self.d_input = torch.empty_like(self.F)
+        self.grads = {n: torch.empty((H, d.C) if n == "W_down" else (d.C, H), dtype=self.F.dtype, device=self.device)
+                      for n in ("W_gate", "W_up", "W_down")}
+        self.x = None
+
+    def forward(self, x, stream=None):
+        self.x = x
+        return super().forward(x, stream)
+
+    def backward(self, dF, stream=None):
+        if self.x is None:
+            raise ValueError("backward without a forward")
+        _expect(dF, self.F.dtype, self.F.shape, "dF")
+        _on(dF, self.device, "dF")
+        g = self.grads
+        xhc_ffn_bwd(self.d, self.H, self.act, self.x, self.packed, self.saved, dF, self.d_input, g["W_gate"],
+                    g["W_up"], g["W_down"], self.ws_bwd, stream)
+        return self.d_input
+
+
+def grad_tensors(grads):
+    """The weight gradients of a backward, as a list: of a TrainableSublayer's
+    or TrainableFlashGroup's dict, of the grads of a norm or block, or of a
+    list of such.  The state's and the sublayer outputs' gradients, which flow
+    on, are not among them."""
+    if torch.is_tensor(grads):
+        return [grads]
+    if grads is None:
+        return []
+    if isinstance(grads, dict):
+        return [t for n, v in grads.items() if n not in ("X", "F", "F_list", "dHres", "dHpost", "dp")
+                for t in grad_tensors(v)]
+    return [t for v in grads for t in grad_tensors(v)]
+
+
+def clip_grad_norm(grads, max_norm, outs=None, stream=None):
+    """Clips gradients by their global norm: out = g min(1, max_norm / (norm +
+    1e-6)), in place unless ``outs`` (a list like ``grads``) is given; left as
+    they are where the norm is not finite.  Returns the norm before the clip,
+    an fp32 [1] tensor (nothing waits for it here)."""
+    grads = list(grads)
+    dev = _here(grads[0].device if grads else "cuda")
+    for g in grads:
+        _on(g, dev, "gradient")
+    for o in outs or []:
+        _on(o, dev, "output")
+    with _within(stream):
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+        ws = _bytes(xhc_grad_workspace_bytes(len(grads)), dev)
+    xhc_grad_clip(grads, max_norm, grads if outs is None else list(outs), norm, ws, stream)
+    return norm

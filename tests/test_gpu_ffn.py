@@ -1,0 +1,48 @@
+"""The gated feed-forward block on the GPU against 64 bits: values within
+derived bounds at odd and ragged sizes, rows and widths that end inside a tile."""
+
+import pytest
+import torch
+
+from paper_2607_14530_amd import xhc as X
+from tests.ffn_util import HALF, assert_within, ffn_backward, ffn_forward, ffn_inputs
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+# T, C, H: one token, ragged tokens, widths and hidden widths that end inside a block of 16, 32, 64 or a
+# tile, more than one tile each way
+SIZES = [(1, 32, 1), (1, 256, 683), (3, 96, 33), (16, 64, 64), (17, 160, 200), (37, 2112, 341), (64, 256, 1000),
+         (65, 512, 129), (130, 352, 520), (200, 32, 48), (257, 384, 1030), (300, 1056, 96)]
+
+
+def make(T, C, H, state, act, seed, train):
+    x, dF, w = ffn_inputs(T, C, H, DT[state], seed)
+    d = X.make_dims(T, 1, 1, 1, C, state=state)
+    cls = X.TrainableFeedForward if train else X.FeedForward
+    return x, dF, w, cls(d, H, {k: v.cuda() for k, v in w.items()}, act=act)
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("T,C,H", SIZES)
+def test_forward_and_backward(T, C, H, state, act):
+    x, dF, w, ff = make(T, C, H, state, act, 100 + T + C + H, True)
+    F = ff.forward(x.cuda())
+    dx = ff.backward(dF.cuda())
+    torch.cuda.synchronize()
+    half = HALF[DT[state]]
+    fw = ffn_forward(x, w, act, half)
+    assert_within(F, fw["F"], "F")
+    bw = ffn_backward(x, dF, fw, act, half)
+    assert_within(dx, bw["dx"], "dx")
+    for n in ("W_gate", "W_up", "W_down"):
+        assert_within(ff.grads[n], bw[n], "d" + n)
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32"])
+@pytest.mark.parametrize("T,C,H", SIZES)
+def test_forward_without_saving_gives_the_same(T, C, H, state):
+    x, _, _, a = make(T, C, H, state, "silu", 7, False)
+    _, _, _, b = make(T, C, H, state, "silu", 7, True)
+    assert torch.equal(a.forward(x.cuda()), b.forward(x.cuda()))
