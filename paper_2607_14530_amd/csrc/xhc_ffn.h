@@ -1,24 +1,28 @@
 // Building blocks of the gated feed-forward block's matrix products (gfx950).
 //
-// Every product is out[t, n] = sum_k A[t, k] B[n, k] on 16x16x32 bf16 MFMA with
-// fp32 sums, the n side as the first operand: a lane then holds four
-// consecutive n of one t.  A workgroup keeps two stages of 64 k of its tile's
-// operands in LDS, filled by copies that go from global memory to LDS without
-// passing through registers.  Three operand layouts:
+// Every product is out[t, n] = sum_k A[t, k] B[n, k] on bf16 MFMA with fp32
+// sums, the n side as the first operand: a lane then holds consecutive n of
+// one t.  Tiles use 32x32x16 (each operand register feeds twice the products
+// of 16x16x32, which counts where the clock is held down by power), the few
+// tokens of a decoding step 16x16x32.
 //
-//   FragTile  packed weights, [n block of 16][k block of 32] fragments of 1 KiB
-//             in the MFMA's own lane order: copied and read linearly
-//   RowTile   rows with k contiguous (activations, [t][k]): 128 bytes of each
-//             row, its 16-byte pieces at (piece ^ row % 8), so that the 16 rows
-//             of a fragment read meet different banks
-//   ColTile   rows along k (the same activations as the operands of a weight
-//             gradient, whose k is the token): 8 x 128-byte pieces, read by the
-//             transposing LDS load; 32-byte pieces at (piece ^ swz(k)), so that
-//             the 8 rows of a half wave meet different banks
+// All operands lie in fragments: 16 rows x 32 columns in 1 KiB, [piece][row][8],
+// piece = columns 8 piece .. + 8 (the lane order of a 16x16x32 operand), in the
+// order [row block][column block].  A workgroup keeps a ring of stages of its
+// tile's operands in LDS, filled by copies that go from global memory to LDS
+// without passing through registers, 1 KiB run each: a stage of 64 KiB comes
+// in 1.05 us so, in 1.45 from rows as torch has them (runs of 128 bytes), which
+// is what its products take.  So x and dF are brought into fragments first,
+// and the epilogues write h, dg and du so.
 //
+//   FragTile  k is the column: a fragment is an operand as it lies
+//   ColTile   k is the row (a weight gradient's token): the transposing LDS
+//             load takes it from the same fragments
+//
+// Either is read without bank conflicts: 16 lanes read a run of 256 bytes, or
+// (ColTile) a half wave reads pieces that the copy has put into different banks.
 // Copies go through buffer descriptors that end with the tensor: what lies
-// behind its last row is read as zero, and k past the last column is sent
-// behind that end, so that no length needs a padded tensor.
+// behind is read as zero.
 #pragma once
 
 #include "xhc_device.h"
@@ -27,151 +31,155 @@ namespace xhc {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kBK = 64;                           // k of a stage
-constexpr uint32_t kNowhere = 0x80000000u;        // an offset behind every descriptor's end
+// v_mfma_f32_32x32x16_bf16: D[32x32] += A[32x16] * B[16x32].  Lane l holds
+// A[l%32][8*(l/32) .. +8], B[8*(l/32) .. +8][l%32] and
+// D[8*(v/4) + 4*(l/32) + v%4][l%32], v = 0..15.
+__device__ __forceinline__ f32x16 mfma_32x32x16(uint4 a, uint4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                 0, 0);
+}
+// Row p of a block of 16 n holds n = 8 (p / 4 % 2) + 4 (p / 8) + p % 4 of it, so
+// that a lane's eight sums of the block (rows 8 i + 4 (l / 32) + 0 .. 3, i = 0, 1)
+// are eight consecutive n.
+__host__ __device__ __forceinline__ constexpr int perm_n(int p) { return 8 * (p / 4 % 2) + 4 * (p / 8) + p % 4; }
 
 // descriptor of `bytes` bytes at p (below 2 GiB of them; none where bytes <= 0)
-__device__ __forceinline__ i32x4 make_srd(const void* p, int64_t bytes) {
-  const uint64_t a = (uint64_t)(uintptr_t)p;
+__device__ __forceinline__ i32x4 make_srd(uint64_t a, int64_t bytes) {
   const int64_t n = bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : bytes;
   return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
                __builtin_amdgcn_readfirstlane((int)((a >> 32) & 0xffff)),
                __builtin_amdgcn_readfirstlane((int)n), 0x00020000};
 }
 
-// 16 bytes per lane into LDS at lds_addr + 16 lane; lds_addr is the same in
-// every lane.  Inline assembly, waited for by the caller, as lds_dma16.
-__device__ __forceinline__ void buf_dma16(const i32x4& srd, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds"
+// 16 bytes per lane from voff + soff into LDS at lds_addr + AT + 16 lane;
+// lds_addr and soff are the same in every lane.  soff does not reach past the
+// descriptor's end where voff does not: it stays within a row.  Inline
+// assembly, waited for by the caller, as lds_dma16 (the s_nop is the wait state
+// that a copy needs after a write of m0).
+template <int AT>
+__device__ __forceinline__ void buf_dma16(const i32x4& srd, uint32_t voff, uint32_t soff, uint32_t lds_addr) {
+  asm volatile("s_add_u32 m0, %1, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
                :
-               : "v"(voff), "s"(lds_addr), "s"(srd)
-               : "memory", "m0");
+               : "v"(voff), "s"(lds_addr), "s"(srd), "s"(soff), "n"(AT)
+               : "memory", "m0", "scc");
 }
 
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// an operand: its planes lie `plane` bytes apart (one for bf16, three for fp32:
-// x = plane 0 + plane 1 + plane 2 exactly)
+// where element (t, c) lies in fragments with kb column blocks
+__host__ __device__ __forceinline__ int64_t frag_at(int64_t t, int64_t c, int64_t kb) {
+  return (t / 16 * kb + c / 32) * 512 + ((c / 8 % 4) * 16 + t % 16) * 8 + c % 8;
+}
+
+// an operand in fragments: its planes lie `plane` bytes apart (one for bf16,
+// three for fp32: x = plane 0 + plane 1 + plane 2 exactly)
 struct Operand {
   const void* p;
   int64_t plane;
-  int64_t ld;     // elements between rows (FragTile: k blocks of 32)
-  int64_t rows;   // rows of the tensor (FragTile: n blocks)
-  int klim;       // columns that exist (RowTile)
+  int64_t rows, kb;   // row blocks of 16, column blocks of 32
 };
 
-template <int ROWS, int NW>
+// Tiles of ROWS rows (COLS columns) by KH blocks of 32 k, copied by NW waves of
+// kCopies instructions each.  A tile's rows past the last read what follows:
+// they only reach sums that nobody writes.
+template <int ROWS, int KH, int NW>
 struct FragTile {
-  static constexpr int kBytes = ROWS * 128, NI = ROWS / 8 / NW;
-  static_assert(ROWS % (8 * NW) == 0, "whole copies for every wave");
+  static constexpr int kBytes = ROWS * 64 * KH, kCopies = ROWS * KH / 16 / NW, kReads = 1;
+  static_assert(ROWS * KH % (16 * NW) == 0, "whole copies for every wave");
   i32x4 srd;
-  uint32_t voff, nstride;
-  int wave;
+  uint32_t voff[kCopies], soff, lds;
   const Operand* op;
-  int64_t row0;
-  __device__ __forceinline__ void init(const Operand& o, int64_t r0, int w, int lane) {
+  int64_t at;
+  __device__ __forceinline__ void init(const Operand& o, int64_t row0, int wave, int lane) {
     op = &o;
-    row0 = r0;
-    wave = w;
-    nstride = (uint32_t)o.ld * 1024;
-    voff = lane * 16;
-    const int64_t at = r0 / 16 * o.ld * 1024;
-    srd = make_srd(reinterpret_cast<const char*>(o.p) + at, o.rows * o.ld * 1024 - at);
-  }
-  __device__ __forceinline__ void plane(int) {}      // weights have one
-  __device__ __forceinline__ void issue(uint32_t lds, int ks) {
+    lds = wave * kCopies * 1024;
+    at = row0 / 16 * o.kb * 1024;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int f = wave * NI + i;
-      buf_dma16(srd, voff + (uint32_t)(f / 2) * nstride + (uint32_t)(ks * 2 + f % 2) * 1024,
-                __builtin_amdgcn_readfirstlane(lds + f * 1024));
+    for (int i = 0; i < kCopies; ++i) {
+      const int f = wave * kCopies + i;
+      voff[i] = lane * 16 + (uint32_t)(f / KH) * (uint32_t)o.kb * 1024 + (uint32_t)(f % KH) * 1024;
     }
   }
-  static __device__ __forceinline__ uint4 frag(const unsigned char* s, int f16, int kk, int lane) {
-    return *reinterpret_cast<const uint4*>(s + (f16 * 2 + kk) * 1024 + lane * 16);
+  // from stage ks of a plane on
+  __device__ __forceinline__ void start(int plane, int64_t ks) {
+    srd = make_srd((uint64_t)(uintptr_t)op->p + plane * op->plane + at, op->rows * op->kb * 1024 - at);
+    soff = (uint32_t)ks * (KH * 1024);
+  }
+  __device__ __forceinline__ void next() { soff += KH * 1024; }
+  // nothing more: copies read no memory and leave zeros
+  __device__ __forceinline__ void end() {
+    srd.z = 0;
+    soff = 0;
+  }
+  template <int I> __device__ __forceinline__ void copy(uint32_t to) const {
+    buf_dma16<I * 1024>(srd, voff[I], soff, to + lds);
+  }
+  // rows 32 f .., k = 32 kk + 16 m + 8 (lane / 32) + e
+  static __device__ __forceinline__ uint4 frag(const unsigned char* s, int f, int kk, int m, int lane) {
+    return *reinterpret_cast<const uint4*>(s + ((f * 2 + lane % 32 / 16) * KH + kk) * 1024 +
+                                           (2 * m + lane / 32) * 256 + lane % 16 * 16);
   }
 };
 
-template <int ROWS, int NW>
-struct RowTile {
-  static constexpr int kBytes = ROWS * 128, NI = ROWS / 8 / NW;
-  static_assert(ROWS % (8 * NW) == 0, "whole copies for every wave");
+// The rows (k) of a piece lie at (row ^ 4 piece), so that the four pieces of a
+// fragment's 32 columns meet different banks.  PERM: columns as perm_n has them.
+template <int COLS, int KH, int NW, bool PERM>
+struct ColTileOf {
+  static constexpr int kBytes = COLS * 64 * KH, kCopies = COLS * KH / 16 / NW, kReads = 2;
+  static_assert(COLS % 32 == 0 && COLS * KH % (16 * NW) == 0, "whole copies for every wave");
+  static constexpr int kBlocks = COLS / 32;          // fragments side by side
+  uint64_t base;
+  int64_t left, step;
   i32x4 srd;
-  uint32_t voff, rstride;
-  int wave, kcol;
-  const Operand* op;
-  int64_t row0;
-  __device__ __forceinline__ void init(const Operand& o, int64_t r0, int w, int lane) {
-    op = &o;
-    row0 = r0;
-    wave = w;
-    const int chunk = (lane % 8) ^ (lane / 8);
-    kcol = chunk * 8;
-    rstride = (uint32_t)o.ld * 16;                   // 8 rows
-    voff = (uint32_t)(w * NI) * rstride + (uint32_t)(lane / 8) * (uint32_t)o.ld * 2 + chunk * 16;
-    plane(0);
-  }
-  __device__ __forceinline__ void plane(int p) {
-    srd = make_srd(reinterpret_cast<const char*>(op->p) + p * op->plane + row0 * op->ld * 2,
-                   (op->rows - row0) * op->ld * 2);
-  }
-  __device__ __forceinline__ void issue(uint32_t lds, int ks) {
-    const uint32_t at = ks * kBK + kcol < op->klim ? voff + (uint32_t)ks * (kBK * 2) : kNowhere;
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-      buf_dma16(srd, at == kNowhere ? kNowhere : at + i * rstride,
-                __builtin_amdgcn_readfirstlane(lds + (wave * NI + i) * 1024));
-  }
-  static __device__ __forceinline__ uint4 frag(const unsigned char* s, int f16, int kk, int lane) {
-    return *reinterpret_cast<const uint4*>(s + (f16 * 16 + lane % 16) * 128 +
-                                           (((kk * 4 + lane / 16) ^ (lane & 7)) << 4));
-  }
-};
-
-// COLS columns of 64 rows along k
-template <int COLS, int NW>
-struct ColTile {
-  static constexpr int kBytes = COLS * 128, NI = COLS / 8 / NW;
-  static_assert(COLS % 64 == 0 && (COLS / 8) % NW == 0, "whole copies for every wave");
-  i32x4 srd;
-  uint32_t voff;
-  int wave, cur = 0;
+  uint32_t voff[kCopies], lds;
   const Operand* op;
   int64_t col0;
-  __device__ __forceinline__ static int swz(int k) { return (k & 3) ^ ((k >> 2) & 1); }
-  __device__ __forceinline__ void init(const Operand& o, int64_t c0, int w, int lane) {
+  __device__ __forceinline__ void init(const Operand& o, int64_t c0, int wave, int lane) {
     op = &o;
     col0 = c0;
-    wave = w;
-    const int k = lane / 8, chunk = (lane % 8) ^ (2 * swz(k));
-    voff = (uint32_t)k * (uint32_t)o.ld * 2 + chunk * 16;
-  }
-  __device__ __forceinline__ void plane(int p) { cur = p; }
-  __device__ __forceinline__ void issue(uint32_t lds, int ks) {
-    const int64_t at = ((int64_t)ks * kBK * op->ld + col0) * 2;
-    srd = make_srd(reinterpret_cast<const char*>(op->p) + cur * op->plane + at, op->rows * op->ld * 2 - at);
+    lds = wave * kCopies * 1024;
+    step = o.kb * (2 * KH * 1024);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int f = wave * NI + i;
-      buf_dma16(srd, voff + (uint32_t)(f % 8) * (uint32_t)op->ld * 16 + (uint32_t)(f / 8) * 128,
-                __builtin_amdgcn_readfirstlane(lds + f * 1024));
+    for (int i = 0; i < kCopies; ++i) {
+      const int f = wave * kCopies + i;
+      voff[i] = (lane ^ (4 * (lane / 16))) * 16 +
+                ((uint32_t)(f / kBlocks) * (uint32_t)o.kb + (uint32_t)(f % kBlocks)) * 1024;
     }
   }
-  // k = 32 kk + 16 j + 4 (lane / 16) + r for element 4 j + r, on both sides alike
-  static __device__ __forceinline__ uint4 frag(const unsigned char* s, int f16, int kk, int lane) {
-    const int g = lane / 16, r = (lane % 16) / 4, q = lane % 4;
-    const unsigned char* p = s + (f16 / 4 * 8 + kk * 4 + g / 2) * 1024 + (4 * (g & 1) + r) * 128 +
-                             (((f16 % 4) ^ r ^ (g & 1)) << 5) + q * 8;
+  __device__ __forceinline__ void start(int plane, int64_t ks) {
+    const int64_t at = ks * step + col0 / 32 * 1024;
+    base = (uint64_t)(uintptr_t)op->p + plane * op->plane + at;
+    left = op->rows * op->kb * 1024 - at;
+    srd = make_srd(base, left);
+  }
+  __device__ __forceinline__ void next() {
+    base += step;
+    left -= step;
+    srd = make_srd(base, left);
+  }
+  __device__ __forceinline__ void end() { srd.z = 0; }
+  template <int I> __device__ __forceinline__ void copy(uint32_t to) const {
+    buf_dma16<I * 1024>(srd, voff[I], 0, to + lds);
+  }
+  // columns 32 f .., k = 32 kk + 16 m + 8 (lane / 32) + e
+  static __device__ __forceinline__ uint4 frag(const unsigned char* s, int f, int kk, int m, int lane) {
+    const int r = lane % 16 / 4, q = PERM ? 2 * (lane % 2) + lane % 4 / 2 : lane % 4;   // a row, four columns
+    const int piece = 2 * (lane / 16 % 2) + q / 2;
+    const unsigned char* p = s + ((kk * 2 + m) * kBlocks + f) * 1024 + piece * 256 + q % 2 * 8;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 2048));
+    const int k = 8 * (lane / 32) + r;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (k ^ 4 * piece) * 16));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + ((k + 4) ^ 4 * piece) * 16));
     const uint2 ua = __builtin_bit_cast(uint2, a), ub = __builtin_bit_cast(uint2, b);
     return make_uint4(ua.x, ua.y, ub.x, ub.y);
   }
 };
+template <int COLS, int KH, int NW> using ColTile = ColTileOf<COLS, KH, NW, false>;
+template <int COLS, int KH, int NW> using ColTilePerm = ColTileOf<COLS, KH, NW, true>;
 
 // The pairs of planes that a product of two fp32 activations takes: those of
 // 2^-16 and more, the small ones first.  (What is left out is below 2^-23 of
@@ -205,68 +213,131 @@ __device__ __forceinline__ void tile_of(int64_t gn, int64_t gt, int64_t& tn, int
   tn = l / rows;
 }
 
-// One tile's product.  FN x FT fragments per wave, WN x WT waves; epi is
-// called once per wave with its sums.
-template <template <int, int> class TN, template <int, int> class TT, int FN, int FT, int WN, int WT, class Epi>
+template <int V> struct Int { static constexpr int value = V; };
+template <int N, class F, int I = 0>
+__device__ __forceinline__ void unroll(F&& f) {
+  if constexpr (I < N) {
+    f(Int<I>{});
+    unroll<N, F, I + 1>(static_cast<F&&>(f));
+  }
+}
+template <int N> __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// How a tile is computed: FN x FT blocks of 32 x 32 per wave, WN x WT waves,
+// a ring of R stages of KH blocks of 32 k.
+template <int FN_, int FT_, int WN_, int WT_, int KH_, int R_>
+struct Shape {
+  static constexpr int FN = FN_, FT = FT_, WN = WN_, WT = WT_, KH = KH_, R = R_;
+  static constexpr int NW = WN * WT, BN = WN * FN * 32, BT = WT * FT * 32;
+  static constexpr int kLds = (BN + BT) * 64 * KH * R;
+};
+
+// One tile's product; epi is called once per wave with its sums.
+//
+// The fragments of 16 k are read into registers while those before them are
+// multiplied.  The barrier of a stage stands before its last 16 k's products:
+// by then all its fragments are in registers, so its place in the ring takes
+// the stage R further on, and the next stage, R - 1 stages' products on the
+// way, has landed.  Copies and reads are issued between products, one at a
+// time: in front of them they kept the matrix cores waiting (a weight gradient
+// at T = 8192, C = 4096, H = 11008 1.64 ms).
+template <template <int, int, int> class TN, template <int, int, int> class TT, class S, class Epi>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& a, unsigned char* lds, Epi&& epi) {
-  constexpr int NW = WN * WT, BN = WN * FN * 16, BT = WT * FT * 16;
-  using LN = TN<BN, NW>;
-  using LT = TT<BT, NW>;
-  constexpr int STAGE = LN::kBytes + LT::kBytes;
+  constexpr int FN = S::FN, FT = S::FT, KH = S::KH, R = S::R;
+  using LN = TN<S::BN, KH, S::NW>;
+  using LT = TT<S::BT, KH, S::NW>;
+  constexpr int STAGE = LN::kBytes + LT::kBytes, COPIES = LN::kCopies + LT::kCopies;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int wn = wave % WN, wt = wave / WN;
+  const int wn = wave % S::WN, wt = wave / S::WN;
   int64_t tn, tt;
   tile_of(a.gn, a.gt, tn, tt);
   LN ln;
   LT lt;
-  ln.init(a.n, tn * BN, wave, lane);
-  lt.init(a.t, tt * BT, wave, lane);
+  ln.init(a.n, tn * S::BN, wave, lane);
+  lt.init(a.t, tt * S::BT, wave, lane);
   const uint32_t base = lds_offset(lds);
 
   const int64_t first = blockIdx.y * a.steps_per_split, all = (int64_t)a.ksteps * a.seg.n;
   const int64_t left = all - first;
   const int steps = (int)(left < a.steps_per_split ? left : a.steps_per_split);
   int seg = (int)(first / a.ksteps), ks = (int)(first % a.ksteps);
-  ln.plane(a.seg.a[seg]);
-  lt.plane(a.seg.b[seg]);
-  auto issue = [&](int buf) {
-    ln.issue(base + buf * STAGE, ks);
-    lt.issue(base + buf * STAGE + LN::kBytes, ks);
-    if (++ks == a.ksteps && seg + 1 < a.seg.n) {
+  ln.start(a.seg.a[seg], ks);
+  lt.start(a.seg.b[seg], ks);
+  // copy c of the stage that is next in order, to `to`; after the last of them
+  // the one after is next
+  auto copy = [&](auto c, uint32_t to) {
+    if constexpr (c.value < LN::kCopies)
+      ln.template copy<c.value>(to);
+    else if constexpr (c.value < COPIES)
+      lt.template copy<c.value - LN::kCopies>(to + LN::kBytes);
+  };
+  int ahead = 0;                  // stages copied or on the way
+  auto next = [&] {
+    if (++ahead >= steps) {
+      ln.end();
+      lt.end();
+    } else if (++ks == a.ksteps) {
       ks = 0;
       ++seg;
-      ln.plane(a.seg.a[seg]);
-      lt.plane(a.seg.b[seg]);
+      ln.start(a.seg.a[seg], 0);
+      lt.start(a.seg.b[seg], 0);
+    } else {
+      ln.next();
+      lt.next();
     }
   };
-  f32x4 acc[FN][FT];
+  f32x16 acc[FN][FT];
 #pragma unroll
   for (int i = 0; i < FN; ++i)
 #pragma unroll
-    for (int j = 0; j < FT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  issue(0);
-  for (int it = 0; it < steps; ++it) {
-    // this wave's copies of the stage have landed; after the barrier everyone's,
-    // and nobody reads the other stage any more
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    lds_barrier();
-    if (it + 1 < steps) issue((it + 1) & 1);
-    const unsigned char* sn = lds + (it & 1) * STAGE;
-    const unsigned char* st = sn + LN::kBytes;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      uint4 fn[FN], ft[FT];
-#pragma unroll
-      for (int i = 0; i < FN; ++i) fn[i] = LN::frag(sn, wn * FN + i, kk, lane);
-#pragma unroll
-      for (int j = 0; j < FT; ++j) ft[j] = LT::frag(st, wt * FT + j, kk, lane);
-#pragma unroll
-      for (int j = 0; j < FT; ++j)
-#pragma unroll
-        for (int i = 0; i < FN; ++i) acc[i][j] = mfma_16x16x32(fn[i], ft[j], acc[i][j]);
-    }
+    for (int j = 0; j < FT; ++j) acc[i][j] = f32x16{};
+  // fragments of 16 k, in two sets: one is read while the other is multiplied
+  uint4 frag[2][FN + FT];
+  auto read = [&](int set, const unsigned char* s, int unit, int i) {
+    frag[set][i] = i < FN ? LN::frag(s, wn * FN + i, unit / 2, unit % 2, lane)
+                          : LT::frag(s + LN::kBytes, wt * FT + i - FN, unit / 2, unit % 2, lane);
+  };
+  constexpr int READS = FN + FT, PRODUCTS = FN * FT, UNITS = 2 * KH;
+  constexpr int READ = (READS + PRODUCTS - 1) / PRODUCTS, COPY = (COPIES + PRODUCTS - 1) / PRODUCTS;
+  // The products of one set.  Between them the reads of the other (16 k number
+  // `unit` of the stage at s) and, with `copied`, the copies of the next stage
+  // to `to`: in this order, which the compiler is kept from changing.
+  auto multiply = [&](auto copied, auto set, const unsigned char* s, auto unit, uint32_t to) {
+    __builtin_amdgcn_sched_barrier(0);
+    unroll<PRODUCTS>([&](auto p) {
+      unroll<READ>([&](auto r) {
+        constexpr int i = p.value * READ + r.value;
+        if constexpr (i < READS) read(set.value ^ 1, s, unit.value, i);
+      });
+      constexpr int j = p.value / FN, i = p.value % FN;
+      acc[i][j] = mfma_32x32x16(frag[set.value][i], frag[set.value][FN + j], acc[i][j]);
+      if constexpr (copied.value) unroll<COPY>([&](auto c) { copy(Int<p.value * COPY + c.value>{}, to); });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (copied.value) next();
+  };
+  for (int i = 0; i < R; ++i) {
+    unroll<COPIES>([&](auto c) { copy(c, base + i * STAGE); });
+    next();
   }
-  epi(acc, tn * BN + wn * FN * 16, tt * BT + wt * FT * 16, lane);
+  wait_vm<(R - 1) * COPIES>();
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < READS; ++i) read(0, lds, 0, i);
+  int at = 0;                     // of the current stage in the ring
+  for (int it = 0; it < steps; ++it) {
+    unroll<UNITS - 1>([&](auto u) {
+      multiply(Int<0>{}, Int<u.value % 2>{}, lds + at * STAGE, Int<u.value + 1>{}, 0);
+    });
+    wait_vm<(R - 2) * COPIES>();
+    lds_barrier();
+    const uint32_t to = base + at * STAGE;
+    at = at + 1 == R ? 0 : at + 1;
+    // past the last stage the fragments are those of an old one, and unused
+    multiply(Int<1>{}, Int<(UNITS - 1) % 2>{}, lds + at * STAGE, Int<0>{}, to);
+  }
+  wait_vm<0>();                   // nothing may still come when the LDS is another workgroup's
+  epi(acc, tn * S::BN + wn * FN * 32, tt * S::BT + wt * FT * 32, lane);
 }
 
 }  // namespace xhc

@@ -8,9 +8,8 @@
 // in its epilogue, F; backward dh with the gate's reverse in its epilogue, dx
 // (one product over k = 2 H), [dW_gate | dW_up] and dW_down.  Weights enter as
 // bf16 (packed once a step), sums are fp32.  bf16 state: h, dg and du are
-// rounded to bf16, as operands of the next product, and so are the saved g and
-// u: each rounding (2^-9 of the value) is of the size of the one that F, dx
-// and the weight gradients get as outputs.  fp32 state: activations are
+// rounded to bf16, as operands of the next product: a rounding of the size of
+// the one that F, dx and the weight gradients get as outputs.  fp32 state: activations are
 // multiplied as three bf16 parts that add up to them exactly, so that nothing
 // is rounded below fp32 (three passes over k; six for the weight gradients).
 #include "xhc_ffn.h"
@@ -22,26 +21,22 @@ namespace xhc {
 namespace {
 
 __host__ __device__ constexpr int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-inline int64_t pad_k(int64_t n) { return round_up(n, kBK); }
+inline int64_t pad_k(int64_t n) { return round_up(n, 64); }   // whole stages
 
 // ---------------------------------------------------------------- packing
-// Fragment (nb, kb) of a packed matrix: lane l holds B[n(nb, l % 16)][32 kb + 8 (l / 16) + e].
-// Two blocks of 16 make up 32 n: row p of block a is n = 32 j + 8 (p / 4) + 4 a
-// + p % 4, so that a lane's sums of the two blocks are eight consecutive n.
-// The up projection's blocks come gate, up, gate, up for each 32 columns of h.
-__device__ __forceinline__ int perm_n(int a, int p) { return 8 * (p / 4) + 4 * a + p % 4; }
-
+// The weights' rows (n) are permuted within blocks of 16 (perm_n).  The up
+// projection's blocks come gate, up, gate, up.
 struct PackArgs {
   const float* W;      // [R, Q]
   int64_t R, Q;
-  // n = column, k = row: blocks of 32 columns are nmul blocks of 16 apart, nadd + step * a within
+  // n = column, k = row: block b of 16 columns is block nmul b + nadd
   uint4* kr;
-  int64_t kr_ld;       // k blocks
-  int nmul, nadd, step;
+  int64_t kr_kb;       // k blocks
+  int nmul, nadd;
   // n = row, k = koff + column (NULL: not wanted)
   uint4* kc;
-  int64_t kc_ld, koff;
-  int64_t nr, nc;      // n up to where blocks exist (of 32; values past the matrix are zero)
+  int64_t kc_kb, koff;
+  int64_t nr, nc;      // n up to where blocks exist (values past the matrix are zero)
 };
 
 __device__ __forceinline__ uint32_t pair(uint16_t a, uint16_t b) { return (uint32_t)a | (uint32_t)b << 16; }
@@ -57,28 +52,18 @@ __global__ __launch_bounds__(256) void k_ffn_pack(const PackArgs a) {
   }
   __syncthreads();
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, p = lane % 16, g = lane / 16;
-  // k = row: n blocks of the columns (two 32s of two blocks) x two k blocks
+  // four blocks of 16 n x two of 32 k, each way
 #pragma unroll
   for (int f = 0; f < 2; ++f) {
-    const int id = wave * 2 + f, j = id / 4, blk = id / 2 % 2, kb = id % 2;
-    const int n = 32 * j + perm_n(blk, p), k = 32 * kb + 8 * g;
-    if (q0 + 32 * j < a.nr) {
+    const int blk = wave, kb = f, n = 16 * blk + perm_n(p), k = 32 * kb + 8 * g;
+    if (q0 + 16 * blk < a.nr) {
       const uint4 v = make_uint4(pair(s[k][n], s[k + 1][n]), pair(s[k + 2][n], s[k + 3][n]),
                                  pair(s[k + 4][n], s[k + 5][n]), pair(s[k + 6][n], s[k + 7][n]));
-      const int64_t nb = (q0 / 32 + j) * a.nmul + a.nadd + blk * a.step;
-      a.kr[(nb * a.kr_ld + r0 / 32 + kb) * 64 + lane] = v;
+      a.kr[(((q0 / 16 + blk) * a.nmul + a.nadd) * a.kr_kb + r0 / 32 + kb) * 64 + lane] = v;
     }
-  }
-  if (!a.kc) return;
-#pragma unroll
-  for (int f = 0; f < 2; ++f) {
-    const int id = wave * 2 + f, j = id / 4, blk = id / 2 % 2, kb = id % 2;
-    const int n = 32 * j + perm_n(blk, p), k = 32 * kb + 8 * g;
-    if (r0 + 32 * j < a.nc) {
-      const uint4 v = *reinterpret_cast<const uint4*>(&s[n][k]);
-      const int64_t nb = (r0 / 32 + j) * 2 + blk;
-      a.kc[(nb * a.kc_ld + (a.koff + q0) / 32 + kb) * 64 + lane] = v;
-    }
+    if (a.kc && r0 + 16 * blk < a.nc)
+      a.kc[((r0 / 16 + blk) * a.kc_kb + (a.koff + q0) / 32 + kb) * 64 + lane] =
+          *reinterpret_cast<const uint4*>(&s[n][k]);
   }
 }
 
@@ -129,58 +114,178 @@ __device__ __forceinline__ void split3(float x, float (&p)[3]) {
   p[2] = r - p[1];
 }
 
-// eight values as the operand of a later product: bf16, or the three parts
-template <typename TS> __device__ __forceinline__ void store_operand(uint16_t* p, int64_t plane, const float (&f)[8]);
-template <>
-__device__ __forceinline__ void store_operand<uint16_t>(uint16_t* p, int64_t, const float (&f)[8]) {
-  Vec8<uint16_t>::store(p, f);
+// W = 4 or 8 consecutive values of the state dtype
+template <int W>
+__device__ __forceinline__ void store_vec(uint16_t* p, const float (&f)[W]) {
+  if constexpr (W == 8)
+    Vec8<uint16_t>::store(p, f);
+  else
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2bf(f[0], f[1]), pack2bf(f[2], f[3]));
 }
-template <>
-__device__ __forceinline__ void store_operand<float>(uint16_t* p, int64_t plane, const float (&f)[8]) {
-  float v[3][8];
+template <int W>
+__device__ __forceinline__ void store_vec(float* p, const float (&f)[W]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float q[3];
-    split3(f[e], q);
-    v[0][e] = q[0];
-    v[1][e] = q[1];
-    v[2][e] = q[2];
+  for (int i = 0; i < W; i += 4)
+    *reinterpret_cast<float4*>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+}
+template <int W>
+__device__ __forceinline__ void load_vec(const uint16_t* p, float (&f)[W]) {
+  if constexpr (W == 8) {
+    Vec8<uint16_t>::load(p, f);
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    f[0] = bf_lo(v.x), f[1] = bf_hi(v.x), f[2] = bf_lo(v.y), f[3] = bf_hi(v.y);
   }
+}
+template <int W>
+__device__ __forceinline__ void load_vec(const float* p, float (&f)[W]) {
 #pragma unroll
-  for (int i = 0; i < 3; ++i) Vec8<uint16_t>::store(p + i * plane, v[i]);
+  for (int i = 0; i < W; i += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p + i);
+    f[i] = v.x, f[i + 1] = v.y, f[i + 2] = v.z, f[i + 3] = v.w;
+  }
 }
 
-__global__ __launch_bounds__(256) void k_ffn_split(const float* __restrict__ x, int64_t n8, uint16_t* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;
-  float f[8];
-  Vec8<float>::load(x + i * 8, f);
-  store_operand<float>(out + i * 8, n8 * 8, f);
+// values as the operand of a later product: bf16, or the three parts
+template <typename TS, int W>
+__device__ __forceinline__ void store_operand(uint16_t* p, int64_t plane, const float (&f)[W]) {
+  if constexpr (sizeof(TS) == 2) {
+    store_vec<W>(p, f);
+  } else {
+    float v[3][W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      float q[3];
+      split3(f[e], q);
+      v[0][e] = q[0], v[1][e] = q[1], v[2][e] = q[2];
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) store_vec<W>(p + i * plane, v[i]);
+  }
+}
+
+// g and u as they are saved.  fp32 state: fp32.  bf16 state: 24 bits, the upper
+// 16 of the fp32 value in one plane and the next 8 in another, the rest cut off
+// (less than 2^-15 of the value; in bf16 alone their rounding would double the
+// error of dx and of the weight gradients, which is otherwise that of rounding
+// dg and du and of their own).
+template <typename TS> struct Saved;
+template <> struct Saved<float> {
+  float* p;
+  int64_t n;           // elements of g, in fragments
+  template <int W> struct Raw { float f[W]; };
+  template <int W> __device__ __forceinline__ void store(int which, int64_t i, const float (&f)[W]) const {
+    store_vec<W>(p + which * n + i, f);
+  }
+  template <int W> __device__ __forceinline__ void load(int which, int64_t i, Raw<W>& r) const {
+    load_vec<W>(p + which * n + i, r.f);
+  }
+  template <int W> static __device__ __forceinline__ void unpack(const Raw<W>& r, float (&f)[W]) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) f[e] = r.f[e];
+  }
+};
+template <> struct Saved<uint16_t> {
+  uint16_t* p;         // upper halves of g and u, then bytes of both
+  int64_t n;
+  template <int W> struct Raw { uint32_t hi[W / 2], lo[W / 4]; };
+  template <int W> __device__ __forceinline__ void store(int which, int64_t i, const float (&f)[W]) const {
+    uint32_t hi[W / 2], lo[W / 4];
+#pragma unroll
+    for (int e = 0; e < W; e += 4) {
+      uint32_t u[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) u[x] = __float_as_uint(f[e + x]);
+      hi[e / 2] = __builtin_amdgcn_perm(u[1], u[0], 0x07060302);
+      hi[e / 2 + 1] = __builtin_amdgcn_perm(u[3], u[2], 0x07060302);
+      const uint32_t a = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0501), b = __builtin_amdgcn_perm(u[3], u[2], 0x05010c0c);
+      lo[e / 4] = a | b;
+    }
+    uint16_t* ph = p + which * n + i;
+    uint8_t* pl = reinterpret_cast<uint8_t*>(p + 2 * n) + which * n + i;
+    if constexpr (W == 8) {
+      *reinterpret_cast<uint4*>(ph) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint2*>(pl) = make_uint2(lo[0], lo[1]);
+    } else {
+      *reinterpret_cast<uint2*>(ph) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint32_t*>(pl) = lo[0];
+    }
+  }
+  template <int W> __device__ __forceinline__ void load(int which, int64_t i, Raw<W>& r) const {
+    const uint16_t* ph = p + which * n + i;
+    const uint8_t* pl = reinterpret_cast<const uint8_t*>(p + 2 * n) + which * n + i;
+    if constexpr (W == 8) {
+      const uint4 a = *reinterpret_cast<const uint4*>(ph);
+      const uint2 b = *reinterpret_cast<const uint2*>(pl);
+      r.hi[0] = a.x, r.hi[1] = a.y, r.hi[2] = a.z, r.hi[3] = a.w, r.lo[0] = b.x, r.lo[1] = b.y;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(ph);
+      r.hi[0] = a.x, r.hi[1] = a.y, r.lo[0] = *reinterpret_cast<const uint32_t*>(pl);
+    }
+  }
+  template <int W> static __device__ __forceinline__ void unpack(const Raw<W>& r, float (&f)[W]) {
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+      f[e] = __uint_as_float((e % 2 ? r.hi[e / 2] & 0xffff0000u : r.hi[e / 2] << 16) |
+                             ((r.lo[e / 4] >> (8 * (e % 4))) & 0xffu) << 8);
+  }
+};
+
+// Rows [T, C] into fragments, one wave a fragment; rows up to a whole block and columns up to 64 are zero.  Bound by HBM:
+// each element read once, written once.
+template <typename TS>
+__global__ __launch_bounds__(256) void k_ffn_arrange(const TS* __restrict__ x, int64_t T, int C, int64_t kb,
+                                                     int64_t frags, uint16_t* __restrict__ out) {
+  const int64_t f = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  const int lane = threadIdx.x % 64;
+  if (f >= frags) return;
+  const int64_t t = f / kb * 16 + lane % 16;
+  const int c = (int)(f % kb) * 32 + lane / 16 * 8;
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (t < T && c < C) Vec8<TS>::load(x + t * C + c, v);
+  store_operand<TS, 8>(out + f * 512 + lane * 8, frags * 512, v);
 }
 
 // ---------------------------------------------------------------- epilogues
 
-// h from g and u (eight columns of one token); g and u saved where wanted
+// sums of a token past the last: zero, whatever the weights hold
+template <int W>
+__device__ __forceinline__ void clear(float (&v)[W], float (&w)[W]) {
+#pragma unroll
+  for (int x = 0; x < W; ++x) v[x] = w[x] = 0.f;
+}
+
+// finish is called for the tokens t < rows (whole blocks of 16) and columns c <
+// cols (whole blocks of 64); past T the sums are zero.  What it reads comes
+// through fetch, some calls ahead.
+struct Nothing {};
+
+// h from g and u (W columns of one token); g and u saved where wanted
 template <typename TS>
 struct EpiUp {
   static constexpr bool kTwo = true;
-  int64_t T;
-  int H, cols;         // cols: Hp
+  static constexpr int kParts = sizeof(TS) == 2 ? 1 : 3;   // of an activation as an operand
+  int64_t T, rows;
+  int H, cols;           // cols: Hp
   int act;
   uint16_t* h;
-  int64_t h_plane;
-  TS* saved;           // [2, T, Hp]: g, u
-  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&g)[8], const float (&u)[8]) const {
-    float f[8];
+  Saved<TS> saved;     // p null: not wanted
+  template <int W> using Pre = Nothing;
+  template <int W> __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return Nothing{}; }
+  template <int W>
+  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&g)[W], const float (&u)[W],
+                                         const Nothing&) const {
+    float f[W];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < W; ++e) {
       float d;
       f[e] = c + e < H ? act_of<false>(act, g[e], d) * u[e] : 0.f;
     }
-    store_operand<TS>(h + t * cols + c, h_plane, f);
-    if (saved) {
-      Vec8<TS>::store(saved + t * cols + c, g);
-      Vec8<TS>::store(saved + (T + t) * cols + c, u);
+    const int64_t at = frag_at(t, c, cols / 32);
+    store_operand<TS, W>(h + at, rows * cols, f);
+    if (saved.p) {
+      saved.template store<W>(0, at, g);
+      saved.template store<W>(1, at, u);
     }
   }
 };
@@ -189,11 +294,16 @@ struct EpiUp {
 template <typename TS>
 struct EpiOut {
   static constexpr bool kTwo = false;
-  int64_t T;
+  static constexpr int kParts = sizeof(TS) == 2 ? 1 : 3;
+  int64_t T, rows;
   int cols;
   TS* out;
-  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&v)[8], const float (&)[8]) const {
-    Vec8<TS>::store(out + t * cols + c, v);
+  template <int W> using Pre = Nothing;
+  template <int W> __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return Nothing{}; }
+  template <int W>
+  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&v)[W], const float (&)[W],
+                                         const Nothing&) const {
+    if (t < T) store_vec<W>(out + t * cols + c, v);
   }
 };
 
@@ -201,18 +311,29 @@ struct EpiOut {
 template <typename TS>
 struct EpiGate {
   static constexpr bool kTwo = false;
-  int64_t T;
-  int H, cols;         // cols: Hp
+  static constexpr int kParts = sizeof(TS) == 2 ? 1 : 3;
+  int64_t T, rows;
+  int H, cols;           // cols: Hp
   int act;
-  const TS* saved;
-  uint16_t *dgu, *h;   // [T, 2 Hp], [T, Hp]
-  int64_t dgu_plane, h_plane;
-  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&dh)[8], const float (&)[8]) const {
-    float g[8], u[8], f[8], dg[8], du[8];
-    Vec8<TS>::load(saved + t * cols + c, g);
-    Vec8<TS>::load(saved + (T + t) * cols + c, u);
+  Saved<TS> saved;
+  uint16_t *dgu, *h;   // 2 Hp and Hp columns
+  template <int W> struct Pre { typename Saved<TS>::template Raw<W> g, u; };
+  template <int W> __device__ __forceinline__ Pre<W> fetch(int64_t t, int64_t c) const {
+    Pre<W> r;
+    const int64_t at = frag_at(t, c, cols / 32);
+    saved.template load<W>(0, at, r.g);
+    saved.template load<W>(1, at, r.u);
+    return r;
+  }
+  template <int W>
+  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&dh)[W], const float (&)[W],
+                                         const Pre<W>& r) const {
+    float g[W], u[W], f[W], dg[W], du[W];
+    const int64_t at = frag_at(t, c, cols / 32);
+    Saved<TS>::unpack(r.g, g);
+    Saved<TS>::unpack(r.u, u);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < W; ++e) {
       float d;
       const float a = act_of<true>(act, g[e], d);
       const bool in = c + e < H;
@@ -220,9 +341,9 @@ struct EpiGate {
       dg[e] = in ? dh[e] * u[e] * d : 0.f;
       du[e] = in ? dh[e] * a : 0.f;
     }
-    store_operand<TS>(dgu + t * 2 * cols + c, dgu_plane, dg);
-    store_operand<TS>(dgu + t * 2 * cols + cols + c, dgu_plane, du);
-    store_operand<TS>(h + t * cols + c, h_plane, f);
+    store_operand<TS, W>(dgu + frag_at(t, c, cols / 16), rows * 2 * cols, dg);
+    store_operand<TS, W>(dgu + frag_at(t, cols + c, cols / 16), rows * 2 * cols, du);
+    store_operand<TS, W>(h + at, rows * cols, f);
   }
 };
 
@@ -233,26 +354,20 @@ struct EpiWeight {
   int64_t ncols;       // columns of one output
   int64_t nsplit;      // product columns of the first
   TS *out0, *out1;
-  __device__ __forceinline__ void finish(int64_t m, int64_t n, const float (&v)[4]) const {
+  __device__ __forceinline__ void finish(int64_t m, int64_t n, const float (&v)[8]) const {
     TS* o = out0;
     if (n >= nsplit) {
       n -= nsplit;
       o = out1;
     }
     o += m * ncols + n;
-    if (ncols % 4 == 0) {          // n too: whole groups of four, aligned
-      if (n < ncols) put4(o, v);
+    if (ncols % 8 == 0) {          // n too: whole groups of eight, aligned
+      if (n < ncols) store_vec<8>(o, v);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 8; ++e)
         if (n + e < ncols) put1(o + e, v[e]);
     }
-  }
-  static __device__ __forceinline__ void put4(uint16_t* p, const float (&v)[4]) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]));
-  }
-  static __device__ __forceinline__ void put4(float* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   }
   static __device__ __forceinline__ void put1(uint16_t* p, float v) { *p = (uint16_t)f2bf(v); }
   static __device__ __forceinline__ void put1(float* p, float v) { *p = v; }
@@ -260,41 +375,42 @@ struct EpiWeight {
 
 // ---------------------------------------------------------------- products
 
-// activations [t, k] times packed weights; part: the sums of a part of k, [part][T][cols (x 2)]
-template <int FN, int FT, int WN, int WT, class Epi>
-__global__ __launch_bounds__(64 * WN * WT) void k_ffn_rows(const GemmArgs a, const Epi e, float* __restrict__ part) {
-  __shared__ __align__(1024) unsigned char lds[2 * 128 * 16 * (FN * WN + FT * WT)];
-  gemm_tile<FragTile, RowTile, FN, FT, WN, WT>(a, lds, [&](f32x4 (&acc)[FN][FT], int64_t n0, int64_t t0, int lane) {
-    constexpr int PER = Epi::kTwo ? 4 : 2;       // blocks of 16 that give eight columns
-    static_assert(FN % PER == 0, "whole groups");
-    const int q = lane / 16;
+// activations [t, k] times packed weights; part: the sums of a part of k, [part][rows][cols (x 2)]
+template <class S, class Epi>
+__global__ __launch_bounds__(64 * S::NW) void k_ffn_rows(const GemmArgs a, const Epi e, float* __restrict__ part) {
+  __shared__ __align__(1024) unsigned char lds[S::kLds];
+  gemm_tile<FragTile, FragTile, S>(a, lds, [&](f32x16 (&acc)[S::FN][S::FT], int64_t n0, int64_t t0, int lane) {
+    // 32 tokens by 16 columns at a time, fetched some ahead
+    constexpr int NB = S::FN * (Epi::kTwo ? 1 : 2), ALL = S::FT * NB, AHEAD = Epi::kParts == 1 ? 4 : 2;
+    const bool whole = gridDim.y == 1;
+    const int64_t c0 = (Epi::kTwo ? n0 / 2 : n0) + lane / 32 * 8;
+    t0 += lane % 32;
+    typename Epi::template Pre<8> pre[AHEAD];
+    const auto inside = [&](int q) { return t0 + q / NB * 32 < e.rows && c0 + q % NB * 16 < e.cols; };
+    const auto fetch = [&](int q) {
+      if (whole && inside(q)) pre[q % AHEAD] = e.template fetch<8>(t0 + q / NB * 32, c0 + q % NB * 16);
+    };
 #pragma unroll
-    for (int j = 0; j < FT; ++j) {
-      const int64_t t = t0 + j * 16 + lane % 16;
+    for (int q = 0; q < AHEAD - 1; ++q) fetch(q);
 #pragma unroll
-      for (int i = 0; i < FN / PER; ++i) {
-        const int64_t c = (Epi::kTwo ? n0 / 2 : n0) + i * 32 + q * 8;
-        if (t >= e.T || c >= e.cols) continue;
-        float v[8], w[8];
+    for (int q = 0; q < ALL; ++q) {
+      if (q + AHEAD - 1 < ALL) fetch(q + AHEAD - 1);
+      if (!inside(q)) continue;
+      const int j = q / NB, i = q % NB;
+      const int64_t t = t0 + j * 32, c = c0 + i * 16;
+      float v[8], w[8];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          if (Epi::kTwo) {
-            v[x] = acc[4 * i][j][x];
-            w[x] = acc[4 * i + 1][j][x];
-            v[4 + x] = acc[4 * i + 2][j][x];
-            w[4 + x] = acc[4 * i + 3][j][x];
-          } else {
-            v[x] = acc[2 * i][j][x];
-            v[4 + x] = acc[2 * i + 1][j][x];
-          }
-        }
-        if (gridDim.y > 1) {
-          float* p = part + ((int64_t)blockIdx.y * e.T + t) * e.cols * (Epi::kTwo ? 2 : 1) + c;
-          Vec8<float>::store(p, v);
-          if (Epi::kTwo) Vec8<float>::store(p + e.cols, w);
-        } else {
-          e.finish(t, c, v, w);
-        }
+      for (int x = 0; x < 8; ++x) {
+        v[x] = Epi::kTwo ? acc[i][j][x] : acc[i / 2][j][i % 2 * 8 + x];
+        w[x] = Epi::kTwo ? acc[i][j][8 + x] : 0.f;
+      }
+      if (t >= e.T) clear<8>(v, w);
+      if (whole) {
+        e.template finish<8>(t, c, v, w, pre[q % AHEAD]);
+      } else {
+        float* p = part + ((int64_t)blockIdx.y * e.rows + t) * e.cols * (Epi::kTwo ? 2 : 1) + c;
+        Vec8<float>::store(p, v);
+        if (Epi::kTwo) Vec8<float>::store(p + e.cols, w);
       }
     }
   });
@@ -305,10 +421,11 @@ template <class Epi>
 __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float* __restrict__ part, int parts) {
   const int64_t g = e.cols / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t t = i / g, c = i % g * 8, ld = (int64_t)e.cols * (Epi::kTwo ? 2 : 1);
-  if (t >= e.T) return;
+  if (t >= e.rows) return;
+  const auto pre = e.template fetch<8>(t, c);
   float v[8] = {}, w[8] = {};
   for (int p = 0; p < parts; ++p) {
-    const float* s = part + ((int64_t)p * e.T + t) * ld + c;
+    const float* s = part + ((int64_t)p * e.rows + t) * ld + c;
     float f[8];
     Vec8<float>::load(s, f);
 #pragma unroll
@@ -319,25 +436,130 @@ __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float*
       for (int x = 0; x < 8; ++x) w[x] += f[x];
     }
   }
-  e.finish(t, c, v, w);
+  e.template finish<8>(t, c, v, w, pre);
+}
+
+// Few tokens (up to 16 MB): bound by the weights' bytes, which go from memory
+// straight to registers, a fragment (1 KiB) a load.  A workgroup takes FR
+// blocks of 16 n, its waves a part of k each, and keeps about 128 KiB of
+// weights in flight: two sets of U k blocks per wave, one under way while the
+// other is multiplied.  The waves' sums are added through LDS in order.  Tokens
+// past the last read it again.
+struct FewArgs {
+  const uint4* w;      // packed
+  int64_t wkb;         // its k blocks
+  int kb;              // k blocks of the activations
+  const uint16_t* x;   // rows [T, ldx] (ldx > 0) or fragments; one or three planes
+  int64_t ldx, plane;  // elements
+  int T;
+};
+template <int FR, int MB, int NW, int U, class Epi>
+__global__ __launch_bounds__(64 * NW) void k_ffn_few(const FewArgs a, const Epi e) {
+  constexpr int P = Epi::kParts, PER = Epi::kTwo ? 2 : 1;
+  static_assert(FR % PER == 0, "gate and up together");
+  __shared__ f32x4 red[NW][FR * MB][64];
+  // wave from a scalar register: a matrix instruction heeds no lane mask, so
+  // what it runs under has to be a real branch
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint4* w = a.w + (int64_t)blockIdx.x * FR * a.wkb * 64 + lane;
+  const uint16_t* x[MB];
+  const int xk = a.ldx ? 32 : 512;       // elements between k blocks
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    const int t = m * 16 + lane % 16 < a.T ? m * 16 + lane % 16 : a.T - 1;
+    x[m] = a.x + (a.ldx ? t * a.ldx + lane / 16 * 8 : frag_at(t, lane / 16 * 8, a.kb));
+  }
+  f32x4 acc[FR][MB];
+#pragma unroll
+  for (int f = 0; f < FR; ++f)
+#pragma unroll
+    for (int m = 0; m < MB; ++m) acc[f][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int k0 = (int)((int64_t)a.kb * wave / NW), k1 = (int)((int64_t)a.kb * (wave + 1) / NW);
+  uint4 wr[2][U][FR], xr[2][U][MB][P];
+  // past the part's end the last block again, with zero weights
+  auto load = [&](int b, int k) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kk = k + u < k1 ? k + u : k1 - 1;
+#pragma unroll
+      for (int f = 0; f < FR; ++f) wr[b][u][f] = w[(f * a.wkb + kk) * 64];
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          xr[b][u][m][p] = *reinterpret_cast<const uint4*>(x[m] + p * a.plane + (int64_t)kk * xk);
+    }
+  };
+  auto multiply = [&](int b, int k) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k + u < k1) {
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+          for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int f = 0; f < FR; ++f) acc[f][m] = mfma_16x16x32(wr[b][u][f], xr[b][u][m][p], acc[f][m]);
+      }
+    }
+  };
+  if (k0 < k1) {
+    load(0, k0);
+    for (int k = k0; k < k1; k += 2 * U) {
+      if (k + U < k1) load(1, k + U);
+      multiply(0, k);
+      if (k + U < k1) {
+        if (k + 2 * U < k1) load(0, k + 2 * U);
+        multiply(1, k + U);
+      }
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < FR; ++f)
+#pragma unroll
+    for (int m = 0; m < MB; ++m) red[wave][f * MB + m][lane] = acc[f][m];
+  __syncthreads();
+  // a wave finishes every NW-th of the (block, 16 tokens) pairs
+  for (int i = wave; i < FR / PER * MB; i += NW) {
+    const int f = i / MB * PER, m = i % MB, t = m * 16 + lane % 16;
+    float v[4], u[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = u[c] = 0.f;
+    for (int n = 0; n < NW; ++n) {
+      const f32x4 r = red[n][f * MB + m][lane];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] += r[c];
+      if (Epi::kTwo) {
+        const f32x4 s = red[n][(f + 1) * MB + m][lane];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) u[c] += s[c];
+      }
+    }
+    const int q = lane / 16;                               // rows 4 q .. + 4 of the block
+    const int64_t c = ((int64_t)blockIdx.x * FR + f) / PER * 16 + perm_n(4 * q);
+    if (t >= a.T) clear<4>(v, u);
+    if (t < e.rows && c < e.cols) e.template finish<4>(t, c, v, u, e.template fetch<4>(t, c));
+  }
 }
 
 // weight gradients: k is the token on both sides; part: [part][M][N]
-template <int FN, int FT, int WN, int WT, class Epi>
-__global__ __launch_bounds__(64 * WN * WT) void k_ffn_cols(const GemmArgs a, const Epi e, float* __restrict__ part) {
-  __shared__ __align__(1024) unsigned char lds[2 * 128 * 16 * (FN * WN + FT * WT)];
-  gemm_tile<ColTile, ColTile, FN, FT, WN, WT>(a, lds, [&](f32x4 (&acc)[FN][FT], int64_t n0, int64_t t0, int lane) {
+template <class S, class Epi>
+__global__ __launch_bounds__(64 * S::NW) void k_ffn_cols(const GemmArgs a, const Epi e, float* __restrict__ part) {
+  __shared__ __align__(1024) unsigned char lds[S::kLds];
+  gemm_tile<ColTilePerm, ColTile, S>(a, lds, [&](f32x16 (&acc)[S::FN][S::FT], int64_t n0, int64_t t0, int lane) {
 #pragma unroll
-    for (int j = 0; j < FT; ++j) {
-      const int64_t m = t0 + j * 16 + lane % 16;
+    for (int j = 0; j < S::FT; ++j) {
+      const int64_t m = t0 + j * 32 + lane % 32;
+      if (m >= e.M) continue;
 #pragma unroll
-      for (int i = 0; i < FN; ++i) {
-        const int64_t n = n0 + i * 16 + lane / 16 * 4;
-        if (m >= e.M || n >= e.N) continue;
-        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+      for (int i = 0; i < S::FN * 2; ++i) {
+        const int64_t n = n0 + i * 16 + lane / 32 * 8;
+        if (n >= e.N) continue;
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = acc[i / 2][j][i % 2 * 8 + x];
         if (gridDim.y > 1)
-          *reinterpret_cast<float4*>(part + ((int64_t)blockIdx.y * e.M + m) * e.N + n) =
-              make_float4(v[0], v[1], v[2], v[3]);
+          Vec8<float>::store(part + ((int64_t)blockIdx.y * e.M + m) * e.N + n, v);
         else
           e.finish(m, n, v);
       }
@@ -347,38 +569,76 @@ __global__ __launch_bounds__(64 * WN * WT) void k_ffn_cols(const GemmArgs a, con
 
 template <class Epi>
 __global__ __launch_bounds__(256) void k_ffn_cols_join(const Epi e, const float* __restrict__ part, int parts) {
-  const int64_t g = e.N / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t m = i / g, n = i % g * 4;
+  const int64_t g = e.N / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t m = i / g, n = i % g * 8;
   if (m >= e.M) return;
-  float v[4] = {};
+  float v[8] = {};
   for (int p = 0; p < parts; ++p) {
-    const float4 f = *reinterpret_cast<const float4*>(part + ((int64_t)p * e.M + m) * e.N + n);
-    v[0] += f.x;
-    v[1] += f.y;
-    v[2] += f.z;
-    v[3] += f.w;
+    float f[8];
+    Vec8<float>::load(part + ((int64_t)p * e.M + m) * e.N + n, f);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] += f[x];
   }
   e.finish(m, n, v);
 }
 
 // ---------------------------------------------------------------- host side
 
+// Rings of 128 KiB in LDS, or 80 and 64 where two workgroups share a CU.  (In us,
+// T = 8192, C = 4096, H = 11008: four stages of 32 k or two of 64 in a large
+// tile up 1252 or 1293, dW_gate and dW_up 1249 or 1309; T = 512, C = 2560, H =
+// 6912: five of 32 or two of 64 in a small one dx 120 or 176, dW_gate and dW_up
+// 63 or 58.)
+using Large = Shape<2, 4, 4, 2, 1, 4>;
+using SmallRows = Shape<2, 2, 2, 2, 1, 5>;
+using SmallCols = Shape<2, 2, 2, 2, 2, 2>;
+
 // How a product runs: its tile and the parts that k is cut into.
 struct Plan {
-  int bn, bt;
-  int64_t gn, gt, ksteps, per;   // per: stages of a part
+  int64_t tile, gn, gt, ksteps, per;   // per: stages of a part
   int nseg, parts;
 };
-Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg) {
-  Plan p{};
-  p.bn = p.bt = 128;
-  p.gn = (n + p.bn - 1) / p.bn;
-  p.gt = (t + p.bt - 1) / p.bt;
-  p.ksteps = std::max<int64_t>(1, (k + kBK - 1) / kBK);   // no tokens: one stage of zeros
-  p.nseg = nseg;
-  p.parts = 1;
-  p.per = p.ksteps * nseg;
-  return p;
+// Tiles of 256 x 256 (a workgroup per CU) or 128 x 128 (two), the latter with k
+// in parts where there are few of them; by an estimate of the time in us.
+// Measured per 32 k and round: a large tile 0.8 on a full chip, below half of it
+// 0.6 (power); small ones 0.57, 0.5 where not every CU has two, 0.3 where none
+// has.  Parts cost a write and a read of fp32 sums and a launch: T = 512, C =
+// 2560, H = 6912 dx (80 small tiles of 432 steps) 242 us with large tiles, 120
+// with small ones, 66 in 4 parts.
+Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64_t out) {
+  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  Plan best{};
+  double least = 0;
+  for (const int64_t tile : {(int64_t)256, (int64_t)128}) {
+    Plan p{};
+    p.tile = tile;
+    p.gn = up(n, tile);
+    p.gt = up(t, tile);
+    p.nseg = nseg;
+    const int stage = tile == 256 ? 32 : stage128;
+    p.ksteps = std::max<int64_t>(1, up(k, stage));   // no tokens: one stage of zeros
+    const int64_t steps = p.ksteps * nseg, tiles = p.gn * p.gt;
+    for (int parts = 1; parts <= (tile == 256 ? 1 : 32); ++parts) {
+      p.per = up(steps, parts);
+      p.parts = (int)up(steps, p.per);
+      if (p.parts != parts) continue;
+      const int64_t w = tiles * parts;
+      double rounds;
+      if (tile == 256) {
+        rounds = w <= 128 ? 0.6 : 0.8 * up(w, 256);
+      } else {
+        const int64_t rest = w % 512;
+        rounds = 0.57 * (w / 512) + (rest == 0 ? 0 : rest <= 256 ? 0.3 : 0.5);
+      }
+      double us = rounds * p.per * (stage / 32) + 3;
+      if (parts > 1) us += 4 + (double)parts * out * 8 / 3.5e6;
+      if (least == 0 || us < least) {
+        least = us;
+        best = p;
+      }
+    }
+  }
+  return best;
 }
 size_t part_floats(const Plan& p, int64_t t, int64_t cols) { return p.parts > 1 ? (size_t)p.parts * t * cols : 0; }
 
@@ -386,20 +646,57 @@ GemmArgs args_of(const Plan& p, const Operand& n, const Operand& t, const Segmen
   return GemmArgs{n, t, seg, (int)p.ksteps, p.per, p.gn, p.gt};
 }
 
+// Up to so many tokens k_ffn_few runs, and reads an input of bf16 rows as it lies.
+constexpr int kFewTokens = 64;
+// all n blocks of the packed matrix a.n; ldx: elements between rows of the activations, 0 for fragments
 template <class Epi>
-hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hipStream_t s) {
-  k_ffn_rows<4, 4, 2, 2, Epi><<<dim3((unsigned)(p.gn * p.gt), (unsigned)p.parts), dim3(256), 0, s>>>(a, e, part);
+hipError_t few(const GemmArgs& a, int64_t ldx, const Epi& e, hipStream_t s) {
+  const FewArgs f{reinterpret_cast<const uint4*>(a.n.p), a.n.kb, (int)a.t.kb,
+                  reinterpret_cast<const uint16_t*>(a.t.p), ldx, a.t.plane / 2, (int)e.T};
+  // Blocks of 16 n per workgroup: one (with its gate's: two) up to 16 tokens,
+  // twice as many beyond, where the activations' bytes count, too.  Waves: 16,
+  // for the most loads in flight where there are few blocks; fewer where their
+  // sums would not fit LDS (gate and up) or their fragments the registers that
+  // 16 waves have (three-part activations).
+  constexpr bool two = Epi::kTwo, f32 = Epi::kParts == 3;
+  constexpr int PER = two ? 2 : 1;
+  const unsigned g1 = (unsigned)(a.n.rows / PER), g2 = g1 / 2;
+  if (e.T <= 16) {
+    constexpr int NW = two ? 8 : 16;
+    k_ffn_few<PER, 1, NW, f32 ? 2 : 4, Epi><<<dim3(g1), dim3(64 * NW), 0, s>>>(f, e);
+  } else if (e.T <= 32) {
+    constexpr int NW = two ? 8 : 16;
+    k_ffn_few<2 * PER, 2, NW, f32 ? 1 : 2, Epi><<<dim3(g2), dim3(64 * NW), 0, s>>>(f, e);
+  } else {
+    constexpr int NW = two ? 4 : f32 ? 8 : 16;
+    k_ffn_few<2 * PER, 4, NW, two && !f32 ? 2 : 1, Epi><<<dim3(g2), dim3(64 * NW), 0, s>>>(f, e);
+  }
+  return hipGetLastError();
+}
+
+template <class Epi>
+hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hipStream_t s, int64_t ldx = 0) {
+  if (e.T <= kFewTokens) return few(a, ldx, e, s);
+  const dim3 grid((unsigned)(p.gn * p.gt), (unsigned)p.parts);
+  if (p.tile == 256)
+    k_ffn_rows<Large, Epi><<<grid, dim3(64 * Large::NW), 0, s>>>(a, e, part);
+  else
+    k_ffn_rows<SmallRows, Epi><<<grid, dim3(64 * SmallRows::NW), 0, s>>>(a, e, part);
   if (p.parts > 1) {
-    const int64_t n = e.T * (e.cols / 8);
+    const int64_t n = e.rows * (e.cols / 8);
     k_ffn_rows_join<Epi><<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(e, part, p.parts);
   }
   return hipGetLastError();
 }
 template <class Epi>
 hipError_t cols(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hipStream_t s) {
-  k_ffn_cols<4, 4, 2, 2, Epi><<<dim3((unsigned)(p.gn * p.gt), (unsigned)p.parts), dim3(256), 0, s>>>(a, e, part);
+  const dim3 grid((unsigned)(p.gn * p.gt), (unsigned)p.parts);
+  if (p.tile == 256)
+    k_ffn_cols<Large, Epi><<<grid, dim3(64 * Large::NW), 0, s>>>(a, e, part);
+  else
+    k_ffn_cols<SmallCols, Epi><<<grid, dim3(64 * SmallCols::NW), 0, s>>>(a, e, part);
   if (p.parts > 1) {
-    const int64_t n = e.M * (e.N / 4);
+    const int64_t n = e.M * (e.N / 8);
     k_ffn_cols_join<Epi><<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(e, part, p.parts);
   }
   return hipGetLastError();
@@ -407,45 +704,54 @@ hipError_t cols(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hip
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// the workspace: the fp32 state's parts of x (and dF), h, [dg|du], parts of k
+// the workspace: x and dF in fragments, h, [dg|du], parts of k
 struct Ws {
   Plan up, down, dh, dx, dwgu, dwd;
+  int64_t rows;                  // tokens in whole blocks
   size_t x, dF, h, dgu, part, total;
   Ws(int state_dtype, int64_t T, int64_t C, int64_t H, bool bwd) {
     const Packed pk(C, H);
     const bool f32 = state_dtype == XHC_F32;
     const int P = f32 ? 3 : 1, ns = f32 ? 3 : 1, nw = f32 ? 6 : 1;
+    rows = round_up(T, 16);
     size_t at = 0;
     const auto take = [&](size_t bytes) {
       const size_t o = at;
       at += align256(bytes);
       return o;
     };
-    x = take(f32 ? (size_t)P * T * C * 2 : 0);
-    dF = take(f32 && bwd ? (size_t)P * T * C * 2 : 0);
-    h = take((size_t)P * T * pk.Hp * 2);
-    dgu = take(bwd ? (size_t)P * T * pk.Hp * 4 : 0);
+    x = take((size_t)P * rows * pk.Cp * 2);
+    dF = take(bwd ? (size_t)P * rows * pk.Cp * 2 : 0);
+    h = take((size_t)P * rows * pk.Hp * 2);
+    dgu = take(bwd ? (size_t)P * rows * pk.Hp * 4 : 0);
     size_t most = 0;
     if (bwd) {
-      dh = plan_product(pk.Hp, T, C, ns);
-      dx = plan_product(C, T, 2 * pk.Hp, ns);
-      dwgu = plan_product(2 * pk.Hp, C, T, nw);
-      dwd = plan_product(C, H, T, nw);
-      most = std::max({part_floats(dh, T, pk.Hp), part_floats(dx, T, C), part_floats(dwgu, C, 2 * pk.Hp),
+      dh = plan_product(pk.Hp, T, pk.Cp, ns, 32, rows * pk.Hp);
+      dx = plan_product(C, T, 2 * pk.Hp, ns, 32, rows * C);
+      dwgu = plan_product(2 * pk.Hp, C, T, nw, 64, C * 2 * pk.Hp);
+      dwd = plan_product(C, H, T, nw, 64, H * C);
+      most = std::max({part_floats(dh, rows, pk.Hp), part_floats(dx, rows, C), part_floats(dwgu, C, 2 * pk.Hp),
                        part_floats(dwd, H, C)});
     } else {
-      up = plan_product(2 * pk.Hp, T, C, ns);
-      down = plan_product(C, T, pk.Hp, ns);
-      most = std::max(part_floats(up, T, 2 * pk.Hp), part_floats(down, T, C));
+      up = plan_product(2 * pk.Hp, T, pk.Cp, ns, 32, rows * 2 * pk.Hp);
+      down = plan_product(C, T, pk.Hp, ns, 32, rows * C);
+      most = std::max(part_floats(up, rows, 2 * pk.Hp), part_floats(down, rows, C));
     }
     part = take(most * sizeof(float));
     total = at;
   }
 };
 
-hipError_t split_planes(const float* x, int64_t n, void* out, hipStream_t s) {
-  if (n == 0) return hipSuccess;
-  k_ffn_split<<<dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, s>>>(x, n / 8, reinterpret_cast<uint16_t*>(out));
+Operand weight(const void* p, int64_t nb, int64_t kb) { return Operand{p, 0, nb, kb}; }
+Operand activation(const void* p, int64_t kb, int64_t tb) { return Operand{p, tb * kb * 1024, tb, kb}; }
+
+// rows in fragments
+template <typename TS>
+hipError_t arrange(const void* x, int64_t T, int64_t C, int64_t kb, void* out, hipStream_t s) {
+  const int64_t frags = (T + 15) / 16 * kb;
+  if (frags == 0) return hipSuccess;
+  k_ffn_arrange<TS><<<dim3((unsigned)((frags + 3) / 4)), dim3(256), 0, s>>>(
+      reinterpret_cast<const TS*>(x), T, (int)C, kb, frags, reinterpret_cast<uint16_t*>(out));
   return hipGetLastError();
 }
 
@@ -454,26 +760,23 @@ hipError_t ffn(int state_dtype, int64_t T, int64_t C, int64_t H, int act, const 
                void* F, void* saved, void* workspace, hipStream_t s) {
   const Packed pk(C, H);
   const Ws w(state_dtype, T, C, H, false);
-  const bool f32 = state_dtype == XHC_F32;
+  const bool f32 = state_dtype == XHC_F32, direct = !f32 && T <= kFewTokens;
   char* ws = reinterpret_cast<char*>(workspace);
   const char* pw = reinterpret_cast<const char*>(packed);
   const Segments seg = f32 ? segs_weights() : segs_bf16();
+  const int64_t tb = w.rows / 16, kc = pk.Cp / 32, kh = pk.Hp / 32;
   float* part = reinterpret_cast<float*>(ws + w.part);
   uint16_t* h = reinterpret_cast<uint16_t*>(ws + w.h);
-  const void* x = input;
-  hipError_t e = hipSuccess;
-  if (f32) {
-    x = ws + w.x;
-    e = split_planes(reinterpret_cast<const float*>(input), T * C, ws + w.x, s);
-  }
+  hipError_t e = direct ? hipSuccess : arrange<TS>(input, T, C, kc, ws + w.x, s);
+  const Operand ox = direct ? Operand{input, 0, tb, C / 32} : activation(ws + w.x, kc, tb);
   if (e == hipSuccess)
-    e = rows(w.up, args_of(w.up, Operand{pw + pk.up, 0, pk.Cp / 32, pk.n32H * 4, 0},
-                           Operand{x, T * C * 2, C, T, (int)C}, seg),
-             EpiUp<TS>{T, (int)H, (int)pk.Hp, act, h, T * pk.Hp, reinterpret_cast<TS*>(saved)}, part, s);
+    e = rows(w.up, args_of(w.up, weight(pw + pk.up, pk.n32H * 4, kc), ox, seg),
+             EpiUp<TS>{T, w.rows, (int)H, (int)pk.Hp, act, h,
+                       Saved<TS>{reinterpret_cast<TS*>(saved), w.rows * pk.Hp}},
+             part, s, direct ? C : 0);
   if (e == hipSuccess)
-    e = rows(w.down, args_of(w.down, Operand{pw + pk.down, 0, pk.Hp / 32, pk.n32C * 2, 0},
-                             Operand{h, T * pk.Hp * 2, pk.Hp, T, (int)pk.Hp}, seg),
-             EpiOut<TS>{T, (int)C, reinterpret_cast<TS*>(F)}, part, s);
+    e = rows(w.down, args_of(w.down, weight(pw + pk.down, pk.n32C * 2, kh), activation(h, kh, tb), seg),
+             EpiOut<TS>{T, w.rows, (int)C, reinterpret_cast<TS*>(F)}, part, s);
   return e;
 }
 
@@ -487,27 +790,21 @@ hipError_t ffn_bwd(int state_dtype, int64_t T, int64_t C, int64_t H, int act, co
   char* ws = reinterpret_cast<char*>(workspace);
   const char* pw = reinterpret_cast<const char*>(packed);
   const Segments sw = f32 ? segs_weights() : segs_bf16(), sa = f32 ? segs_f32() : segs_bf16();
+  const int64_t tb = w.rows / 16, kc = pk.Cp / 32, kh = pk.Hp / 32;
   float* part = reinterpret_cast<float*>(ws + w.part);
   uint16_t *h = reinterpret_cast<uint16_t*>(ws + w.h), *dgu = reinterpret_cast<uint16_t*>(ws + w.dgu);
-  const void *x = input, *df = dF;
-  hipError_t e = hipSuccess;
-  if (f32) {
-    x = ws + w.x;
-    df = ws + w.dF;
-    e = split_planes(reinterpret_cast<const float*>(input), T * C, ws + w.x, s);
-    if (e == hipSuccess) e = split_planes(reinterpret_cast<const float*>(dF), T * C, ws + w.dF, s);
-  }
-  const Operand ox{x, T * C * 2, C, T, (int)C}, odf{df, T * C * 2, C, T, (int)C};
-  const Operand oh{h, T * pk.Hp * 2, pk.Hp, T, (int)pk.Hp};
-  const Operand odgu{dgu, T * pk.Hp * 4, 2 * pk.Hp, T, (int)(2 * pk.Hp)};
+  hipError_t e = arrange<TS>(input, T, C, kc, ws + w.x, s);
+  if (e == hipSuccess) e = arrange<TS>(dF, T, C, kc, ws + w.dF, s);
+  const Operand ox = activation(ws + w.x, kc, tb), odf = activation(ws + w.dF, kc, tb);
+  const Operand oh = activation(h, kh, tb), odgu = activation(dgu, 2 * kh, tb);
   if (e == hipSuccess && T > 0)
-    e = rows(w.dh, args_of(w.dh, Operand{pw + pk.dh, 0, pk.Cp / 32, pk.n32H * 2, 0}, odf, sw),
-             EpiGate<TS>{T, (int)H, (int)pk.Hp, act, reinterpret_cast<const TS*>(saved), dgu, h, T * 2 * pk.Hp,
-                         T * pk.Hp},
+    e = rows(w.dh, args_of(w.dh, weight(pw + pk.dh, pk.n32H * 2, kc), odf, sw),
+             EpiGate<TS>{T, w.rows, (int)H, (int)pk.Hp, act,
+                         Saved<TS>{const_cast<TS*>(reinterpret_cast<const TS*>(saved)), w.rows * pk.Hp}, dgu, h},
              part, s);
   if (e == hipSuccess && T > 0)
-    e = rows(w.dx, args_of(w.dx, Operand{pw + pk.dx, 0, 2 * pk.Hp / 32, pk.n32C * 2, 0}, odgu, sw),
-             EpiOut<TS>{T, (int)C, reinterpret_cast<TS*>(d_input)}, part, s);
+    e = rows(w.dx, args_of(w.dx, weight(pw + pk.dx, pk.n32C * 2, 2 * kh), odgu, sw),
+             EpiOut<TS>{T, w.rows, (int)C, reinterpret_cast<TS*>(d_input)}, part, s);
   if (e == hipSuccess)
     e = cols(w.dwgu, args_of(w.dwgu, odgu, ox, sa),
              EpiWeight<TS>{C, 2 * pk.Hp, H, pk.Hp, reinterpret_cast<TS*>(dW_gate), reinterpret_cast<TS*>(dW_up)},
@@ -525,7 +822,7 @@ size_t ffn_packed_bytes(int64_t C, int64_t H, bool with_bwd) {
   return with_bwd ? p.total : p.total_fwd;
 }
 size_t ffn_saved_bytes(int state_dtype, int64_t T, int64_t H) {
-  return (size_t)2 * T * pad_k(H) * (state_dtype == XHC_F32 ? 4 : 2);
+  return (size_t)2 * round_up(T, 16) * pad_k(H) * (state_dtype == XHC_F32 ? 4 : 3);
 }
 size_t ffn_ws_bytes(int state_dtype, int64_t T, int64_t C, int64_t H, bool bwd) {
   return Ws(state_dtype, T, C, H, bwd).total;
@@ -538,10 +835,10 @@ hipError_t launch_ffn_pack(int64_t C, int64_t H, const float* W_gate, const floa
   const auto at = [&](size_t o) { return reinterpret_cast<uint4*>(b + o); };
   const unsigned tc = (unsigned)(p.Cp / 64), th = (unsigned)(p.Hp / 64);
   for (int i = 0; i < 2; ++i)
-    k_ffn_pack<<<dim3(th, tc), dim3(256), 0, s>>>(PackArgs{i ? W_up : W_gate, C, H, at(p.up), p.Cp / 32, 4, i, 2,
+    k_ffn_pack<<<dim3(th, tc), dim3(256), 0, s>>>(PackArgs{i ? W_up : W_gate, C, H, at(p.up), p.Cp / 32, 2, i,
                                                            with_bwd ? at(p.dx) : nullptr, 2 * p.Hp / 32, i * p.Hp,
                                                            p.Hp, C});
-  k_ffn_pack<<<dim3(tc, th), dim3(256), 0, s>>>(PackArgs{W_down, H, C, at(p.down), p.Hp / 32, 2, 0, 1,
+  k_ffn_pack<<<dim3(tc, th), dim3(256), 0, s>>>(PackArgs{W_down, H, C, at(p.down), p.Hp / 32, 1, 0,
                                                          with_bwd ? at(p.dh) : nullptr, p.Cp / 32, 0, C, p.Hp});
   return hipGetLastError();
 }

@@ -2,8 +2,9 @@
 the CPU, with bounds on what a right kernel may be off, value by value.
 
 Bounds count roundings: HALF = half a step of the state dtype relative to the
-value for each rounding to it (outputs; with a bf16 state also h, the saved g
-and u, dg and du), and for fp32 arithmetic one 2^-24 per operation of the
+value for each rounding to it (outputs; with a bf16 state also h, dg and du),
+2^-15 for the saved g and u of a bf16 state (16 of their 24 significant bits
+are kept, the rest is cut off), and for fp32 arithmetic one 2^-24 per operation of the
 longest chain, i.e. (K + a few) 2^-24 of the sum of absolute products over K
 terms, whatever their order."""
 
@@ -52,7 +53,7 @@ def ffn_backward(x, dF, fw, kind, half):
     (g, eg), (u, eu) = fw["g"], fw["u"]
     C, H = Wg.shape
     T = x.shape[0]
-    save = half if half > U else 0.0
+    save = 2.0 ** -15 if half > U else 0.0
     eg, eu = eg + save * (g.abs() + eg), eu + save * (u.abs() + eu)
     a, da = fw["a"], fw["da"]
     dh = dF @ Wd.t()
