@@ -90,9 +90,9 @@ struct Packed {
 template <bool D>
 __device__ __forceinline__ float act_of(int act, float g, float& d) {
   if (act == XHC_ACT_SILU) {
-    const float e = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
-    if (D) d = e * (1.0f + g * (1.0f - e));
-    return g * e;
+    const float e = __builtin_amdgcn_rcpf(1.0f + __expf(-g)), a = g * e;
+    if (D) d = fmaf(a, 1.0f - e, e);
+    return a;
   }
   const float e = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
   if (D) d = e + g * __expf(-0.5f * g * g) * 0.39894228040143268f;
@@ -225,9 +225,9 @@ template <> struct Saved<uint16_t> {
   }
   template <int W> static __device__ __forceinline__ void unpack(const Raw<W>& r, float (&f)[W]) {
 #pragma unroll
-    for (int e = 0; e < W; ++e)
-      f[e] = __uint_as_float((e % 2 ? r.hi[e / 2] & 0xffff0000u : r.hi[e / 2] << 16) |
-                             ((r.lo[e / 4] >> (8 * (e % 4))) & 0xffu) << 8);
+    for (int e = 0; e < W; ++e)     // bytes 0, lo, hi, hi
+      f[e] = __uint_as_float(__builtin_amdgcn_perm(r.hi[e / 2], r.lo[e / 4],
+                                                   (e % 2 ? 0x0706000cu : 0x0504000cu) + (uint32_t)(e % 4) * 0x100u));
   }
 };
 
@@ -257,8 +257,18 @@ __device__ __forceinline__ void clear(float (&v)[W], float (&w)[W]) {
 
 // finish is called for the tokens t < rows (whole blocks of 16) and columns c <
 // cols (whole blocks of 64); past T the sums are zero.  What it reads comes
-// through fetch, some calls ahead.
+// through fetch, some calls ahead.  Where the values lie in fragments is given
+// as an offset (at), which the caller has without a division: between two calls
+// it grows by constants.  Without that and the byte permutes, 128 values of
+// dg, du and h per lane cost 35 us a tile of 256 x 256, a third of its products.
 struct Nothing {};
+struct Place {
+  int64_t t, c;
+  int64_t at;          // frag_at(t, c, cols / 32)
+};
+__device__ __forceinline__ Place place_of(int64_t t, int64_t c, int64_t cols) {
+  return Place{t, c, frag_at(t, c, cols / 32)};
+}
 
 // h from g and u (W columns of one token); g and u saved where wanted
 template <typename TS>
@@ -271,21 +281,24 @@ struct EpiUp {
   uint16_t* h;
   Saved<TS> saved;     // p null: not wanted
   template <int W> using Pre = Nothing;
-  template <int W> __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return Nothing{}; }
+  template <int W> __device__ __forceinline__ Nothing fetch(const Place&) const { return Nothing{}; }
   template <int W>
-  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&g)[W], const float (&u)[W],
+  __device__ __forceinline__ void finish(const Place& p, const float (&g)[W], const float (&u)[W],
                                          const Nothing&) const {
     float f[W];
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       float d;
-      f[e] = c + e < H ? act_of<false>(act, g[e], d) * u[e] : 0.f;
+      f[e] = act_of<false>(act, g[e], d) * u[e];
     }
-    const int64_t at = frag_at(t, c, cols / 32);
-    store_operand<TS, W>(h + at, rows * cols, f);
+    if (p.c + W > H) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) f[e] = p.c + e < H ? f[e] : 0.f;
+    }
+    store_operand<TS, W>(h + p.at, rows * cols, f);
     if (saved.p) {
-      saved.template store<W>(0, at, g);
-      saved.template store<W>(1, at, u);
+      saved.template store<W>(0, p.at, g);
+      saved.template store<W>(1, p.at, u);
     }
   }
 };
@@ -299,11 +312,11 @@ struct EpiOut {
   int cols;
   TS* out;
   template <int W> using Pre = Nothing;
-  template <int W> __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return Nothing{}; }
+  template <int W> __device__ __forceinline__ Nothing fetch(const Place&) const { return Nothing{}; }
   template <int W>
-  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&v)[W], const float (&)[W],
+  __device__ __forceinline__ void finish(const Place& p, const float (&v)[W], const float (&)[W],
                                          const Nothing&) const {
-    if (t < T) store_vec<W>(out + t * cols + c, v);
+    if (p.t < T) store_vec<W>(out + p.t * cols + p.c, v);
   }
 };
 
@@ -318,32 +331,36 @@ struct EpiGate {
   Saved<TS> saved;
   uint16_t *dgu, *h;   // 2 Hp and Hp columns
   template <int W> struct Pre { typename Saved<TS>::template Raw<W> g, u; };
-  template <int W> __device__ __forceinline__ Pre<W> fetch(int64_t t, int64_t c) const {
+  template <int W> __device__ __forceinline__ Pre<W> fetch(const Place& p) const {
     Pre<W> r;
-    const int64_t at = frag_at(t, c, cols / 32);
-    saved.template load<W>(0, at, r.g);
-    saved.template load<W>(1, at, r.u);
+    saved.template load<W>(0, p.at, r.g);
+    saved.template load<W>(1, p.at, r.u);
     return r;
   }
   template <int W>
-  __device__ __forceinline__ void finish(int64_t t, int64_t c, const float (&dh)[W], const float (&)[W],
+  __device__ __forceinline__ void finish(const Place& p, const float (&dh)[W], const float (&)[W],
                                          const Pre<W>& r) const {
     float g[W], u[W], f[W], dg[W], du[W];
-    const int64_t at = frag_at(t, c, cols / 32);
     Saved<TS>::unpack(r.g, g);
     Saved<TS>::unpack(r.u, u);
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       float d;
       const float a = act_of<true>(act, g[e], d);
-      const bool in = c + e < H;
-      f[e] = in ? a * u[e] : 0.f;
-      dg[e] = in ? dh[e] * u[e] * d : 0.f;
-      du[e] = in ? dh[e] * a : 0.f;
+      f[e] = a * u[e];
+      dg[e] = dh[e] * u[e] * d;
+      du[e] = dh[e] * a;
     }
-    store_operand<TS, W>(dgu + frag_at(t, c, cols / 16), rows * 2 * cols, dg);
-    store_operand<TS, W>(dgu + frag_at(t, cols + c, cols / 16), rows * 2 * cols, du);
-    store_operand<TS, W>(h + at, rows * cols, f);
+    if (p.c + W > H) {
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (p.c + e >= H) f[e] = dg[e] = du[e] = 0.f;
+    }
+    // a row block of dg and du is twice as long: its blocks before this one's, again
+    const int64_t at = p.at + (p.t & ~(int64_t)15) * cols;
+    store_operand<TS, W>(dgu + at, rows * 2 * cols, dg);
+    store_operand<TS, W>(dgu + at + 16 * cols, rows * 2 * cols, du);
+    store_operand<TS, W>(h + p.at, rows * cols, f);
   }
 };
 
@@ -383,34 +400,37 @@ __global__ __launch_bounds__(64 * S::NW) void k_ffn_rows(const GemmArgs a, const
     // 32 tokens by 16 columns at a time, fetched some ahead
     constexpr int NB = S::FN * (Epi::kTwo ? 1 : 2), ALL = S::FT * NB, AHEAD = Epi::kParts == 1 ? 4 : 2;
     const bool whole = gridDim.y == 1;
-    const int64_t c0 = (Epi::kTwo ? n0 / 2 : n0) + lane / 32 * 8;
-    t0 += lane % 32;
+    const Place p0 = place_of(t0 + lane % 32, (Epi::kTwo ? n0 / 2 : n0) + lane / 32 * 8, e.cols);
+    const int64_t step = e.cols * 32;             // 32 tokens on, in fragments
+    const auto place = [&](int q) {               // columns start at a block of 32
+      return Place{p0.t + q / NB * 32, p0.c + q % NB * 16, p0.at + q / NB * step + (q % NB / 2 * 512 + q % 2 * 256)};
+    };
     typename Epi::template Pre<8> pre[AHEAD];
-    const auto inside = [&](int q) { return t0 + q / NB * 32 < e.rows && c0 + q % NB * 16 < e.cols; };
+    const auto inside = [&](const Place& p) { return p.t < e.rows && p.c < e.cols; };
     const auto fetch = [&](int q) {
-      if (whole && inside(q)) pre[q % AHEAD] = e.template fetch<8>(t0 + q / NB * 32, c0 + q % NB * 16);
+      if (whole && inside(place(q))) pre[q % AHEAD] = e.template fetch<8>(place(q));
     };
 #pragma unroll
     for (int q = 0; q < AHEAD - 1; ++q) fetch(q);
 #pragma unroll
     for (int q = 0; q < ALL; ++q) {
       if (q + AHEAD - 1 < ALL) fetch(q + AHEAD - 1);
-      if (!inside(q)) continue;
+      const Place p = place(q);
+      if (!inside(p)) continue;
       const int j = q / NB, i = q % NB;
-      const int64_t t = t0 + j * 32, c = c0 + i * 16;
       float v[8], w[8];
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         v[x] = Epi::kTwo ? acc[i][j][x] : acc[i / 2][j][i % 2 * 8 + x];
         w[x] = Epi::kTwo ? acc[i][j][8 + x] : 0.f;
       }
-      if (t >= e.T) clear<8>(v, w);
+      if (p.t >= e.T) clear<8>(v, w);
       if (whole) {
-        e.template finish<8>(t, c, v, w, pre[q % AHEAD]);
+        e.template finish<8>(p, v, w, pre[q % AHEAD]);
       } else {
-        float* p = part + ((int64_t)blockIdx.y * e.rows + t) * e.cols * (Epi::kTwo ? 2 : 1) + c;
-        Vec8<float>::store(p, v);
-        if (Epi::kTwo) Vec8<float>::store(p + e.cols, w);
+        float* to = part + ((int64_t)blockIdx.y * e.rows + p.t) * e.cols * (Epi::kTwo ? 2 : 1) + p.c;
+        Vec8<float>::store(to, v);
+        if (Epi::kTwo) Vec8<float>::store(to + e.cols, w);
       }
     }
   });
@@ -422,7 +442,8 @@ __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float*
   const int64_t g = e.cols / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t t = i / g, c = i % g * 8, ld = (int64_t)e.cols * (Epi::kTwo ? 2 : 1);
   if (t >= e.rows) return;
-  const auto pre = e.template fetch<8>(t, c);
+  const Place at = place_of(t, c, e.cols);
+  const auto pre = e.template fetch<8>(at);
   float v[8] = {}, w[8] = {};
   for (int p = 0; p < parts; ++p) {
     const float* s = part + ((int64_t)p * e.rows + t) * ld + c;
@@ -436,7 +457,7 @@ __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float*
       for (int x = 0; x < 8; ++x) w[x] += f[x];
     }
   }
-  e.template finish<8>(t, c, v, w, pre);
+  e.template finish<8>(at, v, w, pre);
 }
 
 // Few tokens (up to 16 MB): bound by the weights' bytes, which go from memory
@@ -538,7 +559,10 @@ __global__ __launch_bounds__(64 * NW) void k_ffn_few(const FewArgs a, const Epi 
     const int q = lane / 16;                               // rows 4 q .. + 4 of the block
     const int64_t c = ((int64_t)blockIdx.x * FR + f) / PER * 16 + perm_n(4 * q);
     if (t >= a.T) clear<4>(v, u);
-    if (t < e.rows && c < e.cols) e.template finish<4>(t, c, v, u, e.template fetch<4>(t, c));
+    if (t < e.rows && c < e.cols) {
+      const Place p = place_of(t, c, e.cols);
+      e.template finish<4>(p, v, u, e.template fetch<4>(p));
+    }
   }
 }
 
