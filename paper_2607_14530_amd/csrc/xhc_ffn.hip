@@ -41,11 +41,15 @@ struct PackArgs {
 
 __device__ __forceinline__ uint32_t pair(uint16_t a, uint16_t b) { return (uint32_t)a | (uint32_t)b << 16; }
 
-// one 64 x 64 tile: read once, written in both orders
-__global__ __launch_bounds__(256) void k_ffn_pack(const PackArgs a) {
+// one 64 x 64 tile of one matrix (blockIdx.z; the last has columns and rows the
+// other way round): read once, written in both orders
+struct PackAll { PackArgs m[3]; };
+__global__ __launch_bounds__(256) void k_ffn_pack(const PackAll all) {
   constexpr int LD = 72;
   __shared__ __align__(16) uint16_t s[64][LD];
-  const int64_t r0 = (int64_t)blockIdx.y * 64, q0 = (int64_t)blockIdx.x * 64;
+  const PackArgs a = all.m[blockIdx.z];
+  const int64_t r0 = (int64_t)(blockIdx.z == 2 ? blockIdx.x : blockIdx.y) * 64;
+  const int64_t q0 = (int64_t)(blockIdx.z == 2 ? blockIdx.y : blockIdx.x) * 64;
   for (int i = threadIdx.x; i < 64 * 64; i += 256) {
     const int64_t r = r0 + i / 64, q = q0 + i % 64;
     s[i / 64][i % 64] = r < a.R && q < a.Q ? (uint16_t)f2bf(a.W[r * a.Q + q]) : (uint16_t)0;
@@ -234,8 +238,13 @@ template <> struct Saved<uint16_t> {
 // Rows [T, C] into fragments, one wave a fragment; rows up to a whole block and columns up to 64 are zero.  Bound by HBM:
 // each element read once, written once.
 template <typename TS>
-__global__ __launch_bounds__(256) void k_ffn_arrange(const TS* __restrict__ x, int64_t T, int C, int64_t kb,
-                                                     int64_t frags, uint16_t* __restrict__ out) {
+__global__ __launch_bounds__(256) void k_ffn_arrange(const TS* __restrict__ x, const TS* __restrict__ x2, int64_t T,
+                                                     int C, int64_t kb, int64_t frags, uint16_t* __restrict__ out,
+                                                     uint16_t* __restrict__ out2) {
+  if (blockIdx.y) {
+    x = x2;
+    out = out2;
+  }
   const int64_t f = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
   if (f >= frags) return;
@@ -769,13 +778,15 @@ struct Ws {
 Operand weight(const void* p, int64_t nb, int64_t kb) { return Operand{p, 0, nb, kb}; }
 Operand activation(const void* p, int64_t kb, int64_t tb) { return Operand{p, tb * kb * 1024, tb, kb}; }
 
-// rows in fragments
+// rows in fragments; x2: another tensor like x, or null
 template <typename TS>
-hipError_t arrange(const void* x, int64_t T, int64_t C, int64_t kb, void* out, hipStream_t s) {
+hipError_t arrange(const void* x, const void* x2, int64_t T, int64_t C, int64_t kb, void* out, void* out2,
+                   hipStream_t s) {
   const int64_t frags = (T + 15) / 16 * kb;
   if (frags == 0) return hipSuccess;
-  k_ffn_arrange<TS><<<dim3((unsigned)((frags + 3) / 4)), dim3(256), 0, s>>>(
-      reinterpret_cast<const TS*>(x), T, (int)C, kb, frags, reinterpret_cast<uint16_t*>(out));
+  k_ffn_arrange<TS><<<dim3((unsigned)((frags + 3) / 4), x2 ? 2 : 1), dim3(256), 0, s>>>(
+      reinterpret_cast<const TS*>(x), reinterpret_cast<const TS*>(x2), T, (int)C, kb, frags,
+      reinterpret_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(out2));
   return hipGetLastError();
 }
 
@@ -791,7 +802,7 @@ hipError_t ffn(int state_dtype, int64_t T, int64_t C, int64_t H, int act, const 
   const int64_t tb = w.rows / 16, kc = pk.Cp / 32, kh = pk.Hp / 32;
   float* part = reinterpret_cast<float*>(ws + w.part);
   uint16_t* h = reinterpret_cast<uint16_t*>(ws + w.h);
-  hipError_t e = direct ? hipSuccess : arrange<TS>(input, T, C, kc, ws + w.x, s);
+  hipError_t e = direct ? hipSuccess : arrange<TS>(input, nullptr, T, C, kc, ws + w.x, nullptr, s);
   const Operand ox = direct ? Operand{input, 0, tb, C / 32} : activation(ws + w.x, kc, tb);
   if (e == hipSuccess)
     e = rows(w.up, args_of(w.up, weight(pw + pk.up, pk.n32H * 4, kc), ox, seg),
@@ -817,8 +828,7 @@ hipError_t ffn_bwd(int state_dtype, int64_t T, int64_t C, int64_t H, int act, co
   const int64_t tb = w.rows / 16, kc = pk.Cp / 32, kh = pk.Hp / 32;
   float* part = reinterpret_cast<float*>(ws + w.part);
   uint16_t *h = reinterpret_cast<uint16_t*>(ws + w.h), *dgu = reinterpret_cast<uint16_t*>(ws + w.dgu);
-  hipError_t e = arrange<TS>(input, T, C, kc, ws + w.x, s);
-  if (e == hipSuccess) e = arrange<TS>(dF, T, C, kc, ws + w.dF, s);
+  hipError_t e = arrange<TS>(input, dF, T, C, kc, ws + w.x, ws + w.dF, s);
   const Operand ox = activation(ws + w.x, kc, tb), odf = activation(ws + w.dF, kc, tb);
   const Operand oh = activation(h, kh, tb), odgu = activation(dgu, 2 * kh, tb);
   if (e == hipSuccess && T > 0)
@@ -858,12 +868,12 @@ hipError_t launch_ffn_pack(int64_t C, int64_t H, const float* W_gate, const floa
   char* b = reinterpret_cast<char*>(packed);
   const auto at = [&](size_t o) { return reinterpret_cast<uint4*>(b + o); };
   const unsigned tc = (unsigned)(p.Cp / 64), th = (unsigned)(p.Hp / 64);
+  PackAll all;
   for (int i = 0; i < 2; ++i)
-    k_ffn_pack<<<dim3(th, tc), dim3(256), 0, s>>>(PackArgs{i ? W_up : W_gate, C, H, at(p.up), p.Cp / 32, 2, i,
-                                                           with_bwd ? at(p.dx) : nullptr, 2 * p.Hp / 32, i * p.Hp,
-                                                           p.Hp, C});
-  k_ffn_pack<<<dim3(tc, th), dim3(256), 0, s>>>(PackArgs{W_down, H, C, at(p.down), p.Hp / 32, 1, 0,
-                                                         with_bwd ? at(p.dh) : nullptr, p.Cp / 32, 0, C, p.Hp});
+    all.m[i] = PackArgs{i ? W_up : W_gate, C, H, at(p.up), p.Cp / 32, 2, i, with_bwd ? at(p.dx) : nullptr,
+                        2 * p.Hp / 32, i * p.Hp, p.Hp, C};
+  all.m[2] = PackArgs{W_down, H, C, at(p.down), p.Hp / 32, 1, 0, with_bwd ? at(p.dh) : nullptr, p.Cp / 32, 0, C, p.Hp};
+  k_ffn_pack<<<dim3(th, tc, 3), dim3(256), 0, s>>>(all);
   return hipGetLastError();
 }
 

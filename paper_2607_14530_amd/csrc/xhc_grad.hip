@@ -128,6 +128,10 @@ __device__ __forceinline__ float clip_factor(double norm, float max_norm) {
   return c < 1.0 ? (float)c : 1.0f;
 }
 
+// Few chunks: every workgroup of the clip adds them itself, in the same order,
+// instead of waiting for a launch that does (ten small tensors 8.9 us of kernels,
+// 10 in three launches, and the time between two).
+constexpr int kOwnSum = 512;
 constexpr int kNormThreads = 1024;
 __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const double* __restrict__ part, int64_t chunks,
                                                             float max_norm, float* __restrict__ norm,
@@ -182,9 +186,24 @@ __device__ __forceinline__ void chunk_scale(const TS* src, TS* dst, int64_t n, f
   }
 }
 
-__global__ __launch_bounds__(kGradThreads) void k_grad_scale(const GradBatch b, const float* __restrict__ factor) {
-  const float c = *factor;
-  const GradChunk k = find_chunk(b, (int)blockIdx.x);
+// The workgroups take the chunks from the last to the first: what the pass
+// before read last is still in the caches then (617 MB of eight sublayers 238
+// us, 247 from the first on).  part: the chunks' sums to add here, else null.
+__global__ __launch_bounds__(kGradThreads) void k_grad_scale(const GradBatch b, const float* __restrict__ factor,
+                                                             const double* __restrict__ part, int chunks,
+                                                             float max_norm, float* __restrict__ norm) {
+  float c;
+  if (part) {
+    __shared__ double red[kGradThreads / 64];
+    double s = 0.;
+    for (int i = threadIdx.x; i < chunks; i += kGradThreads) s += part[i];
+    s = sqrt(block_sum_f64<kGradThreads>(s, red));
+    c = clip_factor(s, max_norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)s;
+  } else {
+    c = *factor;
+  }
+  const GradChunk k = find_chunk(b, (int)(gridDim.x - 1 - blockIdx.x));
   const uint64_t src = b.src[k.i], dst = b.dst[k.i];
   if (c == 1.0f && src == dst) return;
   if (k.f32)
@@ -202,34 +221,24 @@ int64_t chunk_elems(int n, const int64_t* counts) {
   return c < 8192 ? 8192 : c;
 }
 
-template <class F>
-hipError_t each_batch(int n, const void* const* grads, void* const* outs, const int64_t* counts,
-                      const int32_t* dtypes, int64_t chunk, F launch, int64_t* chunks) {
-  GradBatch b;
-  int64_t done = 0;
-  int i = 0;
-  while (i < n) {
-    b.n = 0;
-    b.chunk = (int32_t)chunk;
-    b.part_at = done;
-    for (int w = 0; w < kGradBatch / 64; ++w) b.f32[w] = 0;
-    b.first[0] = 0;
-    for (; i < n && b.n < kGradBatch; ++i) {
-      if (counts[i] == 0) continue;
-      b.src[b.n] = (uint64_t)(uintptr_t)grads[i];
-      b.dst[b.n] = outs ? (uint64_t)(uintptr_t)outs[i] : 0;
-      b.count[b.n] = counts[i];
-      if (dtypes[i] == XHC_F32) b.f32[b.n / 64] |= 1ull << (b.n % 64);
-      b.first[b.n + 1] = b.first[b.n] + (int32_t)((counts[i] + chunk - 1) / chunk);
-      ++b.n;
-    }
-    if (b.n == 0) break;
-    launch(b, b.first[b.n]);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    done += b.first[b.n];
+// the table of the tensors from i on, as many as it takes; the tensor after them
+int fill_batch(GradBatch& b, int i, int n, const void* const* grads, void* const* outs, const int64_t* counts,
+               const int32_t* dtypes, int64_t chunk, int64_t part_at) {
+  b.n = 0;
+  b.chunk = (int32_t)chunk;
+  b.part_at = part_at;
+  for (int w = 0; w < kGradBatch / 64; ++w) b.f32[w] = 0;
+  b.first[0] = 0;
+  for (; i < n && b.n < kGradBatch; ++i) {
+    if (counts[i] == 0) continue;
+    b.src[b.n] = (uint64_t)(uintptr_t)grads[i];
+    b.dst[b.n] = outs ? (uint64_t)(uintptr_t)outs[i] : 0;
+    b.count[b.n] = counts[i];
+    if (dtypes[i] == XHC_F32) b.f32[b.n / 64] |= 1ull << (b.n % 64);
+    b.first[b.n + 1] = b.first[b.n] + (int32_t)((counts[i] + chunk - 1) / chunk);
+    ++b.n;
   }
-  *chunks = done;
-  return hipSuccess;
+  return i;
 }
 
 }  // namespace
@@ -242,16 +251,31 @@ hipError_t launch_grad_clip(int n, const void* const* grads, const int64_t* coun
   float* factor = reinterpret_cast<float*>(ws);
   double* part = reinterpret_cast<double*>(reinterpret_cast<char*>(ws) + 16);
   const int64_t chunk = chunk_elems(n, counts);
+  GradBatch b;
   int64_t chunks = 0;
-  hipError_t e = each_batch(n, grads, nullptr, counts, dtypes, chunk, [&](const GradBatch& b, int blocks) {
-    k_grad_squares<<<dim3((unsigned)blocks), dim3(kGradThreads), 0, s>>>(b, part);
-  }, &chunks);
-  if (e != hipSuccess) return e;
-  k_grad_norm<<<dim3(1), dim3(kNormThreads), 0, s>>>(part, chunks, max_norm, norm, outs ? factor : nullptr);
-  if ((e = hipGetLastError()) != hipSuccess || !outs) return e;
-  return each_batch(n, grads, outs, counts, dtypes, chunk, [&](const GradBatch& b, int blocks) {
-    k_grad_scale<<<dim3((unsigned)blocks), dim3(kGradThreads), 0, s>>>(b, factor);
-  }, &chunks);
+  int starts[kMaxGrads / kGradBatch + 1], batches = 0;   // the first tensor of each launch
+  for (int i = 0; i < n;) {
+    const int at = i;
+    i = fill_batch(b, i, n, grads, outs, counts, dtypes, chunk, chunks);
+    if (b.n == 0) break;
+    starts[batches++] = at;
+    k_grad_squares<<<dim3((unsigned)b.first[b.n]), dim3(kGradThreads), 0, s>>>(b, part);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    chunks += b.first[b.n];
+  }
+  const bool own = outs && batches == 1 && chunks <= kOwnSum;
+  if (!own) {
+    k_grad_norm<<<dim3(1), dim3(kNormThreads), 0, s>>>(part, chunks, max_norm, norm, outs ? factor : nullptr);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !outs) return e;
+  }
+  // the last launch's tensors first; its table is still there
+  for (int k = batches - 1; k >= 0; --k) {
+    if (k < batches - 1) fill_batch(b, starts[k], n, grads, outs, counts, dtypes, chunk, 0);
+    k_grad_scale<<<dim3((unsigned)b.first[b.n]), dim3(kGradThreads), 0, s>>>(b, factor, own ? part : nullptr,
+                                                                             (int)chunks, max_norm, norm);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace xhc

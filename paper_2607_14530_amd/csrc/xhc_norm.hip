@@ -3,22 +3,23 @@
 //   r_t = 1 / sqrt(mean_c x[t,c]^2 + eps),  y = x r w
 //   dx  = r v - x r^3 mean_c(v x),  v = dy w;   dw[c] = sum_t dy[t,c] x[t,c] r_t
 //
-// Bound by HBM: 2 T C elements forward, 3 T C backward.  A wave takes a row
-// and holds all of it in registers (C <= 4096: up to eight 8-element vectors
-// per lane), so that each element is read once and there is no barrier; wider
-// rows take a workgroup, which reads them a second time (from the caches).
+// Bound by HBM: 2 T C elements forward, 3 T C backward.  Forward a wave takes
+// a row and holds all of it in registers (C <= 4096: up to eight 8-element
+// vectors per lane), so that each element is read once and there is no barrier;
+// backward up to C = 1024, and up to 4096 a workgroup takes four rows.  Wider
+// rows take a workgroup each, which reads them a second time (from the caches).
 // All sums are fp32; y and dx are rounded once.
 //
-// The gain's gradient: every lane keeps the sums of its columns over the rows
-// of its wave, a workgroup adds its waves' sums, and a second kernel adds the
-// workgroups' in order, so that the result does not depend on timing.
+// The gain's gradient: every lane keeps the sums of its columns over its rows,
+// a workgroup adds its waves' sums, and a second kernel adds the workgroups' in
+// order, so that the result does not depend on timing.
 #include "xhc_device.h"
 
 namespace xhc {
 
 namespace {
 
-constexpr int kNormWaves = 4;            // rows in flight per workgroup of the register form
+constexpr int kNormWaves = 4;            // rows of a workgroup at a time
 constexpr int kNormRegC = 4096;          // widest row that a wave holds
 
 template <int V> __device__ __forceinline__ bool in_row(int v, int lane, int C) { return (v * 64 + lane) * 8 < C; }
@@ -164,6 +165,86 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rmsnorm_bwd(const TS* __res
   }
 }
 
+// The same for wider rows: the workgroup's threads take the columns of four
+// rows at a time, so that a thread has few columns: their sums and their gain
+// stay in registers, with eight vectors on the way (T = 16384, C = 4096 with a
+// wave a row, its gain read twice from the cache: 108 us).
+constexpr int kNormRows = 4;
+template <typename TS, int V>
+__global__ __launch_bounds__(256) void k_rmsnorm_bwd_cols(const TS* __restrict__ x, const float* __restrict__ gain,
+                                                          const float* __restrict__ rstd,
+                                                          const TS* __restrict__ dy, int64_t T, int C,
+                                                          TS* __restrict__ dx, float* __restrict__ part) {
+  using R8 = Raw8<TS>;
+  __shared__ float red[2][kNormRows][4];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  float acc[V][8], w[V][8];
+  bool in[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    in[v] = (v * 256 + tid) * 8 < C;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[v][e] = w[v][e] = 0.f;
+    if (in[v]) Vec8<float>::load(gain + (v * 256 + tid) * 8, w[v]);
+  }
+  int flip = 0;
+  for (int64_t t0 = (int64_t)blockIdx.x * kNormRows; t0 < T; t0 += (int64_t)gridDim.x * kNormRows, flip ^= 1) {
+    typename R8::raw rx[kNormRows][V], rd[kNormRows][V];
+    float r[kNormRows];
+#pragma unroll
+    for (int i = 0; i < kNormRows; ++i) {
+      if (t0 + i >= T) continue;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (in[v]) {
+          rx[i][v] = R8::load(x + (t0 + i) * C + (v * 256 + tid) * 8);
+          rd[i][v] = R8::load(dy + (t0 + i) * C + (v * 256 + tid) * 8);
+        }
+      r[i] = rstd[t0 + i];
+    }
+#pragma unroll
+    for (int i = 0; i < kNormRows; ++i) {
+      float s = 0.f;
+      if (t0 + i < T) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (in[v]) {
+            float fx[8], fd[8];
+            R8::unpack(rx[i][v], fx);
+            R8::unpack(rd[i][v], fd);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              s = fmaf(fd[e] * w[v][e], fx[e], s);
+              acc[v][e] = fmaf(fd[e], fx[e] * r[i], acc[v][e]);
+            }
+          }
+      }
+      s = wave_sum(s);
+      if (lane == 0) red[flip][i][wave] = s;
+    }
+    __syncthreads();   // one a turn: the next turn's sums go to the other half
+#pragma unroll
+    for (int i = 0; i < kNormRows; ++i) {
+      if (t0 + i >= T) continue;
+      const float* q = red[flip][i];
+      const float m = (q[0] + q[1] + q[2] + q[3]) / (float)C * r[i] * r[i];
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (in[v]) {
+          float fx[8], fd[8];
+          R8::unpack(rx[i][v], fx);
+          R8::unpack(rd[i][v], fd);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) fd[e] = r[i] * (fd[e] * w[v][e] - fx[e] * m);
+          Vec8<TS>::store(dx + (t0 + i) * C + (v * 256 + tid) * 8, fd);
+        }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (in[v]) Vec8<float>::store(part + (int64_t)blockIdx.x * C + (v * 256 + tid) * 8, acc[v]);
+}
+
 // dx of any width, one workgroup per row
 template <typename TS>
 __global__ __launch_bounds__(256) void k_rmsnorm_bwd_wide(const TS* __restrict__ x, const float* __restrict__ gain,
@@ -259,24 +340,23 @@ hipError_t rmsnorm_bwd(const TS* x, const float* gain, const float* rstd, const 
                        float* dgain, float* part, hipStream_t s) {
   const int64_t blocks = norm_bwd_blocks(T);
   const dim3 grid((unsigned)blocks), block(64 * kNormWaves);
-  const int v = (C / 8 + 63) / 64;
   int64_t rows = blocks;
   if (T == 0) {
     // no rows: dgain is zero
-  } else if (C > kNormRegC) {
+  } else if (C <= 512) {
+    k_rmsnorm_bwd<TS, 1><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
+  } else if (C <= 1024) {
+    k_rmsnorm_bwd<TS, 2><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
+  } else if (C <= 2048) {
+    k_rmsnorm_bwd_cols<TS, 1><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
+  } else if (C <= 4096) {
+    k_rmsnorm_bwd_cols<TS, 2><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
+  } else {
     const int64_t run = (T + blocks - 1) / blocks;
     rows = (T + run - 1) / run;
     k_rmsnorm_bwd_wide<TS><<<dim3((unsigned)T), dim3(256), 0, s>>>(x, gain, rstd, dy, C, dx);
     k_rmsnorm_dw_wide<TS><<<dim3((unsigned)((C / 8 + 63) / 64), (unsigned)rows), dim3(64), 0, s>>>(x, rstd, dy, T, C,
                                                                                                    run, part);
-  } else if (v <= 1) {
-    k_rmsnorm_bwd<TS, 1><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
-  } else if (v <= 2) {
-    k_rmsnorm_bwd<TS, 2><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
-  } else if (v <= 4) {
-    k_rmsnorm_bwd<TS, 4><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
-  } else {
-    k_rmsnorm_bwd<TS, 8><<<grid, block, 0, s>>>(x, gain, rstd, dy, T, C, dx, part);
   }
   k_rmsnorm_dw<<<dim3((unsigned)((C + 15) / 16)), dim3(256), 0, s>>>(part, (int)rows, C, dgain);
   return hipGetLastError();
