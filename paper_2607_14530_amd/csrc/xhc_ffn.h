@@ -197,20 +197,27 @@ struct GemmArgs {
   Segments seg;
   int ksteps;               // stages of one segment
   int64_t steps_per_split;  // of all ksteps * seg.n stages, in blockIdx.y parts
-  int64_t gn, gt;           // tiles
+  int64_t gn, gt;           // tiles (where `quarters`, of twice the size)
+  int64_t from;             // the launch's first of them
+  int quarters;             // four workgroups share a tile of twice the size
 };
 
 // Workgroup b's tile: each XCD (b % 8) takes a run of consecutive tiles, and
 // tiles go in groups of 8 rows of t, so that the workgroups that an XCD runs
 // at a time share their operands in its L2.
-__device__ __forceinline__ void tile_of(int64_t gn, int64_t gt, int64_t& tn, int64_t& tt) {
-  const int64_t total = gn * gt, b = blockIdx.x, x = b % 8, q = total / 8, r = total % 8;
-  const int64_t t = x * q + (x < r ? x : r) + b / 8;
+__device__ __forceinline__ void tile_of(const GemmArgs& a, int64_t& tn, int64_t& tt) {
+  const int64_t total = gridDim.x, b = blockIdx.x, x = b % 8, q = total / 8, r = total % 8;
+  const int64_t mine = x * q + (x < r ? x : r) + b / 8;
+  const int64_t t = a.from + (a.quarters ? mine / 4 : mine);
   constexpr int64_t G = 8;
-  const int64_t grp = t / (G * gn), first = grp * G, rows = gt - first < G ? gt - first : G;
-  const int64_t l = t - grp * G * gn;
+  const int64_t grp = t / (G * a.gn), first = grp * G, rows = a.gt - first < G ? a.gt - first : G;
+  const int64_t l = t - grp * G * a.gn;
   tt = first + l % rows;
   tn = l / rows;
+  if (a.quarters) {
+    tt = tt * 2 + mine % 4 / 2;
+    tn = tn * 2 + mine % 2;
+  }
 }
 
 template <int V> struct Int { static constexpr int value = V; };
@@ -250,7 +257,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, unsigned char* lds,
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int wn = wave % S::WN, wt = wave / S::WN;
   int64_t tn, tt;
-  tile_of(a.gn, a.gt, tn, tt);
+  tile_of(a, tn, tt);
   LN ln;
   LT lt;
   ln.init(a.n, tn * S::BN, wave, lane);

@@ -629,6 +629,8 @@ using SmallCols = Shape<2, 2, 2, 2, 2, 2>;
 // How a product runs: its tile and the parts that k is cut into.
 struct Plan {
   int64_t tile, gn, gt, ksteps, per;   // per: stages of a part
+  int64_t rest;                        // large tiles computed as four small ones each, at the end
+  int64_t rest_ksteps;                 // their stages
   int nseg, parts;
 };
 // Tiles of 256 x 256 (a workgroup per CU) or 128 x 128 (two), the latter with k
@@ -637,19 +639,21 @@ struct Plan {
 // 0.6 (power); small ones 0.57, 0.5 where not every CU has two, 0.3 where none
 // has.  Parts cost a write and a read of fp32 sums and a launch: T = 512, C =
 // 2560, H = 6912 dx (80 small tiles of 432 steps) 242 us with large tiles, 120
-// with small ones, 66 in 4 parts.
+// with small ones, 66 in 4 parts.  A rest of small tiles: T = 4096, C = 2560, H =
+// 6912 forward 450 -> 437, backward 977 -> 926.
 Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64_t out) {
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   Plan best{};
   double least = 0;
-  for (const int64_t tile : {(int64_t)256, (int64_t)128}) {
+  for (int kind = 0; kind < 3; ++kind) {   // large tiles, with a rest of small ones, small tiles
     Plan p{};
-    p.tile = tile;
+    const int64_t tile = p.tile = kind == 2 ? 128 : 256;
     p.gn = up(n, tile);
     p.gt = up(t, tile);
     p.nseg = nseg;
     const int stage = tile == 256 ? 32 : stage128;
     p.ksteps = std::max<int64_t>(1, up(k, stage));   // no tokens: one stage of zeros
+    p.rest_ksteps = std::max<int64_t>(1, up(k, stage128));
     const int64_t steps = p.ksteps * nseg, tiles = p.gn * p.gt;
     for (int parts = 1; parts <= (tile == 256 ? 1 : 32); ++parts) {
       p.per = up(steps, parts);
@@ -658,12 +662,16 @@ Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64
       const int64_t w = tiles * parts;
       double rounds;
       if (tile == 256) {
-        rounds = w <= 128 ? 0.6 : 0.8 * up(w, 256);
+        // a last round of few large tiles as small ones, in a launch of its own
+        p.rest = kind == 1 && w > 256 && w % 256 <= 128 ? w % 256 : 0;
+        if (kind == 1 && p.rest == 0) continue;
+        rounds = w <= 128 ? 0.6 : 0.8 * up(w - p.rest, 256) + (p.rest == 0 ? 0 : p.rest <= 64 ? 0.3 : 0.57);
       } else {
         const int64_t rest = w % 512;
         rounds = 0.57 * (w / 512) + (rest == 0 ? 0 : rest <= 256 ? 0.3 : 0.5);
       }
       double us = rounds * p.per * (stage / 32) + 3;
+      if (p.rest) us += 8;
       if (parts > 1) us += 4 + (double)parts * out * 8 / 3.5e6;
       if (least == 0 || us < least) {
         least = us;
@@ -676,8 +684,17 @@ Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64
 size_t part_floats(const Plan& p, int64_t t, int64_t cols) { return p.parts > 1 ? (size_t)p.parts * t * cols : 0; }
 
 GemmArgs args_of(const Plan& p, const Operand& n, const Operand& t, const Segments& seg) {
-  return GemmArgs{n, t, seg, (int)p.ksteps, p.per, p.gn, p.gt};
+  return GemmArgs{n, t, seg, (int)p.ksteps, p.per, p.gn, p.gt, 0, 0};
 }
+// the launch of the rest
+GemmArgs rest_of(const Plan& p, GemmArgs a) {
+  a.ksteps = (int)p.rest_ksteps;
+  a.steps_per_split = p.rest_ksteps * p.nseg;
+  a.from = p.gn * p.gt - p.rest;
+  a.quarters = 1;
+  return a;
+}
+dim3 grid_of(const Plan& p) { return dim3((unsigned)(p.gn * p.gt - p.rest), (unsigned)p.parts); }
 
 // Up to so many tokens k_ffn_few runs, and reads an input of bf16 rows as it lies.
 constexpr int kFewTokens = 64;
@@ -710,11 +727,13 @@ hipError_t few(const GemmArgs& a, int64_t ldx, const Epi& e, hipStream_t s) {
 template <class Epi>
 hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hipStream_t s, int64_t ldx = 0) {
   if (e.T <= kFewTokens) return few(a, ldx, e, s);
-  const dim3 grid((unsigned)(p.gn * p.gt), (unsigned)p.parts);
-  if (p.tile == 256)
-    k_ffn_rows<Large, Epi><<<grid, dim3(64 * Large::NW), 0, s>>>(a, e, part);
-  else
-    k_ffn_rows<SmallRows, Epi><<<grid, dim3(64 * SmallRows::NW), 0, s>>>(a, e, part);
+  if (p.tile == 256) {
+    k_ffn_rows<Large, Epi><<<grid_of(p), dim3(64 * Large::NW), 0, s>>>(a, e, part);
+    if (p.rest)
+      k_ffn_rows<SmallRows, Epi><<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallRows::NW), 0, s>>>(rest_of(p, a), e, part);
+  } else {
+    k_ffn_rows<SmallRows, Epi><<<grid_of(p), dim3(64 * SmallRows::NW), 0, s>>>(a, e, part);
+  }
   if (p.parts > 1) {
     const int64_t n = e.rows * (e.cols / 8);
     k_ffn_rows_join<Epi><<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(e, part, p.parts);
@@ -723,11 +742,13 @@ hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hip
 }
 template <class Epi>
 hipError_t cols(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hipStream_t s) {
-  const dim3 grid((unsigned)(p.gn * p.gt), (unsigned)p.parts);
-  if (p.tile == 256)
-    k_ffn_cols<Large, Epi><<<grid, dim3(64 * Large::NW), 0, s>>>(a, e, part);
-  else
-    k_ffn_cols<SmallCols, Epi><<<grid, dim3(64 * SmallCols::NW), 0, s>>>(a, e, part);
+  if (p.tile == 256) {
+    k_ffn_cols<Large, Epi><<<grid_of(p), dim3(64 * Large::NW), 0, s>>>(a, e, part);
+    if (p.rest)
+      k_ffn_cols<SmallCols, Epi><<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallCols::NW), 0, s>>>(rest_of(p, a), e, part);
+  } else {
+    k_ffn_cols<SmallCols, Epi><<<grid_of(p), dim3(64 * SmallCols::NW), 0, s>>>(a, e, part);
+  }
   if (p.parts > 1) {
     const int64_t n = e.M * (e.N / 8);
     k_ffn_cols_join<Epi><<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(e, part, p.parts);

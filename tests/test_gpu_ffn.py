@@ -46,3 +46,19 @@ def test_forward_without_saving_gives_the_same(T, C, H, state):
     x, _, _, a = make(T, C, H, state, "silu", 7, False)
     _, _, _, b = make(T, C, H, state, "silu", 7, True)
     assert torch.equal(a.forward(x.cuda()), b.forward(x.cuda()))
+
+
+@pytest.mark.parametrize("state,T,C,H", [("bf16", 1056, 1024, 8256), ("bf16", 1000, 2080, 4100), ("f32", 1030, 512, 8800)])
+def test_large_tiles_and_a_rest_of_small_ones(state, T, C, H):
+    """More than 256 large tiles, the last few computed as small ones."""
+    x, dF, w, ff = make(T, C, H, state, "silu", 300 + T, True)
+    F = ff.forward(x.cuda())
+    dx = ff.backward(dF.cuda())
+    torch.cuda.synchronize()
+    half = HALF[DT[state]]
+    fw = ffn_forward(x, w, "silu", half)
+    assert_within(F, fw["F"], "F")
+    bw = ffn_backward(x, dF, fw, "silu", half)
+    assert_within(dx, bw["dx"], "dx")
+    for n in ("W_gate", "W_up", "W_down"):
+        assert_within(ff.grads[n], bw[n], "d" + n)
