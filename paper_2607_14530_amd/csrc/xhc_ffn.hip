@@ -625,10 +625,13 @@ __global__ __launch_bounds__(256) void k_ffn_cols_join(const Epi e, const float*
 using Large = Shape<2, 4, 4, 2, 1, 4>;
 using SmallRows = Shape<2, 2, 2, 2, 1, 5>;
 using SmallCols = Shape<2, 2, 2, 2, 2, 2>;
+// 128 n by 64 tokens
+using Narrow = Shape<2, 1, 2, 2, 1, 6>;
+constexpr int64_t kNarrow = 64;
 
 // How a product runs: its tile and the parts that k is cut into.
 struct Plan {
-  int64_t tile, gn, gt, ksteps, per;   // per: stages of a part
+  int64_t tile, gn, gt, ksteps, per;   // tile 0: k_ffn_few; per: stages of a part
   int64_t rest;                        // large tiles computed as four small ones each, at the end
   int64_t rest_ksteps;                 // their stages
   int nseg, parts;
@@ -641,14 +644,14 @@ struct Plan {
 // 2560, H = 6912 dx (80 small tiles of 432 steps) 242 us with large tiles, 120
 // with small ones, 66 in 4 parts.  A rest of small tiles: T = 4096, C = 2560, H =
 // 6912 forward 450 -> 437, backward 977 -> 926.
-Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64_t out) {
+Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64_t out, bool narrow = false) {
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   Plan best{};
   double least = 0;
-  for (int kind = 0; kind < 3; ++kind) {   // large tiles, with a rest of small ones, small tiles
+  for (int kind = narrow ? 2 : 0; kind < 3; ++kind) {   // large tiles, with a rest of small ones, small tiles
     Plan p{};
-    const int64_t tile = p.tile = kind == 2 ? 128 : 256;
-    p.gn = up(n, tile);
+    const int64_t tile = p.tile = kind < 2 ? 256 : narrow ? kNarrow : 128;
+    p.gn = up(n, std::max<int64_t>(tile, 128));
     p.gt = up(t, tile);
     p.nseg = nseg;
     const int stage = tile == 256 ? 32 : stage128;
@@ -696,8 +699,14 @@ GemmArgs rest_of(const Plan& p, GemmArgs a) {
 }
 dim3 grid_of(const Plan& p) { return dim3((unsigned)(p.gn * p.gt - p.rest), (unsigned)p.parts); }
 
-// Up to so many tokens k_ffn_few runs, and reads an input of bf16 rows as it lies.
-constexpr int kFewTokens = 64;
+// Whether k_ffn_few runs (and reads an input of bf16 rows as it lies): up to 16
+// tokens, up to 64 where the weights are small.  Its workgroups read all
+// activations again for every block or two of n, the tiles for every eight; but
+// the tiles take two launches more.  us, forward: T = 64, C = 1024, H = 2816 17
+// here and 25 in tiles, C = 2112, H = 5637 T = 37 35 and 37, T = 64 40 and 38; C
+// = 4096, H = 11008 T = 32 83 and 74, T = 64 101 and 76.
+constexpr int64_t kFewMost = 64;
+bool few_tokens(int64_t T, int64_t C, int64_t H) { return T <= 16 || (T <= kFewMost && C * H <= (1 << 24)); }
 // all n blocks of the packed matrix a.n; ldx: elements between rows of the activations, 0 for fragments
 template <class Epi>
 hipError_t few(const GemmArgs& a, int64_t ldx, const Epi& e, hipStream_t s) {
@@ -726,11 +735,13 @@ hipError_t few(const GemmArgs& a, int64_t ldx, const Epi& e, hipStream_t s) {
 
 template <class Epi>
 hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hipStream_t s, int64_t ldx = 0) {
-  if (e.T <= kFewTokens) return few(a, ldx, e, s);
+  if (p.tile == 0) return few(a, ldx, e, s);
   if (p.tile == 256) {
     k_ffn_rows<Large, Epi><<<grid_of(p), dim3(64 * Large::NW), 0, s>>>(a, e, part);
     if (p.rest)
       k_ffn_rows<SmallRows, Epi><<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallRows::NW), 0, s>>>(rest_of(p, a), e, part);
+  } else if (p.tile == kNarrow) {
+    k_ffn_rows<Narrow, Epi><<<grid_of(p), dim3(64 * Narrow::NW), 0, s>>>(a, e, part);
   } else {
     k_ffn_rows<SmallRows, Epi><<<grid_of(p), dim3(64 * SmallRows::NW), 0, s>>>(a, e, part);
   }
@@ -779,17 +790,25 @@ struct Ws {
     h = take((size_t)P * rows * pk.Hp * 2);
     dgu = take(bwd ? (size_t)P * rows * pk.Hp * 4 : 0);
     size_t most = 0;
+    const auto product = [&](int64_t n, int64_t k) {       // of the tokens by packed weights
+      if (few_tokens(T, C, H)) return Plan{};
+      const Plan p = plan_product(n, T, k, ns, 32, rows * n, T <= kNarrow);
+      most = std::max(most, part_floats(p, rows, n));
+      return p;
+    };
+    const auto weights = [&](int64_t n, int64_t m) {       // their gradients
+      const Plan p = plan_product(n, m, T, nw, 64, n * m);
+      most = std::max(most, part_floats(p, m, n));
+      return p;
+    };
     if (bwd) {
-      dh = plan_product(pk.Hp, T, pk.Cp, ns, 32, rows * pk.Hp);
-      dx = plan_product(C, T, 2 * pk.Hp, ns, 32, rows * C);
-      dwgu = plan_product(2 * pk.Hp, C, T, nw, 64, C * 2 * pk.Hp);
-      dwd = plan_product(C, H, T, nw, 64, H * C);
-      most = std::max({part_floats(dh, rows, pk.Hp), part_floats(dx, rows, C), part_floats(dwgu, C, 2 * pk.Hp),
-                       part_floats(dwd, H, C)});
+      dh = product(pk.Hp, pk.Cp);
+      dx = product(C, 2 * pk.Hp);
+      dwgu = weights(2 * pk.Hp, C);
+      dwd = weights(C, H);
     } else {
-      up = plan_product(2 * pk.Hp, T, pk.Cp, ns, 32, rows * 2 * pk.Hp);
-      down = plan_product(C, T, pk.Hp, ns, 32, rows * C);
-      most = std::max(part_floats(up, rows, 2 * pk.Hp), part_floats(down, rows, C));
+      up = product(2 * pk.Hp, pk.Cp);
+      down = product(C, pk.Hp);
     }
     part = take(most * sizeof(float));
     total = at;
@@ -816,7 +835,7 @@ hipError_t ffn(int state_dtype, int64_t T, int64_t C, int64_t H, int act, const 
                void* F, void* saved, void* workspace, hipStream_t s) {
   const Packed pk(C, H);
   const Ws w(state_dtype, T, C, H, false);
-  const bool f32 = state_dtype == XHC_F32, direct = !f32 && T <= kFewTokens;
+  const bool f32 = state_dtype == XHC_F32, direct = !f32 && few_tokens(T, C, H);
   char* ws = reinterpret_cast<char*>(workspace);
   const char* pw = reinterpret_cast<const char*>(packed);
   const Segments seg = f32 ? segs_weights() : segs_bf16();

@@ -10,9 +10,9 @@ from tests.ffn_util import HALF, assert_within, ffn_backward, ffn_forward, ffn_i
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
-# T, C, H: one token, ragged tokens, widths and hidden widths that end inside a block of 16, 32, 64 or a
+# T, C, H: one token, few tokens with large weights, ragged tokens, widths and hidden widths that end inside a block of 16, 32, 64 or a
 # tile, more than one tile each way
-SIZES = [(1, 32, 1), (1, 256, 683), (3, 96, 33), (16, 64, 64), (17, 160, 200), (37, 2112, 341), (64, 256, 1000),
+SIZES = [(1, 32, 1), (20, 4096, 4160), (64, 2080, 8200), (1, 256, 683), (3, 96, 33), (16, 64, 64), (17, 160, 200), (37, 2112, 341), (64, 256, 1000),
          (65, 512, 129), (130, 352, 520), (200, 32, 48), (257, 384, 1030), (300, 1056, 96)]
 
 
