@@ -408,20 +408,23 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
  * What runs between xhc_pre and xhc_post of an MLP-type sublayer: the norm of
  * its input and a gated feed-forward block, forward and backward.  Only T, C,
  * state_dtype and (norm) eps of d are used.  Tensor pointers are 16-byte
- * aligned; an output may not be one of the other tensors of its call.
+ * aligned; an output may not be one of the other tensors of its call.  Rows
+ * are independent of one another, whatever they hold.
  *
  * xhc_rmsnorm: y [T,C] = x r gain with r_t = 1 / sqrt(mean_c x[t,c]^2 + eps),
  *   rounded once.  x, y in the state dtype, gain [C] fp32; rstd [T] fp32 or
  *   NULL receives r, as xhc_rmsnorm_bwd needs it.
  * xhc_rmsnorm_bwd: dx [T,C] = r v - x r^3 mean_c(v x), v = dy gain, in the
  *   state dtype; dgain [C] fp32 = sum_t dy x r (zero for T = 0), summed in a
- *   fixed order.  workspace: xhc_rmsnorm_workspace_bytes(d) bytes.           */
+ *   fixed order.  workspace: xhc_rmsnorm_workspace_bytes(d) bytes.
+ * XHC_EUNSUPPORTED above 2^23 rows.                                         */
 size_t xhc_rmsnorm_workspace_bytes(const xhc_dims* d);
 xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void* y, float* rstd, void* stream);
 xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, const float* rstd, const void* dy,
                            void* dx, float* dgain, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Gated feed-forward block with H hidden columns (1 <= H <= 2^20, any; C <= 2^20):
+/* Gated feed-forward block with H hidden columns (any from 1 to 2^20; C <= 2^20;
+ * T C, 2 T H and C H up to 2^34; XHC_EUNSUPPORTED beyond):
  *   h = act(input W_gate) * (input W_up),  F = h W_down
  * act: SILU z sigma(z), GELU z Phi(z) (the error function, not its tanh form).
  *
@@ -440,8 +443,8 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
  *   xhc_ffn and 1 for xhc_ffn_bwd.
  *
  * Sums are fp32 (matrix cores), in an order fixed by the sizes.  bf16 state:
- * h, the saved projections and the gradients of the projections are rounded to
- * bf16, everything else once, as output.  fp32 state: activations enter the
+ * h and the gradients of the projections are rounded to bf16 and the saved
+ * projections cut to 24 bits, everything else is rounded once, as output.  fp32 state: activations enter the
  * products as three bf16 parts that add up to them exactly, so that results
  * have fp32 accuracy (for the bf16 weights).                                */
 typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1 } xhc_act;

@@ -1002,7 +1002,7 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
 }
 
 size_t xhc_rmsnorm_workspace_bytes(const xhc_dims* d) {
-  return check_dims(d) == XHC_OK ? rmsnorm_bwd_ws_bytes(d->T, d->C) : 0;
+  return check_dims(d) == XHC_OK && d->T <= kMaxNormT ? rmsnorm_bwd_ws_bytes(d->T, d->C) : 0;
 }
 
 xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void* y, float* rstd, void* stream) {
@@ -1011,7 +1011,8 @@ xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void
   if (d->T == 0) return XHC_OK;
   if (!x || !gain || !y || x == y || gain == y || (rstd && (rstd == x || rstd == y || rstd == gain)))
     return XHC_EINVAL;
-  if (!aligned16(x) || !aligned16(gain) || !aligned16(y) || !aligned16(rstd)) return XHC_EUNSUPPORTED;
+  if (d->T > kMaxNormT || !aligned16(x) || !aligned16(gain) || !aligned16(y) || !aligned16(rstd))
+    return XHC_EUNSUPPORTED;
   clear_stale_error();
   hipError_t e = hipSuccess;
   XHC_STEP("rmsnorm", launch_rmsnorm(d->state_dtype, x, gain, d->T, d->C, d->eps, y, rstd,
@@ -1024,6 +1025,7 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
   xhc_status st = check_dims(d);
   if (st != XHC_OK) return st;
   if (!dgain) return XHC_EINVAL;
+  if (d->T > kMaxNormT) return XHC_EUNSUPPORTED;
   if (d->T > 0) {
     if (!x || !gain || !rstd || !dy || !dx || !workspace) return XHC_EINVAL;
     for (const void* in : {x, (const void*)gain, (const void*)rstd, dy})
@@ -1046,7 +1048,9 @@ static xhc_status check_ffn(const xhc_dims* d, int32_t H) {
   xhc_status st = check_dims(d);
   if (st != XHC_OK) return st;
   if (H < 1) return XHC_EINVAL;
-  return H > kMaxFfn || d->C > kMaxFfn ? XHC_EUNSUPPORTED : XHC_OK;
+  const int64_t C = d->C, wide = std::max<int64_t>(C, 2 * (int64_t)H);
+  if (H > kMaxFfn || C > kMaxFfn || C * H > kMaxFfnElems || d->T > kMaxFfnElems / wide) return XHC_EUNSUPPORTED;
+  return XHC_OK;
 }
 
 size_t xhc_packed_ffn_bytes(const xhc_dims* d, int32_t H, int32_t with_bwd) {

@@ -299,7 +299,9 @@ size_t rmsnorm_bwd_ws_bytes(int64_t T, int C);
 hipError_t launch_rmsnorm_bwd(int state_dtype, const void* x, const float* gain, const float* rstd, const void* dy,
                               int64_t T, int C, void* dx, float* dgain, float* part, hipStream_t s);
 
-constexpr int kMaxFfn = 1 << 20;   // C and H: a tile's rows stay below 2 GiB
+constexpr int64_t kMaxNormT = 1 << 23;       // rows: a launch's threads stay below 2^32
+constexpr int kMaxFfn = 1 << 20;             // C and H: a tile's rows stay below 2 GiB
+constexpr int64_t kMaxFfnElems = (int64_t)1 << 34;   // T C, 2 T H and C H: a launch's threads stay below 2^32
 size_t ffn_packed_bytes(int64_t C, int64_t H, bool with_bwd);
 size_t ffn_saved_bytes(int state_dtype, int64_t T, int64_t H);
 size_t ffn_ws_bytes(int state_dtype, int64_t T, int64_t C, int64_t H, bool bwd);

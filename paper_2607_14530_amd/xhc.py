@@ -332,12 +332,18 @@ def xhc_ffn_bwd(d, H, act, input, packed, saved, dF, d_input, dW_gate, dW_up, dW
 
 def _grad_arrays(grads):
     """Host arrays of the tensors' addresses, counts and dtypes."""
-    n = len(grads)
+    ptrs, counts, dtypes = [], [], []
     for g in grads:
-        if g.dtype not in (torch.bfloat16, torch.float32):
+        if g.dtype is torch.bfloat16:
+            dtypes.append(XHC_BF16)
+        elif g.dtype is torch.float32:
+            dtypes.append(XHC_F32)
+        else:
             raise ValueError(f"gradients are bf16 or fp32, got {g.dtype}")
-    return ((_P * n)(*[_ptr(g) for g in grads]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
-            (ctypes.c_int32 * n)(*[XHC_BF16 if g.dtype == torch.bfloat16 else XHC_F32 for g in grads]))
+        ptrs.append(_ptr(g))
+        counts.append(g.numel())
+    n = len(ptrs)
+    return (_P * n)(*ptrs), (ctypes.c_int64 * n)(*counts), (ctypes.c_int32 * n)(*dtypes)
 
 
 def xhc_grad_workspace_bytes(n):
@@ -352,12 +358,15 @@ def xhc_grad_norm(grads, norm, workspace, stream=None):
 
 def xhc_grad_clip(grads, max_norm, outs, norm, workspace, stream=None):
     """outs: a list of the gradients' shapes and dtypes (the gradients themselves for in place)."""
-    if len(outs) != len(grads):
-        raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
-    for g, o in zip(grads, outs):
-        _expect(o, g.dtype, g.shape, "output of a gradient")
     ptrs, counts, dtypes = _grad_arrays(grads)
-    to = ptrs if outs is grads else (_P * len(outs))(*[_ptr(o) for o in outs])
+    to = ptrs
+    if outs is not grads:
+        if len(outs) != len(grads):
+            raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
+        for g, o in zip(grads, outs):
+            if o.dtype is not g.dtype or o.shape != g.shape:
+                _expect(o, g.dtype, g.shape, "output of a gradient")
+        to = (_P * len(outs))(*[_ptr(o) for o in outs])
     _call("xhc_grad_clip", len(grads), ptrs, counts, dtypes, max_norm, to, _ptr(norm), _ptr(workspace),
           _nbytes(workspace), _stream(stream))
 
@@ -851,12 +860,11 @@ def clip_grad_norm(grads, max_norm, outs=None, stream=None):
     an fp32 [1] tensor (nothing waits for it here)."""
     grads = list(grads)
     dev = _here(grads[0].device if grads else "cuda")
-    for g in grads:
-        _on(g, dev, "gradient")
-    for o in outs or []:
-        _on(o, dev, "output")
+    for g in grads if outs is None else grads + list(outs):
+        if g.get_device() != dev.index:
+            raise ValueError(f"a gradient or output is on {g.device}, expected {dev}")
     with _within(stream):
         norm = torch.empty(1, dtype=torch.float32, device=dev)
-        ws = _bytes(xhc_grad_workspace_bytes(len(grads)), dev)
+        ws = torch.empty(xhc_grad_workspace_bytes(len(grads)), dtype=torch.uint8, device=dev)
     xhc_grad_clip(grads, max_norm, grads if outs is None else list(outs), norm, ws, stream)
     return norm
