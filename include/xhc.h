@@ -440,7 +440,8 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
  *   (overwritten; zero for T = 0).  Weights receive the gradient of their bf16
  *   values.
  * workspace: xhc_ffn_workspace_bytes(d, H, backward) bytes, backward = 0 for
- *   xhc_ffn and 1 for xhc_ffn_bwd.
+ *   xhc_ffn and 1 for xhc_ffn_bwd, of the sizes of the call (fewer tokens can
+ *   need more: their sums are formed in parts).
  *
  * Sums are fp32 (matrix cores), in an order fixed by the sizes.  bf16 state:
  * h and the gradients of the projections are rounded to bf16 and the saved

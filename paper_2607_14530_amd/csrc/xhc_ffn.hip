@@ -9,9 +9,10 @@
 // (one product over k = 2 H), [dW_gate | dW_up] and dW_down.  Weights enter as
 // bf16 (packed once a step), sums are fp32.  bf16 state: h, dg and du are
 // rounded to bf16, as operands of the next product: a rounding of the size of
-// the one that F, dx and the weight gradients get as outputs.  fp32 state: activations are
-// multiplied as three bf16 parts that add up to them exactly, so that nothing
-// is rounded below fp32 (three passes over k; six for the weight gradients).
+// the one that F, dx and the weight gradients get as outputs.  fp32 state:
+// activations are multiplied as three bf16 parts that add up to them exactly,
+// so that nothing is rounded below fp32 (three passes over k; six for the
+// weight gradients).
 #include "xhc_ffn.h"
 
 #include <algorithm>
@@ -739,7 +740,8 @@ hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hip
   if (p.tile == 256) {
     k_ffn_rows<Large, Epi><<<grid_of(p), dim3(64 * Large::NW), 0, s>>>(a, e, part);
     if (p.rest)
-      k_ffn_rows<SmallRows, Epi><<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallRows::NW), 0, s>>>(rest_of(p, a), e, part);
+      k_ffn_rows<SmallRows, Epi>
+          <<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallRows::NW), 0, s>>>(rest_of(p, a), e, part);
   } else if (p.tile == kNarrow) {
     k_ffn_rows<Narrow, Epi><<<grid_of(p), dim3(64 * Narrow::NW), 0, s>>>(a, e, part);
   } else {
@@ -756,7 +758,8 @@ hipError_t cols(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hip
   if (p.tile == 256) {
     k_ffn_cols<Large, Epi><<<grid_of(p), dim3(64 * Large::NW), 0, s>>>(a, e, part);
     if (p.rest)
-      k_ffn_cols<SmallCols, Epi><<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallCols::NW), 0, s>>>(rest_of(p, a), e, part);
+      k_ffn_cols<SmallCols, Epi>
+          <<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallCols::NW), 0, s>>>(rest_of(p, a), e, part);
   } else {
     k_ffn_cols<SmallCols, Epi><<<grid_of(p), dim3(64 * SmallCols::NW), 0, s>>>(a, e, part);
   }
