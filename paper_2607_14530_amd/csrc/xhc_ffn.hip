@@ -91,7 +91,13 @@ struct Packed {
 
 // ---------------------------------------------------------------- activations
 
-// act(g) and, with D, act'(g)
+// act(g) and, with D, act'(g).  The distribution function of GELU by formula
+// 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions:
+//   1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2),  t = 1 / (1 + p x),  x >= 0,
+// to 1.5e-7, with x = |g| / sqrt 2: half of that, 2^-23.7, in the distribution,
+// in a dozen instructions that share the exponential with the density (erff is
+// about eighty, and an epilogue has nothing to hide them behind: T = 8192, C =
+// 4096, H = 11008 forward 1827 us with it, 1788 so).
 template <bool D>
 __device__ __forceinline__ float act_of(int act, float g, float& d) {
   if (act == XHC_ACT_SILU) {
@@ -99,8 +105,15 @@ __device__ __forceinline__ float act_of(int act, float g, float& d) {
     if (D) d = fmaf(a, 1.0f - e, e);
     return a;
   }
-  const float e = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
-  if (D) d = e + g * __expf(-0.5f * g * g) * 0.39894228040143268f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.0f));
+  const float x = __expf(-0.5f * g * g);
+  float q = fmaf(t, 1.061405429f, -1.453152027f);
+  q = fmaf(t, q, 1.421413741f);
+  q = fmaf(t, q, -0.284496736f);
+  q = fmaf(t, q, 0.254829592f);
+  q *= 0.5f * t * x;
+  const float e = g < 0.f ? q : 1.0f - q;
+  if (D) d = fmaf(g * x, 0.39894228040143268f, e);
   return g * e;
 }
 
@@ -637,13 +650,14 @@ struct Plan {
   int64_t rest_ksteps;                 // their stages
   int nseg, parts;
 };
-// Tiles of 256 x 256 (a workgroup per CU) or 128 x 128 (two), the latter with k
-// in parts where there are few of them; by an estimate of the time in us.
+// Tiles of 256 x 256 (a workgroup per CU) or 128 x 128 (two), with k in parts
+// where there are few of them; by an estimate of the time in us.
 // Measured per 32 k and round: a large tile 0.8 on a full chip, below half of it
 // 0.6 (power); small ones 0.57, 0.5 where not every CU has two, 0.3 where none
 // has.  Parts cost a write and a read of fp32 sums and a launch: T = 512, C =
 // 2560, H = 6912 dx (80 small tiles of 432 steps) 242 us with large tiles, 120
-// with small ones, 66 in 4 parts.  A rest of small tiles: T = 4096, C = 2560, H =
+// with small ones, 66 in 4 parts; T = 2048 (80 large tiles of 432) backward 527
+// without parts of large tiles, 487 with them.  A rest of small tiles: T = 4096, C = 2560, H =
 // 6912 forward 450 -> 437, backward 977 -> 926.
 Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64_t out, bool narrow = false) {
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
@@ -659,7 +673,7 @@ Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64
     p.ksteps = std::max<int64_t>(1, up(k, stage));   // no tokens: one stage of zeros
     p.rest_ksteps = std::max<int64_t>(1, up(k, stage128));
     const int64_t steps = p.ksteps * nseg, tiles = p.gn * p.gt;
-    for (int parts = 1; parts <= (tile == 256 ? 1 : 32); ++parts) {
+    for (int parts = 1; parts <= (kind == 1 ? 1 : kind == 0 ? 8 : 32); ++parts) {
       p.per = up(steps, parts);
       p.parts = (int)up(steps, p.per);
       if (p.parts != parts) continue;
