@@ -55,10 +55,10 @@ __device__ __forceinline__ i32x4 make_srd(uint64_t a, int64_t bytes) {
 
 // 16 bytes per lane from voff + soff into LDS at lds_addr + AT + 16 lane;
 // lds_addr and soff are the same in every lane.  soff stays within a row of
-// fragments, and the descriptor holds whole rows: soff is below its length, and
-// does not reach past its end where voff does not.  Inline assembly, waited for
-// by the caller, as lds_dma16 (the s_nop is the wait state that a copy needs
-// after a write of m0).
+// fragments, and the descriptor holds whole rows, at least one: soff is below
+// its length, and does not reach past its end where voff does not.  Inline
+// assembly, waited for by the caller, as lds_dma16 (the s_nop is the wait state
+// that a copy needs after a write of m0).
 template <int AT>
 __device__ __forceinline__ void buf_dma16(const i32x4& srd, uint32_t voff, uint32_t soff, uint32_t lds_addr) {
   asm volatile("s_add_u32 m0, %1, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
@@ -92,9 +92,10 @@ struct FragTile {
   static constexpr int kBytes = ROWS * 64 * KH, kCopies = ROWS * KH / 16 / NW;
   static_assert(ROWS * KH % (16 * NW) == 0, "whole copies for every wave");
   i32x4 srd;
-  uint32_t voff[kCopies], soff, step, lds;
+  uint32_t voff[kCopies], soff, lds;
   const Operand* op;
   int64_t at;
+  static __device__ __forceinline__ int64_t extent(const Operand& o) { return o.rows * 16; }
   __device__ __forceinline__ void init(const Operand& o, int64_t row0, int wave, int lane) {
     op = &o;
     lds = wave * kCopies * 1024;
@@ -108,12 +109,9 @@ struct FragTile {
   // from stage ks of a plane on
   __device__ __forceinline__ void start(int plane, int64_t ks) {
     srd = make_srd((uint64_t)(uintptr_t)op->p + plane * op->plane + at, op->rows * op->kb * 1024 - at);
-    // where there is no row (a quarter tile past the edge) soff stays 0: the
-    // descriptor's check is of voff against its length less soff
-    step = srd.z ? KH * 1024 : 0;
-    soff = (uint32_t)ks * step;
+    soff = (uint32_t)ks * (KH * 1024);
   }
-  __device__ __forceinline__ void next() { soff += step; }
+  __device__ __forceinline__ void next() { soff += KH * 1024; }
   // nothing more: copies read no memory and leave zeros
   __device__ __forceinline__ void end() {
     srd.z = 0;
@@ -142,6 +140,7 @@ struct ColTileOf {
   uint32_t voff[kCopies], lds;
   const Operand* op;
   int64_t col0;
+  static __device__ __forceinline__ int64_t extent(const Operand& o) { return o.kb * 32; }
   __device__ __forceinline__ void init(const Operand& o, int64_t c0, int wave, int lane) {
     op = &o;
     col0 = c0;
@@ -263,6 +262,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, unsigned char* lds,
   const int wn = wave % S::WN, wt = wave / S::WN;
   int64_t tn, tt;
   tile_of(a, tn, tt);
+  // a quarter tile past the edge (a FragTile's descriptor would be empty there
+  // and its check, of voff against its length less soff, could wrap)
+  if (a.quarters && (tn * S::BN >= LN::extent(a.n) || tt * S::BT >= LT::extent(a.t))) return;
   LN ln;
   LT lt;
   ln.init(a.n, tn * S::BN, wave, lane);
