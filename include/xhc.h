@@ -412,7 +412,8 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
  * are independent of one another, whatever they hold.
  *
  * xhc_rmsnorm: y [T,C] = x r gain with r_t = 1 / sqrt(mean_c x[t,c]^2 + eps),
- *   rounded once.  x, y in the state dtype, gain [C] fp32; rstd [T] fp32 or
+ *   rounded once (sums are fp32: a row whose squares pass the largest float
+ *   gives r = 0).  x, y in the state dtype, gain [C] fp32; rstd [T] fp32 or
  *   NULL receives r, as xhc_rmsnorm_bwd needs it.
  * xhc_rmsnorm_bwd: dx [T,C] = r v - x r^3 mean_c(v x), v = dy gain, in the
  *   state dtype; dgain [C] fp32 = sum_t dy x r (zero for T = 0), summed in a
@@ -445,9 +446,9 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
  *
  * Sums are fp32 (matrix cores), in an order fixed by the sizes.  bf16 state:
  * h and the gradients of the projections are rounded to bf16 and the saved
- * projections cut to 24 bits, everything else is rounded once, as output.  fp32 state: activations enter the
- * products as three bf16 parts that add up to them exactly, so that results
- * have fp32 accuracy (for the bf16 weights).                                */
+ * projections cut to 24 bits, everything else is rounded once, as output.
+ * fp32 state: activations enter the products as three bf16 parts that add up
+ * to them exactly, so that results have fp32 accuracy (for the bf16 weights). */
 typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1 } xhc_act;
 size_t xhc_packed_ffn_bytes(const xhc_dims* d, int32_t H, int32_t with_bwd);
 size_t xhc_ffn_saved_bytes(const xhc_dims* d, int32_t H);

@@ -249,7 +249,8 @@ template <> struct Saved<uint16_t> {
   }
 };
 
-// Rows [T, C] into fragments, one wave a fragment; rows up to a whole block and columns up to 64 are zero.  Bound by HBM:
+// Rows [T, C] into fragments, one wave a fragment; rows up to a whole block and
+// columns up to 64 are zero.  Bound by HBM:
 // each element read once, written once.
 template <typename TS>
 __global__ __launch_bounds__(256) void k_ffn_arrange(const TS* __restrict__ x, const TS* __restrict__ x2, int64_t T,
