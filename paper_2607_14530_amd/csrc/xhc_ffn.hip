@@ -643,6 +643,12 @@ using SmallCols = Shape<2, 2, 2, 2, 2, 2>;
 // 128 n by 64 tokens
 using Narrow = Shape<2, 1, 2, 2, 1, 6>;
 constexpr int64_t kNarrow = 64;
+// 64 by 64: four times the workgroups and a quarter of the epilogue's values per
+// lane, which count where a product is short (T = 96, C = 256, H = 683 forward
+// and backward 82 us without these tiles, 62 with them)
+using TinyRows = Shape<1, 1, 2, 2, 1, 6>;
+using TinyCols = Shape<1, 1, 2, 2, 2, 3>;
+constexpr int64_t kTiny = 32;          // their mark in a plan
 
 // How a product runs: its tile and the parts that k is cut into.
 struct Plan {
@@ -651,24 +657,29 @@ struct Plan {
   int64_t rest_ksteps;                 // their stages
   int nseg, parts;
 };
-// Tiles of 256 x 256 (a workgroup per CU) or 128 x 128 (two), with k in parts
-// where there are few of them; by an estimate of the time in us.
+// Tiles of 256 x 256 (a workgroup per CU), 128 x 128 (two) or 64 x 64 (three),
+// with k in parts where there are few of them; by an estimate of the time in us.
 // Measured per 32 k and round: a large tile 0.8 on a full chip, below half of it
 // 0.6 (power); small ones 0.57, 0.5 where not every CU has two, 0.3 where none
-// has.  Parts cost a write and a read of fp32 sums and a launch: T = 512, C =
+// has; tiny ones 0.35, 0.25 and 0.2 with three, two and one.  Parts cost a write and a read of fp32 sums and a launch: T = 512, C =
 // 2560, H = 6912 dx (80 small tiles of 432 steps) 242 us with large tiles, 120
 // with small ones, 66 in 4 parts; T = 2048 (80 large tiles of 432) backward 527
-// without parts of large tiles, 487 with them.  A rest of small tiles: T = 4096, C = 2560, H =
-// 6912 forward 450 -> 437, backward 977 -> 926.
+// without parts of large tiles, 487 with them.  A rest of small tiles: T = 4096,
+// C = 2560, H = 6912 forward 450 -> 437, backward 977 -> 926.  Tiny ones: C =
+// 1024, H = 2816 T = 200 43 -> 34 and 61 -> 51, T = 1500 69 -> 65 and 111 -> 110.
+// `narrow` takes 128 x 64 alone: it is reached with large weights, whose tiny
+// tiles read the tokens twice as often (T = 64, C = 4096, H = 11008 forward 120,
+// 112 so).
 Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64_t out, bool narrow = false) {
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   Plan best{};
   double least = 0;
-  for (int kind = narrow ? 2 : 0; kind < 3; ++kind) {   // large tiles, with a rest of small ones, small tiles
+  // large tiles, with a rest of small ones, small ones, tiny ones
+  for (int kind = narrow ? 2 : 0; kind < (narrow ? 3 : 4); ++kind) {
     Plan p{};
-    const int64_t tile = p.tile = kind < 2 ? 256 : narrow ? kNarrow : 128;
-    p.gn = up(n, std::max<int64_t>(tile, 128));
-    p.gt = up(t, tile);
+    const int64_t tile = p.tile = kind < 2 ? 256 : kind == 3 ? kTiny : narrow ? kNarrow : 128;
+    p.gn = up(n, kind == 3 ? 64 : std::max<int64_t>(tile, 128));
+    p.gt = up(t, kind == 3 ? 64 : tile);
     p.nseg = nseg;
     const int stage = tile == 256 ? 32 : stage128;
     p.ksteps = std::max<int64_t>(1, up(k, stage));   // no tokens: one stage of zeros
@@ -685,11 +696,14 @@ Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64
         p.rest = kind == 1 && w > 256 && w % 256 <= 128 ? w % 256 : 0;
         if (kind == 1 && p.rest == 0) continue;
         rounds = w <= 128 ? 0.6 : 0.8 * up(w - p.rest, 256) + (p.rest == 0 ? 0 : p.rest <= 64 ? 0.3 : 0.57);
+      } else if (kind == 3) {
+        const int64_t rest = w % 768;
+        rounds = 0.35 * (w / 768) + (rest == 0 ? 0 : rest <= 256 ? 0.2 : rest <= 512 ? 0.25 : 0.35);
       } else {
         const int64_t rest = w % 512;
         rounds = 0.57 * (w / 512) + (rest == 0 ? 0 : rest <= 256 ? 0.3 : 0.5);
       }
-      double us = rounds * p.per * (stage / 32) + 3;
+      double us = rounds * p.per * (stage / 32) + (kind == 3 ? up(w, 768) : 3);   // and the epilogue
       if (p.rest) us += 8;
       if (parts > 1) us += 4 + (double)parts * out * 8 / 3.5e6;
       if (least == 0 || us < least) {
@@ -757,6 +771,8 @@ hipError_t rows(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hip
     if (p.rest)
       k_ffn_rows<SmallRows, Epi>
           <<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallRows::NW), 0, s>>>(rest_of(p, a), e, part);
+  } else if (p.tile == kTiny) {
+    k_ffn_rows<TinyRows, Epi><<<grid_of(p), dim3(64 * TinyRows::NW), 0, s>>>(a, e, part);
   } else if (p.tile == kNarrow) {
     k_ffn_rows<Narrow, Epi><<<grid_of(p), dim3(64 * Narrow::NW), 0, s>>>(a, e, part);
   } else {
@@ -775,6 +791,8 @@ hipError_t cols(const Plan& p, const GemmArgs& a, const Epi& e, float* part, hip
     if (p.rest)
       k_ffn_cols<SmallCols, Epi>
           <<<dim3((unsigned)(4 * p.rest)), dim3(64 * SmallCols::NW), 0, s>>>(rest_of(p, a), e, part);
+  } else if (p.tile == kTiny) {
+    k_ffn_cols<TinyCols, Epi><<<grid_of(p), dim3(64 * TinyCols::NW), 0, s>>>(a, e, part);
   } else {
     k_ffn_cols<SmallCols, Epi><<<grid_of(p), dim3(64 * SmallCols::NW), 0, s>>>(a, e, part);
   }
