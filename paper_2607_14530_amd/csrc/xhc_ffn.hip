@@ -665,7 +665,9 @@ struct Plan {
 // 2560, H = 6912 dx (80 small tiles of 432 steps) 242 us with large tiles, 120
 // with small ones, 66 in 4 parts; T = 2048 (80 large tiles of 432) backward 527
 // without parts of large tiles, 487 with them.  A rest of small tiles: T = 4096,
-// C = 2560, H = 6912 forward 450 -> 437, backward 977 -> 926.  Tiny ones: C =
+// C = 2560, H = 6912 forward 450 -> 437, backward 977 -> 926.  An fp32 state's
+// epilogue taken as long as others: T = 1024, C = 1024, H = 2816 backward 260,
+// 248 so.  Tiny ones: C =
 // 1024, H = 2816 T = 200 43 -> 34 and 61 -> 51, T = 1500 69 -> 65 and 111 -> 110.
 // `narrow` takes 128 x 64 alone: it is reached with large weights, whose tiny
 // tiles read the tokens twice as often (T = 64, C = 4096, H = 11008 forward 120,
@@ -703,7 +705,8 @@ Plan plan_product(int64_t n, int64_t t, int64_t k, int nseg, int stage128, int64
         const int64_t rest = w % 512;
         rounds = 0.57 * (w / 512) + (rest == 0 ? 0 : rest <= 256 ? 0.3 : 0.5);
       }
-      double us = rounds * p.per * (stage / 32) + (kind == 3 ? up(w, 768) : 3);   // and the epilogue
+      const double epilogue = nseg == 3 ? 8 : 3;   // three-part activations: many values to write
+      double us = rounds * p.per * (stage / 32) + (kind == 3 ? epilogue / 4 * up(w, 768) : epilogue);
       if (p.rest) us += 8;
       if (parts > 1) us += 4 + (double)parts * out * 8 / 3.5e6;
       if (least == 0 || us < least) {
