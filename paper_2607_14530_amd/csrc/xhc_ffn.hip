@@ -733,35 +733,51 @@ GemmArgs rest_of(const Plan& p, GemmArgs a) {
 dim3 grid_of(const Plan& p) { return dim3((unsigned)(p.gn * p.gt - p.rest), (unsigned)p.parts); }
 
 // Whether k_ffn_few runs (and reads an input of bf16 rows as it lies): up to 16
-// tokens, up to 64 where the weights are small.  Its workgroups read all
-// activations again for every block or two of n, the tiles for every eight; but
-// the tiles take two launches more.  us, forward: T = 64, C = 1024, H = 2816 17
-// here and 25 in tiles, C = 2112, H = 5637 T = 37 35 and 37, T = 64 40 and 38; C
-// = 4096, H = 11008 T = 32 83 and 74, T = 64 101 and 76.
+// tokens, up to 64 where the block is small.  Its workgroups read all activations
+// again for every block or two of n, the tiles for every eight; but the tiles take
+// two launches more, and three passes over the weights for an fp32 state.  us,
+// forward, here and in tiles: C = 1024, H = 2816 T = 64 15 and 25, C = 2560, H =
+// 6912 T = 32 33 and 39, T = 64 46 and 42; C = 4096, H = 11008 T = 32 81 and 72.
+// fp32 state: C = 4096, H = 11008 T = 48 127 and 139, T = 64 153 and 145.
 constexpr int64_t kFewMost = 64;
-bool few_tokens(int64_t T, int64_t C, int64_t H) { return T <= 16 || (T <= kFewMost && C * H <= (1 << 24)); }
+bool few_tokens(bool f32, int64_t T, int64_t C, int64_t H) {
+  return T <= 16 || (T <= kFewMost && T * (C * H) <= (int64_t)5 << (f32 ? 29 : 27));
+}
 // all n blocks of the packed matrix a.n; ldx: elements between rows of the activations, 0 for fragments
 template <class Epi>
 hipError_t few(const GemmArgs& a, int64_t ldx, const Epi& e, hipStream_t s) {
   const FewArgs f{reinterpret_cast<const uint4*>(a.n.p), a.n.kb, (int)a.t.kb,
                   reinterpret_cast<const uint16_t*>(a.t.p), ldx, a.t.plane / 2, (int)e.T};
-  // Blocks of 16 n per workgroup: one (with its gate's: two) up to 16 tokens,
-  // twice as many beyond, where the activations' bytes count, too.  Waves: 16,
-  // for the most loads in flight where there are few blocks; fewer where their
-  // sums would not fit LDS (gate and up) or their fragments the registers that
-  // 16 waves have (three-part activations).
+  // Blocks of 16 n per workgroup: one (with its gate's: two) up to 16 tokens and
+  // where twice as many would leave more than half of the CUs idle; else twice as
+  // many, as the activations' bytes count, too (us, forward, one and two: C =
+  // 1024, H = 2816 T = 24 10.4 and 12.8, T = 64 15 and 17, C = 2560, H = 6528 T =
+  // 48 46 and, gate and up in twos, 41).  Waves: 16, for the most loads in flight
+  // where there are few blocks; fewer where their sums would not fit LDS (gate and
+  // up), their fragments the registers that 16 waves have (three-part
+  // activations), or where the parts of k would be short.
   constexpr bool two = Epi::kTwo, f32 = Epi::kParts == 3;
   constexpr int PER = two ? 2 : 1;
   const unsigned g1 = (unsigned)(a.n.rows / PER), g2 = g1 / 2;
   if (e.T <= 16) {
     constexpr int NW = two ? 8 : 16;
     k_ffn_few<PER, 1, NW, f32 ? 2 : 4, Epi><<<dim3(g1), dim3(64 * NW), 0, s>>>(f, e);
-  } else if (e.T <= 32) {
-    constexpr int NW = two ? 8 : 16;
-    k_ffn_few<2 * PER, 2, NW, f32 ? 1 : 2, Epi><<<dim3(g2), dim3(64 * NW), 0, s>>>(f, e);
+  } else if (g2 >= 128) {
+    constexpr int NW32 = two ? 8 : 16, NW = two ? 4 : f32 ? 8 : 16, U = two && !f32 ? 2 : 1;
+    if (e.T <= 32)
+      k_ffn_few<2 * PER, 2, NW32, f32 ? 1 : 2, Epi><<<dim3(g2), dim3(64 * NW32), 0, s>>>(f, e);
+    else if (e.T <= 48)
+      k_ffn_few<2 * PER, 3, NW, U, Epi><<<dim3(g2), dim3(64 * NW), 0, s>>>(f, e);
+    else
+      k_ffn_few<2 * PER, 4, NW, U, Epi><<<dim3(g2), dim3(64 * NW), 0, s>>>(f, e);
   } else {
-    constexpr int NW = two ? 4 : f32 ? 8 : 16;
-    k_ffn_few<2 * PER, 4, NW, two && !f32 ? 2 : 1, Epi><<<dim3(g2), dim3(64 * NW), 0, s>>>(f, e);
+    constexpr int NW = two ? 4 : 8, U = f32 ? 1 : two ? 4 : 2;
+    if (e.T <= 32)
+      k_ffn_few<PER, 2, NW, f32 ? 2 : U, Epi><<<dim3(g1), dim3(64 * NW), 0, s>>>(f, e);
+    else if (e.T <= 48)
+      k_ffn_few<PER, 3, NW, U, Epi><<<dim3(g1), dim3(64 * NW), 0, s>>>(f, e);
+    else
+      k_ffn_few<PER, 4, NW, U, Epi><<<dim3(g1), dim3(64 * NW), 0, s>>>(f, e);
   }
   return hipGetLastError();
 }
@@ -830,7 +846,7 @@ struct Ws {
     dgu = take(bwd ? (size_t)P * rows * pk.Hp * 4 : 0);
     size_t most = 0;
     const auto product = [&](int64_t n, int64_t k) {       // of the tokens by packed weights
-      if (few_tokens(T, C, H)) return Plan{};
+      if (few_tokens(f32, T, C, H)) return Plan{};
       const Plan p = plan_product(n, T, k, ns, 32, rows * n, T <= kNarrow);
       most = std::max(most, part_floats(p, rows, n));
       return p;
@@ -874,7 +890,7 @@ hipError_t ffn(int state_dtype, int64_t T, int64_t C, int64_t H, int act, const 
                void* F, void* saved, void* workspace, hipStream_t s) {
   const Packed pk(C, H);
   const Ws w(state_dtype, T, C, H, false);
-  const bool f32 = state_dtype == XHC_F32, direct = !f32 && few_tokens(T, C, H);
+  const bool f32 = state_dtype == XHC_F32, direct = !f32 && few_tokens(f32, T, C, H);
   char* ws = reinterpret_cast<char*>(workspace);
   const char* pw = reinterpret_cast<const char*>(packed);
   const Segments seg = f32 ? segs_weights() : segs_bf16();

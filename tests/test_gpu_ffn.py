@@ -62,3 +62,34 @@ def test_large_tiles_and_a_rest_of_small_ones(state, T, C, H):
     assert_within(dx, bw["dx"], "dx")
     for n in ("W_gate", "W_up", "W_down"):
         assert_within(ff.grads[n], bw[n], "d" + n)
+
+
+def check(T, C, H, state, seed):
+    x, dF, w, ff = make(T, C, H, state, "silu", seed, True)
+    F = ff.forward(x.cuda())
+    dx = ff.backward(dF.cuda())
+    torch.cuda.synchronize()
+    half = HALF[DT[state]]
+    fw = ffn_forward(x, w, "silu", half)
+    assert_within(F, fw["F"], "F")
+    bw = ffn_backward(x, dF, fw, "silu", half)
+    assert_within(dx, bw["dx"], "dx")
+    for n in ("W_gate", "W_up", "W_down"):
+        assert_within(ff.grads[n], bw[n], "d" + n)
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [16, 17, 32, 33, 48, 49, 64])
+@pytest.mark.parametrize("C,H", [(64, 4160), (4128, 65), (224, 350)])
+def test_few_tokens_with_many_and_few_blocks_of_weights(C, H, T, state):
+    check(T, C, H, state, 400 + T)
+
+
+def test_few_tokens_with_large_weights_and_an_fp32_state():
+    check(61, 4128, 10700, "f32", 500)
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32"])
+@pytest.mark.parametrize("T,C,H", [(97, 256, 683), (190, 544, 1311), (700, 320, 70), (1100, 96, 200)])
+def test_short_products(T, C, H, state):
+    check(T, C, H, state, 600 + T)
