@@ -294,7 +294,9 @@ __global__ __launch_bounds__(64) void k_rmsnorm_dw_wide(const TS* __restrict__ x
 }
 
 // dw[c] = sum over the rows of part, in order: 16 threads take every 16th row
-// of a column, then their sums are added in order
+// of a column, kDwRows on the way, then their sums are added in order (512 rows
+// of C = 4096: 4.8 us, 9.7 with a row at a time)
+constexpr int kDwRows = 16;
 __global__ __launch_bounds__(256) void k_rmsnorm_dw(const float* __restrict__ part, int rows, int C,
                                                     float* __restrict__ dw) {
   __shared__ float red[16][16];
@@ -302,7 +304,13 @@ __global__ __launch_bounds__(256) void k_rmsnorm_dw(const float* __restrict__ pa
   const int c = (int)blockIdx.x * 16 + cl;
   float s = 0.f;
   if (c < C)
-    for (int i = g; i < rows; i += 16) s += part[(int64_t)i * C + c];
+    for (int i = g; i < rows; i += 16 * kDwRows) {
+      float f[kDwRows];
+#pragma unroll
+      for (int u = 0; u < kDwRows; ++u) f[u] = i + 16 * u < rows ? part[(int64_t)(i + 16 * u) * C + c] : 0.f;
+#pragma unroll
+      for (int u = 0; u < kDwRows; ++u) s += f[u];
+    }
   red[g][cl] = s;
   __syncthreads();
   if (g == 0 && c < C) {
