@@ -154,7 +154,7 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream   # an index: looked up fastest
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -330,20 +330,25 @@ def xhc_ffn_bwd(d, H, act, input, packed, saved, dF, d_input, dW_gate, dW_up, dW
           _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down), _ptr(workspace), _nbytes(workspace), _stream(stream))
 
 
+_GRAD_DTYPES = {torch.bfloat16: XHC_BF16, torch.float32: XHC_F32}
+
+
+def _ptrs(tensors):
+    """Host array of the tensors' addresses."""
+    for t in tensors:
+        if not (t.is_cuda and t.is_contiguous()):
+            _ptr(t)
+    return (_P * len(tensors))(*[t.data_ptr() for t in tensors])
+
+
 def _grad_arrays(grads):
     """Host arrays of the tensors' addresses, counts and dtypes."""
-    ptrs, counts, dtypes = [], [], []
     for g in grads:
-        if g.dtype is torch.bfloat16:
-            dtypes.append(XHC_BF16)
-        elif g.dtype is torch.float32:
-            dtypes.append(XHC_F32)
-        else:
+        if g.dtype not in _GRAD_DTYPES:
             raise ValueError(f"gradients are bf16 or fp32, got {g.dtype}")
-        ptrs.append(_ptr(g))
-        counts.append(g.numel())
-    n = len(ptrs)
-    return (_P * n)(*ptrs), (ctypes.c_int64 * n)(*counts), (ctypes.c_int32 * n)(*dtypes)
+    n = len(grads)
+    return (_ptrs(grads), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
+            (ctypes.c_int32 * n)(*[_GRAD_DTYPES[g.dtype] for g in grads]))
 
 
 def xhc_grad_workspace_bytes(n):
@@ -366,7 +371,7 @@ def xhc_grad_clip(grads, max_norm, outs, norm, workspace, stream=None):
         for g, o in zip(grads, outs):
             if o.dtype is not g.dtype or o.shape != g.shape:
                 _expect(o, g.dtype, g.shape, "output of a gradient")
-        to = (_P * len(outs))(*[_ptr(o) for o in outs])
+        to = _ptrs(outs)
     _call("xhc_grad_clip", len(grads), ptrs, counts, dtypes, max_norm, to, _ptr(norm), _ptr(workspace),
           _nbytes(workspace), _stream(stream))
 
