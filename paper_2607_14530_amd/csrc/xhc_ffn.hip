@@ -460,7 +460,25 @@ __global__ __launch_bounds__(64 * S::NW) void k_ffn_rows(const GemmArgs a, const
   });
 }
 
-// the parts of k added in order, then the epilogue
+// eight columns of the parts of k added in order, four parts on the way (eleven
+// one after another, T = 96, C = 256: 5.6 us, 4.0 so)
+__device__ __forceinline__ void add_parts(const float* p, int64_t stride, int parts, float (&v)[8]) {
+  constexpr int AHEAD = 4;
+  for (int i = 0; i < parts; i += AHEAD, p += AHEAD * stride) {
+    float f[AHEAD][8];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (i + u < parts) Vec8<float>::load(p + u * stride, f[u]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (i + u < parts) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] += f[u][x];
+      }
+  }
+}
+
+// the parts joined, then the epilogue
 template <class Epi>
 __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float* __restrict__ part, int parts) {
   const int64_t g = e.cols / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -469,18 +487,8 @@ __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float*
   const Place at = place_of(t, c, e.cols);
   const auto pre = e.template fetch<8>(at);
   float v[8] = {}, w[8] = {};
-  for (int p = 0; p < parts; ++p) {
-    const float* s = part + ((int64_t)p * e.rows + t) * ld + c;
-    float f[8];
-    Vec8<float>::load(s, f);
-#pragma unroll
-    for (int x = 0; x < 8; ++x) v[x] += f[x];
-    if (Epi::kTwo) {
-      Vec8<float>::load(s + e.cols, f);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) w[x] += f[x];
-    }
-  }
+  add_parts(part + t * ld + c, e.rows * ld, parts, v);
+  if (Epi::kTwo) add_parts(part + t * ld + c + e.cols, e.rows * ld, parts, w);
   e.template finish<8>(at, v, w, pre);
 }
 
@@ -621,12 +629,7 @@ __global__ __launch_bounds__(256) void k_ffn_cols_join(const Epi e, const float*
   const int64_t m = i / g, n = i % g * 8;
   if (m >= e.M) return;
   float v[8] = {};
-  for (int p = 0; p < parts; ++p) {
-    float f[8];
-    Vec8<float>::load(part + ((int64_t)p * e.M + m) * e.N + n, f);
-#pragma unroll
-    for (int x = 0; x < 8; ++x) v[x] += f[x];
-  }
+  add_parts(part + m * e.N + n, e.M * e.N, parts, v);
   e.finish(m, n, v);
 }
 
