@@ -13,27 +13,14 @@
 #include <math.h>
 
 #include "xhc_device.h"
+#include "xhc_grad_launches.h"
 
 namespace xhc {
 
 namespace {
 
 constexpr int kGradThreads = 256;
-constexpr int64_t kChunks = 16384;
 constexpr int kGradVecs = 8;         // vectors of 8 elements that a thread has on the way
-
-// Tensors of one launch.  first[i]: the launch's first chunk of tensor i;
-// first[n]: its chunks.  28 bytes a tensor, under the 4 KiB of a launch's arguments.
-struct GradBatch {
-  uint64_t src[kGradBatch], dst[kGradBatch];
-  int64_t count[kGradBatch];
-  int32_t first[kGradBatch + 1];
-  uint64_t f32[kGradBatch / 64];   // a bit for each tensor: fp32, else bf16
-  int32_t n;
-  int32_t chunk;                   // elements, a multiple of 8
-  int64_t part_at;                 // the launch's first chunk among all
-};
-static_assert(sizeof(GradBatch) + 64 <= 4096, "the arguments of a launch");
 
 struct GradChunk {
   int i;
@@ -130,10 +117,6 @@ __device__ __forceinline__ float clip_factor(double norm, float max_norm) {
   return c < 1.0 ? (float)c : 1.0f;
 }
 
-// Few chunks: every workgroup of the clip adds them itself, in the same order,
-// instead of waiting for a launch that does (ten small tensors 8.9 us of kernels,
-// 10 in three launches, and the time between two).
-constexpr int kOwnSum = 512;
 constexpr int kNormThreads = 1024;
 __global__ __launch_bounds__(kNormThreads) void k_grad_norm(const double* __restrict__ part, int64_t chunks,
                                                             float max_norm, float* __restrict__ norm,
@@ -218,72 +201,36 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_scale(const GradBatch b, 
     chunk_scale(reinterpret_cast<const uint16_t*>(src) + k.at, reinterpret_cast<uint16_t*>(dst) + k.at, k.n, c);
 }
 
-// Elements per chunk: about kChunks chunks in all, and not under 8192 elements,
-// below which a workgroup's start costs more than its bytes.  (With 4096 chunks
-// the last workgroups run long alone: the clip pass over 617 MB 240 us, 210 with
-// 16384; their sum then takes 7 us instead of 5.)
-int64_t chunk_elems(int n, const int64_t* counts) {
-  int64_t total = 0;
-  for (int i = 0; i < n; ++i) total += counts[i];
-  int64_t c = (total / kChunks + 2047) / 2048 * 2048;
-  return c < 8192 ? 8192 : c;
-}
-
-// the table of the tensors from i on, as many as it takes; the tensor after them
-int fill_batch(GradBatch& b, int i, int n, const void* const* grads, void* const* outs, const int64_t* counts,
-               const int32_t* dtypes, int64_t chunk, int64_t part_at) {
-  b.n = 0;
-  b.chunk = (int32_t)chunk;
-  b.part_at = part_at;
-  for (int w = 0; w < kGradBatch / 64; ++w) b.f32[w] = 0;
-  b.first[0] = 0;
-  for (; i < n && b.n < kGradBatch; ++i) {
-    if (counts[i] == 0) continue;
-    b.src[b.n] = (uint64_t)(uintptr_t)grads[i];
-    b.dst[b.n] = outs ? (uint64_t)(uintptr_t)outs[i] : 0;
-    b.count[b.n] = counts[i];
-    if (dtypes[i] == XHC_F32) b.f32[b.n / 64] |= 1ull << (b.n % 64);
-    b.first[b.n + 1] = b.first[b.n] + (int32_t)((counts[i] + chunk - 1) / chunk);
-    ++b.n;
+// the launches themselves, on a stream
+struct GradStream {
+  double* part;
+  float *factor, *norm_out;
+  float max_norm;
+  hipStream_t s;
+  hipError_t squares(const GradBatch& b) {
+    k_grad_squares<<<dim3((unsigned)b.first[b.n]), dim3(kGradThreads), 0, s>>>(b, part);
+    return hipGetLastError();
   }
-  return i;
-}
+  hipError_t norm(int64_t chunks, bool clip) {
+    k_grad_norm<<<dim3(1), dim3(kNormThreads), 0, s>>>(part, chunks, max_norm, norm_out, clip ? factor : nullptr);
+    return hipGetLastError();
+  }
+  hipError_t scale(const GradBatch& b, bool own, int64_t chunks) {
+    k_grad_scale<<<dim3((unsigned)b.first[b.n]), dim3(kGradThreads), 0, s>>>(b, factor, own ? part : nullptr,
+                                                                             (int)chunks, max_norm, norm_out);
+    return hipGetLastError();
+  }
+};
 
 }  // namespace
 
-// the factor, then the chunks' sums: at most kChunks whole chunks and a last one for each tensor
-size_t grad_ws_bytes(int n) { return 16 + (size_t)(kChunks + n) * sizeof(double); }
+size_t grad_ws_bytes(int n) { return 16 + grad_places(n) * sizeof(double); }
 
 hipError_t launch_grad_clip(int n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
                             float max_norm, void* const* outs, float* norm, void* ws, hipStream_t s) {
-  float* factor = reinterpret_cast<float*>(ws);
-  double* part = reinterpret_cast<double*>(reinterpret_cast<char*>(ws) + 16);
-  const int64_t chunk = chunk_elems(n, counts);
-  GradBatch b;
-  int64_t chunks = 0;
-  int starts[kMaxGrads / kGradBatch + 1], batches = 0;   // the first tensor of each launch
-  for (int i = 0; i < n;) {
-    const int at = i;
-    i = fill_batch(b, i, n, grads, outs, counts, dtypes, chunk, chunks);
-    if (b.n == 0) break;
-    starts[batches++] = at;
-    k_grad_squares<<<dim3((unsigned)b.first[b.n]), dim3(kGradThreads), 0, s>>>(b, part);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    chunks += b.first[b.n];
-  }
-  const bool own = outs && batches == 1 && chunks <= kOwnSum;
-  if (!own) {
-    k_grad_norm<<<dim3(1), dim3(kNormThreads), 0, s>>>(part, chunks, max_norm, norm, outs ? factor : nullptr);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || !outs) return e;
-  }
-  // the last launch's tensors first; its table is still there
-  for (int k = batches - 1; k >= 0; --k) {
-    if (k < batches - 1) fill_batch(b, starts[k], n, grads, outs, counts, dtypes, chunk, 0);
-    k_grad_scale<<<dim3((unsigned)b.first[b.n]), dim3(kGradThreads), 0, s>>>(b, factor, own ? part : nullptr,
-                                                                             (int)chunks, max_norm, norm);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  GradStream launch{reinterpret_cast<double*>(reinterpret_cast<char*>(ws) + 16), reinterpret_cast<float*>(ws), norm,
+                    max_norm, s};
+  return grad_launches(launch, n, grads, counts, dtypes, outs);
 }
 
 }  // namespace xhc
