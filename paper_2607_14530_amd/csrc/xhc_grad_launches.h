@@ -70,13 +70,14 @@ template <class L>
 hipError_t grad_launches(L& launch, int n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
                          void* const* outs) {
   const int64_t chunk = chunk_elems(n, counts);
+  // empty tensors behind the last other one would make a table of their own, with no chunk
+  while (n > 0 && counts[n - 1] == 0) --n;
   GradBatch b;
   int64_t chunks = 0;
   int starts[kMaxGrads / kGradBatch + 1], batches = 0;   // the first tensor of each launch
   for (int i = 0; i < n;) {
     const int at = i;
     i = fill_batch(b, i, n, grads, outs, counts, dtypes, chunk, chunks);
-    if (b.n == 0) break;
     starts[batches++] = at;
     if (hipError_t e = launch.squares(b); e != hipSuccess) return e;
     chunks += b.first[b.n];

@@ -32,3 +32,35 @@ def test_the_workspace_of_the_query_is_enough(q):
     v = 0.5 / (ref + 1e-6) * 2.0 ** -10
     assert bool((out == out[0]).all())
     assert abs(float(out[0]) - v) <= v * (2.0 ** -8 + 2.1 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("empty", [1, 200])
+@pytest.mark.parametrize("full", [128, 256])
+@pytest.mark.parametrize("size", [10, 40000])
+def test_full_tables_followed_by_empty_tensors(full, empty, size):
+    """As many tensors as whole launches take, then empty ones: clipped as
+    without those, into other buffers and in place, with few sums and many."""
+    gen = torch.Generator(device="cuda").manual_seed(full + size)
+    base = [torch.randn(size + i % 7, generator=gen, device="cuda").to(BF if i % 3 else F32) for i in range(full)]
+    none = [torch.empty(0, device="cuda") for _ in range(empty)]
+    outs = [torch.full_like(g, 7.0) for g in base]
+    ref = X.clip_grad_norm(base, 0.5, outs=outs)
+    total = sum(float(g.double().pow(2).sum()) for g in base) ** 0.5
+    assert abs(float(ref) - total) <= 2.0 ** -24 * total * 1.001
+    outs2 = [torch.full_like(g, 7.0) for g in base]
+    norm = X.clip_grad_norm(base + none, 0.5, outs=outs2 + [torch.empty(0, device="cuda") for _ in none])
+    assert torch.equal(norm, ref)
+    assert all(torch.equal(a, b) for a, b in zip(outs, outs2))
+    n2 = torch.empty(1, device="cuda")
+    X.xhc_grad_norm(base + none, n2,
+                    torch.empty(X.xhc_grad_workspace_bytes(full + empty), dtype=torch.uint8, device="cuda"))
+    assert torch.equal(n2, ref)
+    inplace = [g.clone() for g in base]
+    assert torch.equal(X.clip_grad_norm(inplace + none, 0.5), ref)
+    assert all(torch.equal(a, b) for a, b in zip(outs, inplace))
+    # every value is clipped: c and the product rounded to fp32, a bf16 output once more
+    c = 0.5 / (total + 1e-6)
+    for g, o in zip(base, outs):
+        v = g.double() * c
+        tol = v.abs() * (2.1 * 2.0 ** -24 + (2.0 ** -8 if g.dtype == BF else 0)) + 1e-40
+        assert bool(((o.double() - v).abs() <= tol).all())

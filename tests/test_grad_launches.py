@@ -94,3 +94,15 @@ def test_every_sum_has_a_place(record, q, more):
 def test_the_largest_total(record):
     check(record, [1 << 40])
     check(record, [(1 << 40) - 4095] + [1] * 4095)
+
+
+@pytest.mark.parametrize("full", [0, 1, 127, 128, 129, 256, 384])
+@pytest.mark.parametrize("empty", [0, 1, 127, 128, 300])
+def test_empty_tensors_at_any_place(record, full, empty):
+    """Empty tensors before, behind and between the others: no launch without
+    a chunk, none left out."""
+    some = [5 + 9000 * (i % 3) for i in range(full)]
+    mixed = [c for i in range(max(full, empty)) for c in some[i:i + 1] + [0] * (i < empty)]
+    for counts in (some + [0] * empty, [0] * empty + some, mixed):
+        check(record, counts)
+        check(record, counts, clip=False)
