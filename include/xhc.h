@@ -446,7 +446,8 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
  *
  * Sums are fp32 (matrix cores), in an order fixed by the sizes.  bf16 state:
  * h and the gradients of the projections are rounded to bf16 and the saved
- * projections cut to 24 bits, everything else is rounded once, as output.
+ * projections cut to 24 bits, everything else is rounded once, as output;
+ * GELU's Phi is within 2^-21 of 1 (not of its value, in the lower tail).
  * fp32 state: activations enter the products as three bf16 parts that add up
  * to them exactly, so that results have fp32 accuracy (for the bf16 weights). */
 typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1 } xhc_act;

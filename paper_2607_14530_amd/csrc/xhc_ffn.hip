@@ -91,28 +91,38 @@ struct Packed {
 
 // ---------------------------------------------------------------- activations
 
-// act(g) and, with D, act'(g).  The distribution function of GELU by formula
-// 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions:
+// act(g) and, with D, act'(g).  The distribution function of GELU: for an fp32
+// state half of the complementary error function at -g / sqrt 2, which keeps its
+// relative accuracy in the lower tail; for a bf16 state formula 7.1.26 of
+// Abramowitz and Stegun, Handbook of Mathematical Functions:
 //   1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2),  t = 1 / (1 + p x),  x >= 0,
-// to 1.5e-7, with x = |g| / sqrt 2: half of that, 2^-23.7, in the distribution,
-// in a dozen instructions that share the exponential with the density (erff is
-// about eighty, and an epilogue has nothing to hide them behind: T = 8192, C =
-// 4096, H = 11008 forward 1827 us with it, 1788 so).
-template <bool D>
+// to 1.5e-7, with x = |g| / sqrt 2: evaluated in fp32 the distribution is within
+// 2^-21 (of 1: 6e-5 of the value at g = -3, 1.7e-3 at -5), below the rounding
+// of h where a sum of them counts, in a dozen instructions that share the
+// exponential with the density (erff is about eighty, and an epilogue has nothing
+// to hide them behind: T = 8192, C = 4096, H = 11008 forward 1827 us with it,
+// 1788 so).
+template <bool D, typename TS>
 __device__ __forceinline__ float act_of(int act, float g, float& d) {
   if (act == XHC_ACT_SILU) {
     const float e = __builtin_amdgcn_rcpf(1.0f + __expf(-g)), a = g * e;
     if (D) d = fmaf(a, 1.0f - e, e);
     return a;
   }
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.0f));
-  const float x = __expf(-0.5f * g * g);
-  float q = fmaf(t, 1.061405429f, -1.453152027f);
-  q = fmaf(t, q, 1.421413741f);
-  q = fmaf(t, q, -0.284496736f);
-  q = fmaf(t, q, 0.254829592f);
-  q *= 0.5f * t * x;
-  const float e = g < 0.f ? q : 1.0f - q;
+  float e, x;
+  if (sizeof(TS) == 4) {
+    e = 0.5f * erfcf(-0.70710678118654752f * g);
+    if (D) x = __expf(-0.5f * g * g);
+  } else {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.0f));
+    x = __expf(-0.5f * g * g);
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f);
+    q *= 0.5f * t * x;
+    e = g < 0.f ? q : 1.0f - q;
+  }
   if (D) d = fmaf(g * x, 0.39894228040143268f, e);
   return g * e;
 }
@@ -313,7 +323,7 @@ struct EpiUp {
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       float d;
-      f[e] = act_of<false>(act, g[e], d) * u[e];
+      f[e] = act_of<false, TS>(act, g[e], d) * u[e];
     }
     if (p.c + W > H) {
 #pragma unroll
@@ -370,7 +380,7 @@ struct EpiGate {
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       float d;
-      const float a = act_of<true>(act, g[e], d);
+      const float a = act_of<true, TS>(act, g[e], d);
       f[e] = a * u[e];
       dg[e] = dh[e] * u[e] * d;
       du[e] = dh[e] * a;
