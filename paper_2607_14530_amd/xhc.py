@@ -764,8 +764,9 @@ class TrainableRMSNorm(RMSNorm):
         self.x = None
 
     def forward(self, x, stream=None):
-        self.x = x
-        return super().forward(x, stream)
+        out = super().forward(x, stream)
+        self.x = x                     # (of a forward that ran: a refused one changes nothing)
+        return out
 
     def backward(self, dy, stream=None):
         if self.x is None:
@@ -829,8 +830,9 @@ class TrainableFeedForward(FeedForward):
         self.x = None
 
     def forward(self, x, stream=None):
-        self.x = x
-        return super().forward(x, stream)
+        out = super().forward(x, stream)
+        self.x = x                     # (of a forward that ran: a refused one changes nothing)
+        return out
 
     def backward(self, dF, stream=None):
         if self.x is None:
