@@ -706,9 +706,17 @@ class Stack:
 
 # ---------------------------------------------------------------- the sublayer's own function
 
+def _enqueues(dev):
+    """Refuses a call of a bundle while another device is current: it would be enqueued there."""
+    if dev.type == "cuda" and torch.cuda.current_device() != dev.index:
+        raise ValueError(f"the current device is cuda:{torch.cuda.current_device()}, not the bundle's {dev}")
+
+
 def _on(t, dev, name):
+    """An argument of a bundle's call, on the bundle's device, which is the current one."""
     if t.device != dev:
         raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    _enqueues(dev)
 
 
 def _here(device):
@@ -801,6 +809,7 @@ class FeedForward:
         w = [weights[n] for n in ("W_gate", "W_up", "W_down")]
         for t, n in zip(w, ("W_gate", "W_up", "W_down")):
             _expect(t, torch.float32, (self.H, self.d.C) if n == "W_down" else (self.d.C, self.H), n)
+        _enqueues(self.device)
         with _within(stream):
             w = [t.to(self.device).contiguous() for t in w]
         xhc_pack_ffn(self.d, self.H, *w, self.with_bwd, self.packed, stream)

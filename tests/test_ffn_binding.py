@@ -1,6 +1,8 @@
 """What the bundles of the norm and the feed-forward block hand to the C entry
 points, with those replaced by a record (no GPU needed)."""
 
+from types import SimpleNamespace
+
 import pytest
 import torch
 
@@ -48,3 +50,24 @@ def test_a_refused_forward_leaves_the_last_ones_input(calls, make, back, at):
             f.forward(b)
         f.backward(dy)
         assert calls[-1][0] == back and calls[-1][1][at] is x
+
+
+@pytest.mark.parametrize("make", [norm, block])
+def test_a_call_while_another_device_is_current_is_refused(calls, make, monkeypatch):
+    """Launches go to the current device: it has to be the one that holds the bundle's buffers."""
+    f, there = make(), torch.device("cuda", 1)
+    x = SimpleNamespace(dtype=BF, shape=(T, C), device=there, is_cuda=True, is_contiguous=lambda: True)
+    f.device = there
+    current = [1]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    f.forward(x)
+    f.backward(x)
+    current[0] = 0
+    made = len(calls)
+    for call in (f.forward, f.backward):
+        with pytest.raises(ValueError, match="current device"):
+            call(x)
+    if make is block:
+        with pytest.raises(ValueError, match="current device"):
+            f.pack({"W_gate": torch.ones(C, H), "W_up": torch.ones(C, H), "W_down": torch.ones(H, C)})
+    assert len(calls) == made
