@@ -418,7 +418,7 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
  * xhc_rmsnorm_bwd: dx [T,C] = r v - x r^3 mean_c(v x), v = dy gain, in the
  *   state dtype; dgain [C] fp32 = sum_t dy x r (zero for T = 0), summed in a
  *   fixed order.  workspace: xhc_rmsnorm_workspace_bytes(d) bytes.
- * XHC_EUNSUPPORTED above 2^23 rows.                                         */
+ * XHC_EUNSUPPORTED above 2^23 rows or 2^27 columns.                         */
 size_t xhc_rmsnorm_workspace_bytes(const xhc_dims* d);
 xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void* y, float* rstd, void* stream);
 xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, const float* rstd, const void* dy,

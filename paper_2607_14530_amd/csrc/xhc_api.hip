@@ -1001,8 +1001,10 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
   return hip_status(e);
 }
 
+static bool norm_fits(const xhc_dims* d) { return d->T <= kMaxNormT && d->C <= kMaxNormC; }
+
 size_t xhc_rmsnorm_workspace_bytes(const xhc_dims* d) {
-  return check_dims(d) == XHC_OK && d->T <= kMaxNormT ? rmsnorm_bwd_ws_bytes(d->T, d->C) : 0;
+  return check_dims(d) == XHC_OK && norm_fits(d) ? rmsnorm_bwd_ws_bytes(d->T, d->C) : 0;
 }
 
 xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void* y, float* rstd, void* stream) {
@@ -1011,7 +1013,7 @@ xhc_status xhc_rmsnorm(const xhc_dims* d, const void* x, const float* gain, void
   if (d->T == 0) return XHC_OK;
   if (!x || !gain || !y || x == y || gain == y || (rstd && (rstd == x || rstd == y || rstd == gain)))
     return XHC_EINVAL;
-  if (d->T > kMaxNormT || !aligned16(x) || !aligned16(gain) || !aligned16(y) || !aligned16(rstd))
+  if (!norm_fits(d) || !aligned16(x) || !aligned16(gain) || !aligned16(y) || !aligned16(rstd))
     return XHC_EUNSUPPORTED;
   clear_stale_error();
   hipError_t e = hipSuccess;
@@ -1025,7 +1027,7 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
   xhc_status st = check_dims(d);
   if (st != XHC_OK) return st;
   if (!dgain) return XHC_EINVAL;
-  if (d->T > kMaxNormT) return XHC_EUNSUPPORTED;
+  if (!norm_fits(d)) return XHC_EUNSUPPORTED;
   if (d->T > 0) {
     if (!x || !gain || !rstd || !dy || !dx || !workspace) return XHC_EINVAL;
     for (const void* in : {x, (const void*)gain, (const void*)rstd, dy})

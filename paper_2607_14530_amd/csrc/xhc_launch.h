@@ -300,6 +300,7 @@ hipError_t launch_rmsnorm_bwd(int state_dtype, const void* x, const float* gain,
                               int64_t T, int C, void* dx, float* dgain, float* part, hipStream_t s);
 
 constexpr int64_t kMaxNormT = 1 << 23;       // rows: a launch's threads stay below 2^32
+constexpr int kMaxNormC = 1 << 27;           // columns: so do those of the gain's gradient
 constexpr int kMaxFfn = 1 << 20;             // C and H: a tile's rows stay below 2 GiB
 constexpr int64_t kMaxFfnElems = (int64_t)1 << 34;   // T C, 2 T H and C H: a launch's threads stay below 2^32
 size_t ffn_packed_bytes(int64_t C, int64_t H, bool with_bwd);
