@@ -425,7 +425,8 @@ xhc_status xhc_rmsnorm_bwd(const xhc_dims* d, const void* x, const float* gain, 
                            void* dx, float* dgain, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Gated feed-forward block with H hidden columns (any from 1 to 2^20; C <= 2^20;
- * T C, 2 T H and C H up to 2^34; XHC_EUNSUPPORTED beyond):
+ * T C, 2 T H and C H up to 2^34, T in whole blocks of 16 times C in blocks of
+ * 64 up to 2^35 - 2048; XHC_EUNSUPPORTED beyond):
  *   h = act(input W_gate) * (input W_up),  F = h W_down
  * act: SILU z sigma(z), GELU z Phi(z) (the error function, not its tanh form).
  *

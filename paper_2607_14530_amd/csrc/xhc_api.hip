@@ -1052,6 +1052,7 @@ static xhc_status check_ffn(const xhc_dims* d, int32_t H) {
   if (H < 1) return XHC_EINVAL;
   const int64_t C = d->C, wide = std::max<int64_t>(C, 2 * (int64_t)H);
   if (H > kMaxFfn || C > kMaxFfn || C * H > kMaxFfnElems || d->T > kMaxFfnElems / wide) return XHC_EUNSUPPORTED;
+  if ((d->T + 15) / 16 * ((C + 63) / 64 * 2) > kMaxFfnFrags) return XHC_EUNSUPPORTED;
   return XHC_OK;
 }
 

@@ -303,6 +303,7 @@ constexpr int64_t kMaxNormT = 1 << 23;       // rows: a launch's threads stay be
 constexpr int kMaxNormC = 1 << 27;           // columns: so do those of the gain's gradient
 constexpr int kMaxFfn = 1 << 20;             // C and H: a tile's rows stay below 2 GiB
 constexpr int64_t kMaxFfnElems = (int64_t)1 << 34;   // T C, 2 T H and C H: a launch's threads stay below 2^32
+constexpr int64_t kMaxFfnFrags = ((int64_t)1 << 26) - 4;   // of an input: so do those that bring it into fragments
 size_t ffn_packed_bytes(int64_t C, int64_t H, bool with_bwd);
 size_t ffn_saved_bytes(int state_dtype, int64_t T, int64_t H);
 size_t ffn_ws_bytes(int state_dtype, int64_t T, int64_t C, int64_t H, bool bwd);

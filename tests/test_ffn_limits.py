@@ -26,3 +26,18 @@ def norm(T, C):
     (1 << 23, 4096, True), ((1 << 23) + 1, 32, False)])
 def test_norm(T, C, fits):
     assert norm(T, C) == ((OK, OK, True) if fits else (X.XHC_EUNSUPPORTED,) * 2 + (False,))
+
+
+def block(T, C, H):
+    d = X.make_dims(T, 1, 1, 1, C)
+    back = X.lib().xhc_ffn_bwd(ctypes.byref(d), H, 0, *A[:9], BIG, None)
+    return X.lib().xhc_ffn(ctypes.byref(d), H, 0, *A[:5], BIG, None), back, X.xhc_ffn_workspace_bytes(d, H, 1) > 0
+
+
+# the rows are brought into fragments by a wave each: T in whole blocks of 16, C in blocks of 64, 8 elements a thread
+@pytest.mark.parametrize("T,C,H,fits", [
+    ((1 << 29) - 32, 32, 16, True), ((1 << 29) - 16, 32, 16, False), ((1 << 29) - 31, 32, 1, False),
+    (1 << 29, 32, 1, False), (1 << 28, 64, 32, True), ((1 << 28) + 1, 64, 32, False),
+    (1 << 14, 1 << 20, 8192, True), (1 << 13, 8192, 1 << 20, True), (1, 32, (1 << 20) + 1, False)])
+def test_block(T, C, H, fits):
+    assert block(T, C, H) == ((OK, OK, True) if fits else (X.XHC_EUNSUPPORTED,) * 2 + (False,))
