@@ -475,7 +475,8 @@ xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* in
  *   c = min(1, max_norm / (norm + 1e-6)); outs[i] may be grads[i] (in place).
  *   Where norm is not finite (an element is not, or the norm is above the
  *   largest float) out_i = grads_i: the caller sees it from norm.  max_norm >= 0.
- *   XHC_EINVAL where an output overlaps another tensor of the call.
+ *   XHC_EINVAL where an output overlaps another tensor of the call, or one of
+ *   them the workspace.
  * Squares and sums are fp64, added in a fixed order.  workspace:
  * xhc_grad_workspace_bytes(n) bytes.                                        */
 size_t xhc_grad_workspace_bytes(int32_t n);

@@ -1129,16 +1129,16 @@ xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* in
   return hip_status(e);
 }
 
-// Whether every output is apart from all else of the call (but its own
-// gradient, in place).  Sorted by start, a range overlaps an earlier one if it
+// Whether every output, and the workspace, is apart from all else of the call
+// (but an output from its own gradient, in place).  Sorted by start, a range overlaps an earlier one if it
 // starts before the furthest end so far.
 static xhc_status check_apart(int n, const void* const* grads, void* const* outs, const int64_t* counts,
-                              const int32_t* dtypes, const float* norm) {
+                              const int32_t* dtypes, const float* norm, const void* workspace) {
   struct Range {
     uintptr_t at, end;
     bool out;
   };
-  Range* r = new (std::nothrow) Range[2 * (size_t)n + 1];
+  Range* r = new (std::nothrow) Range[2 * (size_t)n + 2];
   if (!r) return XHC_EUNSUPPORTED;
   int m = 0;
   for (int i = 0; i < n; ++i) {
@@ -1150,6 +1150,8 @@ static xhc_status check_apart(int n, const void* const* grads, void* const* outs
   }
   const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
   r[m++] = Range{at, at + sizeof(float), true};
+  const uintptr_t ws = reinterpret_cast<uintptr_t>(workspace);
+  r[m++] = Range{ws, ws + grad_ws_bytes(n), true};
   std::sort(r, r + m, [](const Range& a, const Range& b) { return a.at < b.at; });
   uintptr_t all = 0, written = 0;
   bool apart = true;
@@ -1180,7 +1182,7 @@ static xhc_status grad_call(const char* step, int32_t n, const void* const* grad
   if ((reinterpret_cast<uintptr_t>(norm) & 3) || !aligned16(workspace)) return XHC_EUNSUPPORTED;
   if (workspace_bytes < grad_ws_bytes(n)) return XHC_EWORKSPACE;
   if (outs) {
-    const xhc_status st = check_apart(n, grads, outs, counts, dtypes, norm);
+    const xhc_status st = check_apart(n, grads, outs, counts, dtypes, norm, workspace);
     if (st != XHC_OK) return st;
   }
   clear_stale_error();
