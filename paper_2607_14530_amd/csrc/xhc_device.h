@@ -171,12 +171,13 @@ __device__ __forceinline__ void lds_barrier() {
 // does not track the copy (it would otherwise make every later LDS access of
 // the wave wait for it: it cannot tell which LDS a copy writes); the caller
 // waits for it explicitly (s_waitcnt vmcnt) before the data is read, and
-// before the wave ends.
+// before the wave ends.  A copy needs a wait state between the write of m0,
+// its LDS address, and itself (s_nop; inside an asm nobody else puts it there).
 __device__ __forceinline__ void lds_dma16(const void* src, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_addr) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_addr) : "memory", "m0");
 }
 __device__ __forceinline__ void lds_dma4(const void* src, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds_addr) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds_addr) : "memory", "m0");
 }
 
 __device__ __forceinline__ float sigmoidf(float z) { return 1.0f / (1.0f + __expf(-z)); }

@@ -57,8 +57,8 @@ __device__ __forceinline__ i32x4 make_srd(uint64_t a, int64_t bytes) {
 // lds_addr and soff are the same in every lane.  soff stays within a row of
 // fragments, and the descriptor holds whole rows, at least one: soff is below
 // its length, and does not reach past its end where voff does not.  Inline
-// assembly, waited for by the caller, as lds_dma16 (the s_nop is the wait state
-// that a copy needs after a write of m0).
+// assembly, waited for by the caller, as lds_dma16 (the wait state after the
+// write of m0 too).
 template <int AT>
 __device__ __forceinline__ void buf_dma16(const i32x4& srd, uint32_t voff, uint32_t soff, uint32_t lds_addr) {
   asm volatile("s_add_u32 m0, %1, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
