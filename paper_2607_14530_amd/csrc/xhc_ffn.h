@@ -58,7 +58,11 @@ __device__ __forceinline__ i32x4 make_srd(uint64_t a, int64_t bytes) {
 // fragments, and the descriptor holds whole rows, at least one: soff is below
 // its length, and does not reach past its end where voff does not.  Inline
 // assembly, waited for by the caller, as lds_dma16 (the wait state after the
-// write of m0 too).
+// write of m0 too).  The five wait states between a vector write of a scalar
+// register (make_srd's readfirstlane) and its read here are in the code around
+// it, which a test checks in the built library (within the statement, or where
+// a descriptor is made, they cost: T = 8192, C = 4096, H = 11008 forward 1748
+// us, 1780 with either).
 template <int AT>
 __device__ __forceinline__ void buf_dma16(const i32x4& srd, uint32_t voff, uint32_t soff, uint32_t lds_addr) {
   asm volatile("s_add_u32 m0, %1, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
