@@ -407,9 +407,10 @@ xhc_status xhc_stream_sum_bwd(const xhc_dims* d, const void* dout, void* dX, int
 /* ------------------------------------------------------------ the sublayer's own function
  * What runs between xhc_pre and xhc_post of an MLP-type sublayer: the norm of
  * its input and a gated feed-forward block, forward and backward.  Only T, C,
- * state_dtype and (norm) eps of d are used.  Tensor pointers are 16-byte
- * aligned; an output may not be one of the other tensors of its call.  Rows
- * are independent of one another, whatever they hold.
+ * state_dtype and (norm) eps of d are used; its other fields have to be valid
+ * all the same (those of the sublayer's own xhc_dims are).  Tensor pointers are
+ * 16-byte aligned; an output may not overlap another tensor of its call or the
+ * workspace.  Rows are independent of one another, whatever they hold.
  *
  * xhc_rmsnorm: y [T,C] = x r gain with r_t = 1 / sqrt(mean_c x[t,c]^2 + eps),
  *   rounded once (sums are fp32: a row whose squares pass the largest float

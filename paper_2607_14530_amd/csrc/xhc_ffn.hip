@@ -509,12 +509,13 @@ __global__ __launch_bounds__(256) void k_ffn_rows_join(const Epi e, const float*
   e.template finish<8>(at, v, w, pre);
 }
 
-// Few tokens (up to 16 MB): bound by the weights' bytes, which go from memory
-// straight to registers, a fragment (1 KiB) a load.  A workgroup takes FR
-// blocks of 16 n, its waves a part of k each, and keeps about 128 KiB of
-// weights in flight: two sets of U k blocks per wave, one under way while the
-// other is multiplied.  The waves' sums are added through LDS in order.  Tokens
-// past the last read it again.
+// Few tokens (up to 16 for each of MB blocks): bound by the weights' bytes, which
+// go from memory straight to registers, a fragment (1 KiB) a load.  A workgroup
+// takes FR blocks of 16 n, its waves a part of k each, and keeps two sets of U k
+// blocks per wave in flight, one under way while the other is multiplied: 128
+// KiB of weights up to 16 tokens (64 with three-part activations), 32 to 128
+// beyond, where the activations take registers.  The waves' sums are added
+// through LDS in order.  Tokens past the last read it again.
 struct FewArgs {
   const uint4* w;      // packed
   int64_t wkb;         // its k blocks
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(64 * NW) void k_ffn_few(const FewArgs a, const Epi 
     for (int m = 0; m < MB; ++m) acc[f][m] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int k0 = (int)((int64_t)a.kb * wave / NW), k1 = (int)((int64_t)a.kb * (wave + 1) / NW);
   uint4 wr[2][U][FR], xr[2][U][MB][P];
-  // past the part's end the last block again, with zero weights
+  // past the part's end the last block again, whose products are left out
   auto load = [&](int b, int k) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {

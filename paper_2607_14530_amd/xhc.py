@@ -741,8 +741,10 @@ def _state_dtype(d):
 
 
 class RMSNorm:
-    """RMS norm of [T, C] rows with a gain (fp32 [C]); eps is d.eps.  Outputs
-    go to a buffer of this object, overwritten by its next forward."""
+    """RMS norm of [T, C] rows with a gain (fp32 [C]); eps is d.eps.  The gain
+    is read at every call: where it is contiguous on the device already it is
+    not copied, and new values written to it count.  Outputs go to a buffer of
+    this object, overwritten by its next forward."""
 
     def __init__(self, d: Dims, gain, device="cuda"):
         self.d, self.device = d, _here(device)
