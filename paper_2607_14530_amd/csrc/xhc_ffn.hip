@@ -448,7 +448,7 @@ __global__ __launch_bounds__(64 * S::NW) void k_ffn_rows(const GemmArgs a, const
     for (int q = 0; q < AHEAD - 1; ++q) fetch(q);
     // unrolled by hand: with EpiGate<float> it is more than the compiler unrolls, and
     // sums indexed in a loop lie in scratch memory (T = 2048, C = 2560, H = 6912 dh
-    // 3990 us)
+    // 3990 us, 268 so)
     unroll<ALL>([&](auto qc) {
       constexpr int q = qc.value, j = q / NB, i = q % NB;
       if constexpr (q + AHEAD - 1 < ALL) fetch(q + AHEAD - 1);
