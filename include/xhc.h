@@ -464,6 +464,124 @@ xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* in
                        const void* saved, const void* dF, void* d_input, void* dW_gate, void* dW_up, void* dW_down,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------ an attention-type sublayer's own function
+ * What runs between xhc_pre and xhc_post of an attention-type sublayer, behind
+ * its projection to queries, keys and values: the position rotation, attention
+ * with its backward, and for serving a paged cache that holds keys and values
+ * in 4 bits.  qkv [T, Hq + 2 Hkv, D] has a token's query heads, then its key
+ * heads, then its value heads; query head h goes with key and value head
+ * h / (Hq / Hkv).  T, S and state_dtype of d are used; its other fields have to
+ * be valid all the same.  Tensors are of the state dtype and 16-byte aligned;
+ * an output may not overlap another tensor of its call, its workspace or its
+ * pool, unless it says so.  Constraints of xhc_heads (XHC_EINVAL where one is
+ * out of range, XHC_EUNSUPPORTED where this library does not take it):
+ *   Hkv >= 1, Hq a multiple of it, Hq + 2 Hkv <= 1024;  D 32, 64, 96 or 128;
+ *   R from 0 to D, a multiple of 16;  pairs an xhc_pairs;  window >= 0;
+ *   scale > 0 and cap >= 0, finite.  T <= 2^23, T (Hq + 2 Hkv) <= 2^29.          */
+typedef enum { XHC_PAIRS_HALVES = 0, XHC_PAIRS_NEIGHBOURS = 1 } xhc_pairs;
+typedef struct xhc_heads {
+  int32_t Hq;             /* query heads                                         */
+  int32_t Hkv;            /* key and value heads                                 */
+  int32_t D;              /* width of a head                                     */
+  int32_t R;              /* channels of a head that are rotated, its first ones */
+  int32_t pairs;          /* xhc_pairs: channels (i, i + R / 2) or (2 i, 2 i + 1) */
+  int32_t window;         /* a token sees its last `window` positions; 0: all    */
+  float scale;            /* of the products q k, D^-1/2 as a rule               */
+  float cap;              /* scores are cap tanh(scale q k / cap); 0: scale q k  */
+} xhc_heads;
+
+/* xhc_rotate - pair i of each query and key head at position p becomes
+ *   (a c - b s, b c + a s), (c, s) = table[p, i];  inverse = 1: s taken as -s,
+ * which is the reverse of a gradient.
+ *   in, out [T, Hq + 2 Hkv, D]: out may be in itself, whose values and
+ *           unrotated channels are then not touched (elsewhere they are copied)
+ *   pos     [T] int32 or NULL (t % S); a token whose position is not in
+ *           0 .. positions - 1 keeps its values (without pos, S <= positions)
+ *   table   [positions, R/2, 2] fp32, cosine and sine; NULL where R = 0
+ * fp32 arithmetic, each product and sum rounded, and the result once more.    */
+xhc_status xhc_rotate(const xhc_dims* d, const xhc_heads* h, const void* in, const int32_t* pos, const float* table,
+                      int64_t positions, int32_t inverse, void* out, void* stream);
+
+/* xhc_attn_spans - the keys that each token sees, span [T,2] int32 (8-byte
+ * aligned): the first, and one behind the last.  With starts [n + 1] int32
+ * (ascending) document i has the tokens starts[i] .. starts[i + 1] - 1, and
+ * attention stays within it; tokens of none see nothing.  prefix [n] int32 or
+ * NULL: the first prefix[i] tokens of document i are seen by all of it (cut at
+ * its end).  Without starts (NULL, n = 0, prefix NULL) a document is a sequence
+ * of S tokens.  Otherwise token t sees up to t, of the last h->window positions
+ * where that is not 0.                                                        */
+xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, const int32_t* starts,
+                          const int32_t* prefix, int32_t* span, void* stream);
+
+/* xhc_attn - out [T, Hq, D] = sum_j p_ij v_j, p_i the softmax over the keys that
+ * token i sees of  cap tanh(scale q_i k_j / cap) - slopes[h] |i - j|.
+ *   span    [T,2] int32 as above, or any (cut to 0 .. T), or NULL: causal within
+ *           sequences of S tokens, with h->window
+ *   slopes  [Hq] fp32 or NULL
+ *   lse     [T,Hq] fp32 or NULL: base-2 logarithm of the sum of exp, as
+ *           xhc_attn_bwd needs it
+ * A token that sees nothing gets zeros, and an lse of -infinity.  Tokens that
+ * are not seen do not matter, whatever they hold; where a token that is seen
+ * holds infinities or NaN, all of a row that sees it may become NaN.
+ * xhc_attn_bwd - dqkv [T, Hq + 2 Hkv, D] from qkv, span, slopes as in the
+ *   forward, its out and lse, and dout [T,Hq,D]; slopes get no gradient.
+ *   workspace: xhc_attn_workspace_bytes(d, h) bytes.
+ * Sums and softmax are fp32, in an order that the sizes fix.  bf16 state:
+ * probabilities and the gradients of scores are rounded to bf16 as operands of
+ * the next product; fp32 state: products are those of fp32 values in full.     */
+size_t xhc_attn_workspace_bytes(const xhc_dims* d, const xhc_heads* h);
+xhc_status xhc_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span, const float* slopes,
+                    void* out, float* lse, void* stream);
+xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
+                        const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Paged cache of a layer: a pool of npages pages of `page` tokens, of which
+ * each of B sequences holds some.  A sequence's row of the page table names the
+ * pages of its positions, page by page; an entry outside 0 .. npages - 1 is a
+ * page that is not there: its tokens are neither stored nor seen.  A call is
+ * about the T newest tokens: sequence b has tokens starts[b] .. starts[b+1] - 1
+ * of it (none or more), the last of lens[b] tokens in all, so that token t has
+ * position lens[b] - (starts[b+1] - t).  Tokens of no sequence are left alone,
+ * as are those whose position is not in 0 .. per_seq page - 1.  A page that
+ * several sequences hold must not be appended to.
+ *   starts [B + 1], lens [B], pages [B, per_seq] int32, device
+ *   pool    xhc_cache_bytes(h, c) bytes, 256-byte aligned
+ * Keys and values are held as 4-bit floats (sign, 2 exponent, 1 fraction bits:
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6; nearest, ties to even) times a bf16 scale for 32
+ * consecutive channels of a head and token, their largest magnitude / 6 (zeros
+ * where that is below 2^-100, NaN where it is not finite): D / 2 + D / 16 bytes.
+ *
+ * xhc_cache_append - q [T,Hq,D] (or NULL) = the rotated query heads of qkv; the
+ *   rotated key heads and the value heads go into the pool.  table as for
+ *   xhc_rotate, positions >= per_seq page.
+ * xhc_cache_read - k, v [T,Hkv,D]: the values held for the call's tokens, in
+ *   the state dtype (one rounding).  Tokens that are not stored are left alone.
+ * xhc_attn_cache - out [T,Hq,D] from q [T,Hq,D]: token t sees what the cache
+ *   holds of its sequence up to its own position (of h->window positions), with
+ *   scores as in xhc_attn; zeros where it sees nothing.  The call's tokens
+ *   have to be appended before.  Lengths are read on the device: a captured call
+ *   follows them.  workspace: xhc_attn_cache_workspace_bytes(d, h, c) bytes.
+ * page: a multiple of 32 up to 1024;  B from 1 to 65536;  per_seq >= 1 and
+ * per_seq page <= 2^24;  npages >= 1.                                          */
+typedef struct xhc_cache {
+  int32_t page;           /* tokens of a page                                    */
+  int32_t npages;         /* pages of the pool                                   */
+  int32_t B;              /* sequences                                           */
+  int32_t per_seq;        /* entries of a sequence's row of the page table       */
+} xhc_cache;
+size_t xhc_cache_bytes(const xhc_heads* h, const xhc_cache* c);
+size_t xhc_attn_cache_workspace_bytes(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c);
+xhc_status xhc_cache_append(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* qkv,
+                            const float* table, int64_t positions, const int32_t* starts, const int32_t* lens,
+                            const int32_t* pages, void* pool, void* q, void* stream);
+xhc_status xhc_cache_read(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const int32_t* starts,
+                          const int32_t* lens, const int32_t* pages, const void* pool, void* k, void* v,
+                          void* stream);
+xhc_status xhc_attn_cache(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* q,
+                          const float* slopes, const int32_t* starts, const int32_t* lens, const int32_t* pages,
+                          const void* pool, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------ gradient norm and clip
  * Over n tensors (0 <= n <= 4096) of any sizes: grads, counts, dtypes (and
  * outs) are HOST arrays, read before the call returns: device pointer, number

@@ -2,9 +2,11 @@
 // Every check happens before the first launch, so an error return leaves
 // all outputs untouched.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <stdio.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 
@@ -1126,6 +1128,222 @@ xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* in
   hipError_t e = hipSuccess;
   XHC_STEP("ffn_bwd", launch_ffn_bwd(d->state_dtype, d->T, d->C, H, act, input, packed, saved, dF, d_input, dW_gate,
                                      dW_up, dW_down, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+// ---- an attention-type sublayer's own function
+
+static xhc_status check_heads(const xhc_dims* d, const xhc_heads* h) {
+  xhc_status st = check_dims(d);
+  if (st != XHC_OK) return st;
+  if (!h || h->Hkv < 1 || h->Hq < 1 || h->Hq % h->Hkv != 0 || h->D < 1 || h->R < 0 || h->R > h->D || h->window < 0)
+    return XHC_EINVAL;
+  if (h->pairs != XHC_PAIRS_HALVES && h->pairs != XHC_PAIRS_NEIGHBOURS) return XHC_EINVAL;
+  if (!(h->scale > 0.f && h->scale <= FLT_MAX && h->cap >= 0.f && h->cap <= FLT_MAX)) return XHC_EINVAL;
+  if (h->D % 32 != 0 || h->D > 128 || h->R % 16 != 0) return XHC_EUNSUPPORTED;
+  if (h->Hkv > kMaxHeads || h->Hq > kMaxHeads - 2 * h->Hkv) return XHC_EUNSUPPORTED;
+  if (d->T > kMaxAttnT || d->T * (h->Hq + 2 * h->Hkv) > kMaxAttnHeads) return XHC_EUNSUPPORTED;
+  return XHC_OK;
+}
+
+// bytes of `heads` heads of every token
+static size_t heads_bytes(const xhc_dims* d, const xhc_heads* h, int heads) {
+  return (size_t)d->T * heads * h->D * (d->state_dtype == XHC_BF16 ? 2 : 4);
+}
+
+namespace {
+struct Buffer {
+  const void* p;
+  size_t bytes;
+  bool out;
+};
+}  // namespace
+
+// whether no output overlaps another of a call's buffers
+static bool buffers_apart(std::initializer_list<Buffer> all) {
+  for (const Buffer* a = all.begin(); a != all.end(); ++a)
+    for (const Buffer* b = all.begin(); b != a; ++b) {
+      if (!(a->out || b->out) || !a->p || !b->p) continue;
+      const uintptr_t x = reinterpret_cast<uintptr_t>(a->p), y = reinterpret_cast<uintptr_t>(b->p);
+      if (x < y + b->bytes && y < x + a->bytes) return false;
+    }
+  return true;
+}
+
+static bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+xhc_status xhc_rotate(const xhc_dims* d, const xhc_heads* h, const void* in, const int32_t* pos, const float* table,
+                      int64_t positions, int32_t inverse, void* out, void* stream) {
+  xhc_status st = check_heads(d, h);
+  if (st != XHC_OK) return st;
+  if (positions < 0 || (inverse != 0 && inverse != 1)) return XHC_EINVAL;
+  if (d->T == 0) return XHC_OK;
+  if (!in || !out || (h->R > 0 && (!table || (!pos && d->S > positions)))) return XHC_EINVAL;
+  if (!aligned16(in) || !aligned16(out) || !aligned16(table) || !aligned(pos, 4)) return XHC_EUNSUPPORTED;
+  if (h->R > 0 && positions > (INT64_MAX >> 3) / h->R) return XHC_EUNSUPPORTED;
+  const size_t bytes = heads_bytes(d, h, h->Hq + 2 * h->Hkv);
+  if (!buffers_apart({{in == out ? nullptr : in, bytes, false}, {out, bytes, true}, {pos, (size_t)d->T * 4, false},
+                      {table, (size_t)positions * h->R * 4, false}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("rotate", launch_rotate(d, h, in, pos, table, positions, inverse != 0, out,
+                                   reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, const int32_t* starts,
+                          const int32_t* prefix, int32_t* span, void* stream) {
+  xhc_status st = check_heads(d, h);
+  if (st != XHC_OK) return st;
+  if (n < 0 || (!starts && (n != 0 || prefix))) return XHC_EINVAL;
+  if (d->T == 0) return XHC_OK;
+  if (!span) return XHC_EINVAL;
+  if (!aligned(starts, 4) || !aligned(prefix, 4) || !aligned(span, 8)) return XHC_EUNSUPPORTED;
+  if (!buffers_apart({{starts, ((size_t)n + 1) * 4, false}, {prefix, (size_t)n * 4, false},
+                      {span, (size_t)d->T * 8, true}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("attn_spans", launch_attn_spans(d->T, d->S, h->window, n, starts, prefix, span,
+                                           reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span, const float* slopes,
+                    void* out, float* lse, void* stream) {
+  xhc_status st = check_heads(d, h);
+  if (st != XHC_OK) return st;
+  if (d->T == 0) return XHC_OK;
+  if (!qkv || !out) return XHC_EINVAL;
+  if (!aligned16(qkv) || !aligned16(out) || !aligned(span, 8) || !aligned(slopes, 4) || !aligned(lse, 4))
+    return XHC_EUNSUPPORTED;
+  if (!buffers_apart({{qkv, heads_bytes(d, h, h->Hq + 2 * h->Hkv), false}, {span, (size_t)d->T * 8, false},
+                      {slopes, (size_t)h->Hq * 4, false}, {out, heads_bytes(d, h, h->Hq), true},
+                      {lse, (size_t)d->T * h->Hq * 4, true}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("attn", launch_attn(d, h, qkv, span, slopes, out, lse, reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+size_t xhc_attn_workspace_bytes(const xhc_dims* d, const xhc_heads* h) {
+  return check_heads(d, h) == XHC_OK ? attn_bwd_ws_bytes(d->T, h->Hq, h->Hkv, h->D) : 0;
+}
+
+xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
+                        const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  xhc_status st = check_heads(d, h);
+  if (st != XHC_OK) return st;
+  if (d->T == 0) return XHC_OK;
+  if (!qkv || !out || !lse || !dout || !dqkv || !workspace) return XHC_EINVAL;
+  for (const void* p : {qkv, out, dout, (const void*)dqkv, (const void*)workspace})
+    if (!aligned16(p)) return XHC_EUNSUPPORTED;
+  if (!aligned(span, 8) || !aligned(slopes, 4) || !aligned(lse, 4)) return XHC_EUNSUPPORTED;
+  const size_t need = attn_bwd_ws_bytes(d->T, h->Hq, h->Hkv, h->D);
+  if (workspace_bytes < need) return XHC_EWORKSPACE;
+  const size_t all = heads_bytes(d, h, h->Hq + 2 * h->Hkv), rows = heads_bytes(d, h, h->Hq);
+  if (!buffers_apart({{qkv, all, false}, {span, (size_t)d->T * 8, false}, {slopes, (size_t)h->Hq * 4, false},
+                      {out, rows, false}, {lse, (size_t)d->T * h->Hq * 4, false}, {dout, rows, false},
+                      {dqkv, all, true}, {workspace, need, true}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("attn_bwd", launch_attn_bwd(d, h, qkv, span, slopes, out, lse, dout, dqkv, workspace,
+                                       reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+static xhc_status check_cache(const xhc_cache* c) {
+  if (!c || c->page < 1 || c->npages < 1 || c->B < 1 || c->per_seq < 1) return XHC_EINVAL;
+  if (c->page % 32 != 0 || c->page > 1024 || c->B > kMaxSequences || (int64_t)c->per_seq * c->page > kMaxCached)
+    return XHC_EUNSUPPORTED;
+  return XHC_OK;
+}
+
+static xhc_status check_cache_call(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c) {
+  const xhc_status st = check_heads(d, h);
+  return st != XHC_OK ? st : check_cache(c);
+}
+
+size_t xhc_cache_bytes(const xhc_heads* h, const xhc_cache* c) {
+  xhc_dims d = {};
+  d.S = d.N = d.k = d.Kr = 1, d.C = 32, d.eps = 1.f;
+  return check_cache_call(&d, h, c) == XHC_OK ? cache_bytes(h, c) : 0;
+}
+
+size_t xhc_attn_cache_workspace_bytes(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c) {
+  return check_cache_call(d, h, c) == XHC_OK ? cache_attend_ws_bytes(d, h, c) : 0;
+}
+
+xhc_status xhc_cache_append(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* qkv,
+                            const float* table, int64_t positions, const int32_t* starts, const int32_t* lens,
+                            const int32_t* pages, void* pool, void* q, void* stream) {
+  xhc_status st = check_cache_call(d, h, c);
+  if (st != XHC_OK) return st;
+  if (h->R > 0 && positions < (int64_t)c->per_seq * c->page) return XHC_EINVAL;
+  if (d->T == 0) return XHC_OK;
+  if (!qkv || (h->R > 0 && !table) || !starts || !lens || !pages || !pool) return XHC_EINVAL;
+  if (!aligned16(qkv) || !aligned16(table) || !aligned16(q) || !aligned(pool, 256) || !aligned(starts, 4) ||
+      !aligned(lens, 4) || !aligned(pages, 4) || (h->R > 0 && positions > (INT64_MAX >> 3) / h->R))
+    return XHC_EUNSUPPORTED;
+  if (!buffers_apart({{qkv, heads_bytes(d, h, h->Hq + 2 * h->Hkv), false},
+                      {table, h->R > 0 ? (size_t)positions * h->R * 4 : 0, false},
+                      {starts, ((size_t)c->B + 1) * 4, false}, {lens, (size_t)c->B * 4, false},
+                      {pages, (size_t)c->B * c->per_seq * 4, false}, {pool, cache_bytes(h, c), true},
+                      {q, heads_bytes(d, h, h->Hq), true}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("cache_append", launch_cache_append(d, h, c, qkv, table, starts, lens, pages, pool, q,
+                                               reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_cache_read(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const int32_t* starts,
+                          const int32_t* lens, const int32_t* pages, const void* pool, void* k, void* v,
+                          void* stream) {
+  xhc_status st = check_cache_call(d, h, c);
+  if (st != XHC_OK) return st;
+  if (d->T == 0) return XHC_OK;
+  if (!starts || !lens || !pages || !pool || !k || !v) return XHC_EINVAL;
+  if (!aligned16(k) || !aligned16(v) || !aligned(pool, 256) || !aligned(starts, 4) || !aligned(lens, 4) ||
+      !aligned(pages, 4))
+    return XHC_EUNSUPPORTED;
+  const size_t bytes = heads_bytes(d, h, h->Hkv);
+  if (!buffers_apart({{starts, ((size_t)c->B + 1) * 4, false}, {lens, (size_t)c->B * 4, false},
+                      {pages, (size_t)c->B * c->per_seq * 4, false}, {pool, cache_bytes(h, c), false},
+                      {k, bytes, true}, {v, bytes, true}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("cache_read", launch_cache_read(d, h, c, starts, lens, pages, pool, k, v,
+                                           reinterpret_cast<hipStream_t>(stream)));
+  return hip_status(e);
+}
+
+xhc_status xhc_attn_cache(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* q,
+                          const float* slopes, const int32_t* starts, const int32_t* lens, const int32_t* pages,
+                          const void* pool, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  xhc_status st = check_cache_call(d, h, c);
+  if (st != XHC_OK) return st;
+  if (d->T == 0) return XHC_OK;
+  if (!q || !starts || !lens || !pages || !pool || !out || !workspace) return XHC_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned(pool, 256) || !aligned(slopes, 4) ||
+      !aligned(starts, 4) || !aligned(lens, 4) || !aligned(pages, 4))
+    return XHC_EUNSUPPORTED;
+  const size_t need = cache_attend_ws_bytes(d, h, c), rows = heads_bytes(d, h, h->Hq);
+  if (workspace_bytes < need) return XHC_EWORKSPACE;
+  if (!buffers_apart({{q, rows, false}, {slopes, (size_t)h->Hq * 4, false}, {starts, ((size_t)c->B + 1) * 4, false},
+                      {lens, (size_t)c->B * 4, false}, {pages, (size_t)c->B * c->per_seq * 4, false},
+                      {pool, cache_bytes(h, c), false}, {out, rows, true}, {workspace, need, true}}))
+    return XHC_EINVAL;
+  clear_stale_error();
+  hipError_t e = hipSuccess;
+  XHC_STEP("attn_cache", launch_cache_attend(d, h, c, q, slopes, starts, lens, pages, pool, out, workspace,
+                                             reinterpret_cast<hipStream_t>(stream)));
   return hip_status(e);
 }
 

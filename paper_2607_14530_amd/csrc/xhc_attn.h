@@ -1,0 +1,301 @@
+// Building blocks of the attention kernels (gfx950).
+//
+// Every product is one of 32x32 blocks on matrix instructions with fp32 sums.
+// A wave owns 32 columns (queries forward and for dq, keys for dk and dv), a
+// lane one of them, l % 32; the other side comes from LDS tiles of 64 rows that
+// the workgroup's waves share.  The order of an instruction's inner index is
+// free as long as both operands agree on it, and that is used throughout:
+//
+//   row_frag   eight consecutive channels of one row: the operand whose rows the
+//              block's rows are, of the products over channels
+//   col_frag   eight rows of one channel, in the order in which a lane holds the
+//              sums of such a product (rows 16 s + 8 (j / 4) + 4 (l / 32) + j % 4),
+//              so that those, rounded, are the other operand as they lie: the
+//              probabilities never leave their lane's registers
+//
+// fp32 tensors use the 32x32x2 instruction eight times on the same eight
+// elements, which takes their products in full at a sixteenth of the rate.
+#pragma once
+
+#include "xhc_ffn.h"
+
+namespace xhc {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kTile = 64;                     // rows of an LDS tile
+constexpr int kAttnWaves = 4;
+
+struct Frag32 {
+  float v[8];
+};
+template <typename TS> struct FragOf;
+template <> struct FragOf<uint16_t> { using type = uint4; };
+template <> struct FragOf<float> { using type = Frag32; };
+template <typename TS> using Frag = typename FragOf<TS>::type;
+
+__device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 c) { return mfma_32x32x16(a, b, c); }
+__device__ __forceinline__ f32x16 mfma32(const Frag32& a, const Frag32& b, f32x16 c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+  return c;
+}
+
+// sums 8 s .. 8 s + 7 of a block, as the operand that col_frag goes with
+__device__ __forceinline__ void sums_frag(const f32x16& x, int s, uint4& f) {
+  f = make_uint4(pack2bf(x[8 * s], x[8 * s + 1]), pack2bf(x[8 * s + 2], x[8 * s + 3]),
+                 pack2bf(x[8 * s + 4], x[8 * s + 5]), pack2bf(x[8 * s + 6], x[8 * s + 7]));
+}
+__device__ __forceinline__ void sums_frag(const f32x16& x, int s, Frag32& f) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.v[j] = x[8 * s + j];
+}
+
+__device__ __forceinline__ void load_frag(const uint16_t* p, uint4& f) { f = *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void load_frag(const float* p, Frag32& f) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  f = Frag32{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+
+// whether one of a 16-byte piece's elements is an infinity or NaN
+template <typename TS> __device__ __forceinline__ bool not_finite(const uint4& w);
+template <> __device__ __forceinline__ bool not_finite<uint16_t>(const uint4& w) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    bad |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
+  }
+  return bad;
+}
+template <> __device__ __forceinline__ bool not_finite<float>(const uint4& w) {
+  constexpr uint32_t e = 0x7f800000u;
+  return (w.x & e) == e || (w.y & e) == e || (w.z & e) == e || (w.w & e) == e;
+}
+
+// A tile of kTile rows of D elements in LDS, in 16-byte pieces.  Piece c of row
+// r lies at place c ^ turn(r), so that eight rows' pieces of one number, which
+// row_frag reads at a time, and four rows' pairs of pieces, which the transposing
+// read takes, meet different banks.  The copy leaves a run of 1 KiB where it
+// puts it, so the pieces are turned on the way: each lane reads the piece that
+// belongs to its place.
+template <typename TS, int D>
+struct Tile {
+  static constexpr int kPieces = D * (int)sizeof(TS) / 16, kRowBytes = kPieces * 16, kBytes = kTile * kRowBytes;
+  static constexpr int kCopies = kTile * kPieces / 64 / kAttnWaves;
+  static constexpr bool kEight = kPieces % 8 == 0;
+  static_assert(kTile * kPieces % (64 * kAttnWaves) == 0, "whole copies for every wave");
+  static __device__ __forceinline__ int turn(int r) {
+    return kEight ? 2 * (r % 4) + r / 4 % 2 : 2 * (r / 2 % 2) + r / 4 % 2;
+  }
+  // rows row0 .. of a tensor whose rows lie `stride` bytes apart, those behind
+  // `last` as copies of it (what becomes of them is masked)
+  static __device__ __forceinline__ void copy(const unsigned char* base, uint32_t stride, int row0, int last,
+                                              uint32_t to, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int at = (wave * kCopies + i) * 64 + lane, r = at / kPieces, c = (at % kPieces) ^ turn(r);
+      const int t = row0 + r < last ? row0 + r : last;
+      lds_dma16(base + ((uint64_t)(uint32_t)t * stride + c * 16), to + (wave * kCopies + i) * 1024);
+    }
+  }
+  static __device__ __forceinline__ uint4& piece(unsigned char* s, int r, int c) {
+    return *reinterpret_cast<uint4*>(s + r * kRowBytes + (c ^ turn(r)) * 16);
+  }
+  // channels 16 ks + 8 (lane / 32) .. of row 32 rb + lane % 32
+  static __device__ __forceinline__ void row_frag(const unsigned char* s, int rb, int ks, int lane, uint4& f) {
+    const int r = lane % 32;
+    f = *reinterpret_cast<const uint4*>(s + (rb * 32 + r) * kRowBytes + ((2 * ks + lane / 32) ^ turn(r)) * 16);
+  }
+  static __device__ __forceinline__ void row_frag(const unsigned char* s, int rb, int ks, int lane, Frag32& f) {
+    const int r = lane % 32, c = 4 * ks + 2 * (lane / 32);
+    const unsigned char* p = s + (rb * 32 + r) * kRowBytes;
+    const float4 a = *reinterpret_cast<const float4*>(p + (c ^ turn(r)) * 16);
+    const float4 b = *reinterpret_cast<const float4*>(p + ((c + 1) ^ turn(r)) * 16);
+    f = Frag32{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+  }
+  // rows 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4 of channel 32 f + lane % 32, j = 0 .. 7
+  static __device__ __forceinline__ void col_frag(const unsigned char* s, int f, int st, int lane, uint4& out) {
+    const int r = 4 * (lane / 32) + lane % 16 / 4, q = lane % 4;   // of this lane's read: a row, four channels
+    const int c = 4 * f + 2 * (lane / 16 % 2) + q / 2;
+    const unsigned char* p = s + (16 * st + r) * kRowBytes + (c ^ turn(r)) * 16 + q % 2 * 8;
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRowBytes));
+    const uint2 ua = __builtin_bit_cast(uint2, a), ub = __builtin_bit_cast(uint2, b);
+    out = make_uint4(ua.x, ua.y, ub.x, ub.y);
+  }
+  static __device__ __forceinline__ void col_frag(const unsigned char* s, int f, int st, int lane, Frag32& out) {
+    const int c = 8 * f + lane % 32 / 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = 8 * (j / 4) + 4 * (lane / 32) + j % 4;
+      out.v[j] = *reinterpret_cast<const float*>(s + (16 * st + r) * kRowBytes + (c ^ turn(r)) * 16 + lane % 4 * 4);
+    }
+  }
+  // Rows that hold an infinity or NaN become zeros; they are the result's bits.
+  // A product over rows adds 0 times what lies in a row that its column does not
+  // see, which has to be finite: so tiles that a mask cuts are looked over, and
+  // for the columns that do see such a row the caller puts a NaN in the row's
+  // place.  Called by all waves between barriers of its own.
+  static __device__ __forceinline__ uint64_t clean(unsigned char* s, uint16_t* bits, int wave, int lane) {
+    const int r = wave * 16 + lane / 4;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPieces / 4; ++i) bad |= not_finite<TS>(piece(s, r, lane % 4 + 4 * i));
+    const uint64_t all = __ballot(bad);
+    uint32_t rows = 0;
+    if (all) {
+      const bool mine = (all >> (lane / 4 * 4)) & 15;
+      rows = 0;
+      for (int i = 0; i < 16; ++i) rows |= (uint32_t)(((all >> (4 * i)) & 15) != 0) << i;
+      if (mine) {
+#pragma unroll
+        for (int i = 0; i < kPieces / 4; ++i) piece(s, r, lane % 4 + 4 * i) = make_uint4(0, 0, 0, 0);
+      }
+    }
+    if (lane == 0) bits[wave] = (uint16_t)rows;
+    lds_barrier();
+    return *reinterpret_cast<const uint64_t*>(bits);
+  }
+};
+
+// What an attention call is about, as its kernels take it.
+struct AttnArgs {
+  const void* qkv;          // [T][Hq + 2 Hkv][D]
+  const int2* span;         // [T]: the first key that a token sees, and one behind the last; null: causal
+  const float* slopes;      // [Hq] or null
+  void* out;                // [T][Hq][D]
+  float* lse;               // [T][Hq] or null: base-2 logarithms of the rows' sums
+  const void* dout;
+  void* dqkv;
+  const float* lsep;        // [Hq][Tp]: of a backward
+  const float* delta;       // [Hq][Tp]
+  const int* lo;            // [Tp], [Tp]: spans, cut to 0 .. T, 0 .. 0 for rows behind the last
+  const int* hi;
+  const int4* range;        // [Tp / kTile]: of a tile's rows that see keys, min lo, max hi; of all, max lo, min hi
+  float* part;              // dk, dv of parts of a group's heads
+  int64_t T, S, Tp;
+  int Hq, Hkv, window;
+  int parts;                // of a group's query heads, each one workgroup's (dk, dv)
+  float scale, cap;
+};
+
+// keys that token t sees
+__device__ __forceinline__ int2 span_of(const AttnArgs& a, int t) {
+  if (t >= a.T) return make_int2(0, 0);
+  if (a.span) {
+    const int2 s = a.span[t];
+    const int T = (int)a.T;
+    return make_int2(min(max(s.x, 0), T), min(max(s.y, 0), T));
+  }
+  int lo = t - (int)(t % a.S);
+  if (a.window > 0 && t - a.window + 1 > lo) lo = t - a.window + 1;
+  return make_int2(lo, t + 1);
+}
+
+// Scores in units of log2 e (their softmax then takes exp2), in place of the
+// raw products of one block of 32 keys x 32 queries or queries x keys:
+// (cap tanh(scale x / cap) - slope |i - j|) log2 e; der: d score / d (scale x),
+// which is 1 without a cap.
+struct Score {
+  float mul, cap, slope;    // mul: scale log2 e, or 2 log2 e scale / cap
+  __device__ __forceinline__ void init(const AttnArgs& a, int head) {
+    cap = a.cap * kLog2e;
+    mul = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e;
+    slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  }
+};
+template <typename TS> __device__ __forceinline__ float tanh_of(float x);
+// 1 - 2 / (1 + exp 2x): off by some 2^-23 of 1, where a bf16 product's factors are off by 2^-9 of it
+template <> __device__ __forceinline__ float tanh_of<uint16_t>(float x) {
+  return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+}
+template <> __device__ __forceinline__ float tanh_of<float>(float x) { return tanhf(x); }
+
+__device__ __forceinline__ float max_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// the row of sum r of a block, less 4 (lane / 32)
+__host__ __device__ __forceinline__ constexpr int sum_row(int r) { return 8 * (r / 4) + r % 4; }
+
+// The workgroup's extremes of its rows' spans: x min lo, y max hi of the rows
+// that see keys (x >= y where none does), z max lo, w min hi of all.  Rows
+// behind the last are left out.
+__device__ __forceinline__ int4 attn_extremes(int2 s, bool row, int4* red, int wave, int lane) {
+  const bool some = row && s.x < s.y;
+  int4 e = make_int4(some ? s.x : INT32_MAX, some ? s.y : 0, row ? (some ? s.x : INT32_MAX) : 0,
+                     row ? (some ? s.y : 0) : INT32_MAX);
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    e.x = min(e.x, __shfl_xor(e.x, d));
+    e.y = max(e.y, __shfl_xor(e.y, d));
+    e.z = max(e.z, __shfl_xor(e.z, d));
+    e.w = min(e.w, __shfl_xor(e.w, d));
+  }
+  if (lane == 0) red[wave] = e;
+  __syncthreads();
+  e = red[0];
+#pragma unroll
+  for (int w = 1; w < kAttnWaves; ++w) {
+    e.x = min(e.x, red[w].x);
+    e.y = max(e.y, red[w].y);
+    e.z = max(e.z, red[w].z);
+    e.w = min(e.w, red[w].w);
+  }
+  return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y),
+                   __builtin_amdgcn_readfirstlane(e.z), __builtin_amdgcn_readfirstlane(e.w));
+}
+
+// Sums of one 32-channel block of 32 tokens (a lane: token lane % 32, channels
+// 8 i + 4 (lane / 32) + 0 .. 3) times m, to row p of the lane's token: the two
+// halves exchange fours of channels, so that each writes runs of eight.
+template <typename TS>
+__device__ __forceinline__ void store_sums(const f32x16& x, float m, TS* p, bool row, int lane) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[8 * i + e] * m),
+                                                      __float_as_uint(x[8 * i + 4 + e] * m), false, false);
+      f[e] = __uint_as_float(r[0]);
+      f[4 + e] = __uint_as_float(r[1]);
+    }
+    // the lower half now has channels 16 i + 0 .. 7, the upper 16 i + 8 .. 15
+    if (row) Vec8<TS>::store(p + 16 * i + 8 * (lane / 32), f);
+  }
+}
+
+// The rotation: pairs (a, b) -> (a c - b s, b c + a s), products and sums
+// rounded one by one (no fused ones), so that the result is the formula's to
+// the bit in fp32 whatever compiles it.
+template <int N>
+__device__ __forceinline__ void turn(float (&a)[N], float (&b)[N], const float* cs, float sign) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float c = cs[2 * i], s = cs[2 * i + 1] * sign;
+    const float x = a[i] * c - b[i] * s, y = b[i] * c + a[i] * s;
+    a[i] = x;
+    b[i] = y;
+  }
+}
+
+// Workgroup b's head and tile of rows, of `tiles` tiles and `heads` heads: an
+// XCD (b % 8) takes heads of its own where they divide among the eight, so that
+// its L2 keeps their keys and values, and later tiles, which see more, go first.
+__device__ __forceinline__ void attn_place(int heads, int tiles, int& head, int& tile) {
+  const uint32_t b = blockIdx.x;
+  if (heads % 8 == 0) {
+    const uint32_t mine = heads / 8, l = b / 8;
+    head = (int)(b % 8 * mine + l % mine);
+    tile = tiles - 1 - (int)(l / mine);
+  } else {
+    head = (int)(b % heads);
+    tile = tiles - 1 - (int)(b / heads);
+  }
+}
+
+}  // namespace xhc

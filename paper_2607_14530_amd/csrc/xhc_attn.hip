@@ -1,0 +1,295 @@
+// Attention of token rows, its spans and its rotation:
+//
+//   s_ij = cap tanh(scale q_i k_j / cap) - slope |i - j|,  lo_i <= j < hi_i
+//   p_i = softmax_j s_ij,  o_i = sum_j p_ij v_j,  lse_i = log2 sum_j exp s_ij
+//
+// Forward (k_attn): a workgroup takes 128 queries of a head, a wave 32 of them,
+// and goes once over the keys that its rows see, 64 at a time, with the running
+// maximum and sum of each row.
+#include "xhc_attn.h"
+
+namespace xhc {
+
+namespace {
+
+constexpr float kNoKey = -__builtin_huge_valf();
+
+template <typename TS, int D>
+__global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn(AttnArgs a) {
+  using TL = Tile<TS, D>;
+  constexpr int KS = D / 16, F = D / 32;
+  __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
+  __shared__ int4 red[kAttnWaves];
+  __shared__ __align__(8) uint16_t bits[4];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  int head, tile;
+  attn_place(a.Hq, (int)((a.T + 127) / 128), head, tile);
+  const int kvh = head / (a.Hq / a.Hkv), H = a.Hq + 2 * a.Hkv;
+  const int t = tile * 128 + wave * 32 + lane % 32, T1 = (int)a.T - 1;
+  const bool row = t <= T1;
+  const int2 see = span_of(a, t);
+  const int4 ex = attn_extremes(see, row, red, wave, lane);
+  const uint32_t stride = (uint32_t)H * D * sizeof(TS);
+  const unsigned char* base = reinterpret_cast<const unsigned char*>(a.qkv);
+  const unsigned char* kb = base + (size_t)(a.Hq + kvh) * D * sizeof(TS);
+  const unsigned char* vb = kb + (size_t)a.Hkv * D * sizeof(TS);
+  const uint32_t at = lds_offset(lds);
+
+  f32x16 o[F];
+#pragma unroll
+  for (int f = 0; f < F; ++f) o[f] = f32x16{};
+  float m = kNoKey, l = 0.f;
+  const int first = ex.x / kTile, end = (ex.y + kTile - 1) / kTile;
+  if (ex.x < ex.y) {
+    Score sc;
+    sc.init(a, head);
+    Frag<TS> q[KS];
+    const TS* qp = reinterpret_cast<const TS*>(base) + (int64_t)(row ? t : T1) * H * D + head * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) load_frag(qp + 16 * ks + 8 * (lane / 32), q[ks]);
+    TL::copy(kb, stride, first * kTile, T1, at, wave, lane);
+    TL::copy(vb, stride, first * kTile, T1, at + TL::kBytes, wave, lane);
+    for (int kt = first; kt < end; ++kt) {
+      const uint32_t off = (kt - first) % 2 * 2 * TL::kBytes, next = 2 * TL::kBytes - off;
+      wait_vm<0>();
+      lds_barrier();
+      if (kt + 1 < end) {
+        TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, lane);
+        TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, lane);
+      }
+      unsigned char *K = lds + off, *V = K + TL::kBytes;
+      const int j0 = kt * kTile;
+      const bool cut = j0 < ex.z || j0 + kTile > ex.w;      // some row does not see all of the tile
+      uint64_t bad = 0;
+      if (cut) bad = TL::clean(V, bits, wave, lane);
+      f32x16 s[2];
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        s[rb] = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          Frag<TS> k;
+          TL::row_frag(K, rb, ks, lane, k);
+          s[rb] = mfma32(k, q[ks], s[rb]);
+        }
+      }
+      // a lane's keys: j0 + 32 rb + sum_row(r) + 4 (lane / 32)
+      if (a.cap > 0.f) {
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[rb][r] = sc.cap * tanh_of<TS>(s[rb][r] * sc.mul);
+      } else {
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[rb][r] *= sc.mul;
+      }
+      if (a.slopes) {
+        const float d0 = (float)(t - j0 - 4 * (lane / 32));
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[rb][r] = fmaf(-sc.slope, fabsf(d0 - (float)(32 * rb + sum_row(r))), s[rb][r]);
+      }
+      if (cut) {
+        const int lo = see.x - j0 - 4 * (lane / 32), hi = see.y - j0 - 4 * (lane / 32);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * rb + sum_row(r);
+            if (!(j >= lo && j < hi)) s[rb][r] = kNoKey;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[rb][r]);
+      top = max_halves(top);
+      // The row's reference only follows its maximum when that is 2^8 above it:
+      // probabilities up to 256 are as exact, and sums are rarely rescaled.
+      if (__any(top > m + 8.f)) {
+        const float to = top > m + 8.f ? top : m;           // (from -inf: the first maximum)
+        const float c = m == kNoKey ? 0.f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= c;
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[f][r] *= c;
+      }
+      const float ref = m == kNoKey ? 0.f : m;              // a row that has seen nothing: exp2(-inf) = 0
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[rb][r] = __builtin_amdgcn_exp2f(s[rb][r] - ref);
+          l += s[rb][r];
+        }
+      if (bad) {
+        const int lo = see.x - j0, hi = see.y - j0;
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * rb + sum_row(r) + 4 * (lane / 32);
+            if (((bad >> j) & 1) && j >= lo && j < hi) s[rb][r] = __builtin_nanf("");
+          }
+      }
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        Frag<TS> p;
+        sums_frag(s[st / 2], st % 2, p);
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          Frag<TS> v;
+          TL::col_frag(V, f, st, lane, v);
+          o[f] = mfma32(v, p, o[f]);
+        }
+      }
+    }
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const float inv = see.x < see.y ? 1.f / l : 0.f;
+  TS* op = reinterpret_cast<TS*>(a.out) + ((int64_t)t * a.Hq + head) * D;
+#pragma unroll
+  for (int f = 0; f < F; ++f) store_sums<TS>(o[f], inv, op + 32 * f, row, lane);
+  if (a.lse && row && lane < 32)
+    a.lse[(int64_t)t * a.Hq + head] = see.x < see.y ? m + __builtin_amdgcn_logf(l) : kNoKey;
+}
+
+// The spans of documents, by one thread each token.  Document i holds the
+// tokens starts[i] .. starts[i + 1] - 1; its first prefix[i] see one another.
+__global__ __launch_bounds__(256) void k_attn_spans(int64_t T, int64_t S, int window, int n, const int* starts,
+                                                    const int* prefix, int2* span) {
+  const int64_t t64 = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t64 >= T) return;
+  const int t = (int)t64;
+  int from = t - (int)(t % S), hi = t + 1;
+  if (starts) {
+    int a = 0, b = n;                       // the last i in [0, n] with starts[i] <= t, if starts[0] is
+    while (a < b) {
+      const int c = (a + b + 1) / 2;
+      if (starts[c] <= t) a = c; else b = c - 1;
+    }
+    if (starts[0] > t || a == n) {
+      span[t] = make_int2(0, 0);
+      return;
+    }
+    const int64_t s0 = starts[a], s1 = starts[a + 1] < T ? starts[a + 1] : T;
+    from = s0 > 0 ? (int)s0 : 0;
+    if (prefix) {
+      const int64_t p = s0 + prefix[a] < s1 ? s0 + prefix[a] : s1;
+      if (p > hi) hi = (int)p;
+    }
+  }
+  if (window > 0 && t - window + 1 > from) from = t - window + 1;
+  span[t] = make_int2(from, hi);
+}
+
+// A thread takes 16 channels of a head: eight pairs, or sixteen behind the
+// rotated ones; eight or fewer threads a head, the heads of a token (or of
+// several) side by side, so that a workgroup reads runs.  Bound by HBM.
+template <typename TS>
+__global__ __launch_bounds__(256) void k_rotate(int64_t T, int64_t S, int H, int Hrot, int D, int R, int pairs,
+                                                const TS* src, const int* pos, const float* table, int64_t positions,
+                                                float sign, TS* dst, int heads, int tokens) {
+  const int per = D / 16, j = threadIdx.x % per, slot = threadIdx.x / per;
+  const int64_t t = (int64_t)blockIdx.x * tokens + slot / heads;
+  if (slot / heads >= tokens || t >= T) return;
+  const int64_t p = pos ? pos[t] : t % S;
+  const bool turned = 16 * j < R && p >= 0 && p < positions;
+  float cs[16];
+  if (turned) {
+    Vec8<float>::load(table + p * R + 16 * j, *reinterpret_cast<float(*)[8]>(cs));
+    Vec8<float>::load(table + p * R + 16 * j + 8, *reinterpret_cast<float(*)[8]>(cs + 8));
+  }
+  for (int h = slot % heads; h < H; h += heads) {
+    const bool now = turned && h < Hrot;
+    if (!now && src == dst) continue;
+    const int64_t at = (t * H + h) * D;
+    const bool split = now && !pairs;        // halves: channels 8 j .. + 8 with R / 2 + 8 j .. + 8
+    const int xa = split ? 8 * j : 16 * j, xb = split ? 8 * j + R / 2 : 16 * j + 8;
+    float a[8], b[8];
+    Vec8<TS>::load(src + at + xa, a);
+    Vec8<TS>::load(src + at + xb, b);
+    if (split) {
+      turn<8>(a, b, cs, sign);
+    } else if (now) {                        // neighbours: a and b hold four pairs each
+      float x[8], y[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = a[2 * i], y[i] = a[2 * i + 1];
+        x[4 + i] = b[2 * i], y[4 + i] = b[2 * i + 1];
+      }
+      turn<8>(x, y, cs, sign);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[2 * i] = x[i], a[2 * i + 1] = y[i];
+        b[2 * i] = x[4 + i], b[2 * i + 1] = y[4 + i];
+      }
+    }
+    Vec8<TS>::store(dst + at + xa, a);
+    Vec8<TS>::store(dst + at + xb, b);
+  }
+}
+
+template <typename TS, int D> hipError_t run_attn(const AttnArgs& a, hipStream_t s) {
+  const int64_t tiles = (a.T + 127) / 128;
+  k_attn<TS, D><<<dim3((unsigned)(tiles * a.Hq)), dim3(64 * kAttnWaves), 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename TS> hipError_t run_attn_of(int D, const AttnArgs& a, hipStream_t s) {
+  switch (D) {
+    case 32: return run_attn<TS, 32>(a, s);
+    case 64: return run_attn<TS, 64>(a, s);
+    case 96: return run_attn<TS, 96>(a, s);
+    default: return run_attn<TS, 128>(a, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
+                       const float* slopes, void* out, float* lse, hipStream_t s) {
+  AttnArgs a{};
+  a.qkv = qkv;
+  a.span = reinterpret_cast<const int2*>(span);
+  a.slopes = slopes;
+  a.out = out;
+  a.lse = lse;
+  a.T = d->T, a.S = d->S;
+  a.Hq = h->Hq, a.Hkv = h->Hkv, a.window = h->window;
+  a.scale = h->scale, a.cap = h->cap;
+  return d->state_dtype == XHC_BF16 ? run_attn_of<uint16_t>(h->D, a, s) : run_attn_of<float>(h->D, a, s);
+}
+
+hipError_t launch_attn_spans(int64_t T, int64_t S, int window, int n, const int32_t* starts, const int32_t* prefix,
+                             int32_t* span, hipStream_t s) {
+  k_attn_spans<<<dim3((unsigned)((T + 255) / 256)), dim3(256), 0, s>>>(T, S, window, n, starts, prefix,
+                                                                      reinterpret_cast<int2*>(span));
+  return hipGetLastError();
+}
+
+hipError_t launch_rotate(const xhc_dims* d, const xhc_heads* h, const void* src, const int32_t* pos,
+                         const float* table, int64_t positions, bool inverse, void* dst, hipStream_t s) {
+  const int H = h->Hq + 2 * h->Hkv, slots = 256 / (h->D / 16);
+  const int heads = H < slots ? H : slots, tokens = slots / heads;
+  const dim3 grid((unsigned)((d->T + tokens - 1) / tokens)), block(256);
+  const float sign = inverse ? -1.f : 1.f;
+  if (d->state_dtype == XHC_BF16)
+    k_rotate<uint16_t><<<grid, block, 0, s>>>(d->T, d->S, H, h->Hq + h->Hkv, h->D, h->R, h->pairs,
+                                              static_cast<const uint16_t*>(src), pos, table, positions, sign,
+                                              static_cast<uint16_t*>(dst), heads, tokens);
+  else
+    k_rotate<float><<<grid, block, 0, s>>>(d->T, d->S, H, h->Hq + h->Hkv, h->D, h->R, h->pairs,
+                                           static_cast<const float*>(src), pos, table, positions, sign,
+                                           static_cast<float*>(dst), heads, tokens);
+  return hipGetLastError();
+}
+
+}  // namespace xhc

@@ -1,0 +1,461 @@
+// Reverse of the attention of token rows, given do:
+//
+//   p_ij = exp2(s_ij - lse_i),  delta_i = sum_c do_ic o_ic,  dP_ij = do_i v_j
+//   dS_ij = p_ij (dP_ij - delta_i) d s_ij / d (scale q_i k_j)
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i p_ij do_i
+//
+// Two kernels form the probabilities again, each with the sums that it owns in
+// registers: k_attn_dq as the forward goes, k_attn_dkv with a wave's 32 keys
+// fixed and the queries of all heads of the group passing by.  That is seven
+// products in place of five, but no sum is shared between workgroups: no
+// atomics, no fp32 copy of dq, and an order that only the sizes fix.
+#include "xhc_attn.h"
+
+namespace xhc {
+
+namespace {
+
+// Tile blockIdx.x of 64 rows: for head blockIdx.y < Hq the rows' delta and
+// lse, in the order in which k_attn_dkv reads them; in the last of them the
+// spans and what they have in common.
+template <typename TS, int D>
+__global__ __launch_bounds__(256) void k_attn_prep(AttnArgs a, float* lsep, float* delta, int* lo, int* hi,
+                                                   int4* range) {
+  constexpr int LP = D == 96 ? 16 : D / 8;       // lanes of a row
+  const int tile = blockIdx.x, head = blockIdx.y, t0 = tile * kTile;
+  if (head == a.Hq) {
+    if (threadIdx.x >= 64) return;
+    const int t = t0 + threadIdx.x;
+    const int2 s = span_of(a, t);
+    const bool some = s.x < s.y;
+    lo[t] = s.x;
+    hi[t] = s.y;
+    int4 e = make_int4(some ? s.x : INT32_MAX, some ? s.y : 0, some ? s.x : INT32_MAX, some ? s.y : 0);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      e.x = min(e.x, __shfl_xor(e.x, d));
+      e.y = max(e.y, __shfl_xor(e.y, d));
+      e.z = max(e.z, __shfl_xor(e.z, d));
+      e.w = min(e.w, __shfl_xor(e.w, d));
+    }
+    if (threadIdx.x == 0) range[tile] = e;
+    return;
+  }
+  const int c = threadIdx.x % LP * 8;
+#pragma unroll
+  for (int r = threadIdx.x / LP; r < kTile; r += 256 / LP) {
+    const int t = t0 + r;
+    float sum = 0.f;
+    if (t < a.T && c < D) {
+      const int64_t at = ((int64_t)t * a.Hq + head) * D + c;
+      float x[8], y[8];
+      Vec8<TS>::load(reinterpret_cast<const TS*>(a.out) + at, x);
+      Vec8<TS>::load(reinterpret_cast<const TS*>(a.dout) + at, y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], y[i], sum);
+    }
+#pragma unroll
+    for (int d = 1; d < LP; d *= 2) sum += __shfl_xor(sum, d);
+    if (threadIdx.x % LP == 0) {
+      const int64_t to = (int64_t)head * a.Tp + t;
+      delta[to] = sum;
+      lsep[to] = t < a.T ? a.lse[(int64_t)t * a.Hq + head] : 0.f;
+    }
+  }
+}
+
+// p and dS of one pair from the raw product and dP
+template <typename TS>
+__device__ __forceinline__ void reverse_score(float& x, float& dp, const Score& sc, bool capped, float bias, float lse,
+                                              float delta) {
+  float der = 1.f;
+  if (capped) {
+    const float t = tanh_of<TS>(x * sc.mul);
+    x = sc.cap * t;
+    der = 1.f - t * t;
+  } else {
+    x *= sc.mul;
+  }
+  x = __builtin_amdgcn_exp2f(x + bias - lse);
+  dp = x * (dp - delta) * der;
+}
+
+template <typename TS, int D>
+__global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a) {
+  using TL = Tile<TS, D>;
+  constexpr int KS = D / 16, F = D / 32;
+  __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
+  __shared__ int4 red[kAttnWaves];
+  __shared__ __align__(8) uint16_t bits[4];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  int head, tile;
+  attn_place(a.Hq, (int)((a.T + 127) / 128), head, tile);
+  const int kvh = head / (a.Hq / a.Hkv), H = a.Hq + 2 * a.Hkv;
+  const int t = tile * 128 + wave * 32 + lane % 32, T1 = (int)a.T - 1;
+  const bool row = t <= T1;
+  const int2 see = span_of(a, t);
+  const int4 ex = attn_extremes(see, row, red, wave, lane);
+  const uint32_t stride = (uint32_t)H * D * sizeof(TS);
+  const unsigned char* base = reinterpret_cast<const unsigned char*>(a.qkv);
+  const unsigned char* kb = base + (size_t)(a.Hq + kvh) * D * sizeof(TS);
+  const unsigned char* vb = kb + (size_t)a.Hkv * D * sizeof(TS);
+  const uint32_t at = lds_offset(lds);
+
+  f32x16 dq[F];
+#pragma unroll
+  for (int f = 0; f < F; ++f) dq[f] = f32x16{};
+  const int first = ex.x / kTile, end = (ex.y + kTile - 1) / kTile;
+  if (ex.x < ex.y) {
+    Score sc;
+    sc.init(a, head);
+    const int64_t tc = row ? t : T1;
+    const float lse = a.lsep[(int64_t)head * a.Tp + tc], delta = a.delta[(int64_t)head * a.Tp + tc];
+    Frag<TS> q[KS], go[KS];
+    const TS* qp = reinterpret_cast<const TS*>(base) + tc * H * D + head * D;
+    const TS* gp = reinterpret_cast<const TS*>(a.dout) + (tc * a.Hq + head) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      load_frag(qp + 16 * ks + 8 * (lane / 32), q[ks]);
+      load_frag(gp + 16 * ks + 8 * (lane / 32), go[ks]);
+    }
+    TL::copy(kb, stride, first * kTile, T1, at, wave, lane);
+    TL::copy(vb, stride, first * kTile, T1, at + TL::kBytes, wave, lane);
+    for (int kt = first; kt < end; ++kt) {
+      const uint32_t off = (kt - first) % 2 * 2 * TL::kBytes, next = 2 * TL::kBytes - off;
+      wait_vm<0>();
+      lds_barrier();
+      if (kt + 1 < end) {
+        TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, lane);
+        TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, lane);
+      }
+      unsigned char *K = lds + off, *V = K + TL::kBytes;
+      const int j0 = kt * kTile;
+      const bool cut = j0 < ex.z || j0 + kTile > ex.w;
+      uint64_t bad = 0;
+      if (cut) bad = TL::clean(K, bits, wave, lane);
+      const float d0 = (float)(t - j0 - 4 * (lane / 32));
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          Frag<TS> k, v;
+          TL::row_frag(K, rb, ks, lane, k);
+          s = mfma32(k, q[ks], s);
+          TL::row_frag(V, rb, ks, lane, v);
+          dp = mfma32(v, go[ks], dp);
+        }
+        if (a.slopes || a.cap > 0.f) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float x = s[r], y = dp[r];
+            reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 - (float)(32 * rb + sum_row(r))), lse, delta);
+            dp[r] = y;
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            dp[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.mul, -lse)) * (dp[r] - delta);
+        }
+        if (cut) {
+          const int lo = see.x - j0, hi = see.y - j0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * rb + sum_row(r) + 4 * (lane / 32);
+            const bool seen = j >= lo && j < hi;
+            if (bad && ((bad >> j) & 1)) dp[r] = __builtin_nanf("");
+            if (!seen) dp[r] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          Frag<TS> ds;
+          sums_frag(dp, st, ds);
+#pragma unroll
+          for (int f = 0; f < F; ++f) {
+            Frag<TS> k;
+            TL::col_frag(K, f, 2 * rb + st, lane, k);
+            dq[f] = mfma32(k, ds, dq[f]);
+          }
+        }
+      }
+    }
+  }
+  TS* p = reinterpret_cast<TS*>(a.dqkv) + (int64_t)t * H * D + head * D;
+#pragma unroll
+  for (int f = 0; f < F; ++f) store_sums<TS>(dq[f], a.scale, p + 32 * f, row, lane);
+}
+
+// A stage of k_attn_dkv: a tile of queries and of do, and lse, delta, lo and hi
+// of their rows.
+template <typename TL> struct QStage {
+  static constexpr int kRows = 2 * TL::kBytes, kBytes = kRows + 1024;
+};
+
+template <typename TS, int D>
+__global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dkv(AttnArgs a) {
+  using TL = Tile<TS, D>;
+  using ST = QStage<TL>;
+  constexpr int KS = D / 16, F = D / 32;
+  __shared__ __align__(1024) unsigned char lds[2 * ST::kBytes];
+  __shared__ __align__(8) uint16_t bits[8];
+  __shared__ int reach[2];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int g = a.Hq / a.Hkv, mine = g / a.parts, H = a.Hq + 2 * a.Hkv;
+  const int tiles = (int)((a.T + 127) / 128), qtiles = (int)(a.Tp / kTile);
+  int which, tile;
+  attn_place(a.Hkv * a.parts, tiles, which, tile);
+  tile = tiles - 1 - tile;                       // the first keys are seen by most queries
+  const int kvh = which / a.parts, part = which % a.parts;
+  const int head0 = kvh * g + part * mine;
+  const int j0 = tile * 128, T1 = (int)a.T - 1;
+  const int key = j0 + wave * 32 + lane % 32;
+  const bool row = key <= T1;
+  const unsigned char* qb = reinterpret_cast<const unsigned char*>(a.qkv);
+  const unsigned char* gb = reinterpret_cast<const unsigned char*>(a.dout);
+  const uint32_t qstride = (uint32_t)H * D * sizeof(TS), gstride = (uint32_t)a.Hq * D * sizeof(TS);
+  const uint32_t at = lds_offset(lds);
+
+  // the first and last tile of queries of which some row sees one of these keys
+  if (threadIdx.x < 2) reach[threadIdx.x] = threadIdx.x ? -1 : INT32_MAX;
+  __syncthreads();
+  auto sees = [&](const int4& e) { return e.x < j0 + 128 && e.y > j0 && e.x < e.y; };
+  int from = INT32_MAX, upto = -1;
+  for (int i = threadIdx.x; i < qtiles; i += 64 * kAttnWaves)
+    if (sees(a.range[i])) {
+      from = min(from, i);
+      upto = max(upto, i);
+    }
+  if (upto >= 0) {
+    atomicMin(&reach[0], from);
+    atomicMax(&reach[1], upto);
+  }
+  __syncthreads();
+  from = __builtin_amdgcn_readfirstlane(reach[0]);
+  upto = __builtin_amdgcn_readfirstlane(reach[1]);
+
+  f32x16 dk[F], dv[F];
+#pragma unroll
+  for (int f = 0; f < F; ++f) dk[f] = dv[f] = f32x16{};
+  if (from <= upto) {
+    Frag<TS> kf[KS], vf[KS];
+    const TS* kp = reinterpret_cast<const TS*>(qb) + ((int64_t)(row ? key : T1) * H + a.Hq + kvh) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      load_frag(kp + 16 * ks + 8 * (lane / 32), kf[ks]);
+      load_frag(kp + (int64_t)a.Hkv * D + 16 * ks + 8 * (lane / 32), vf[ks]);
+    }
+    auto copy = [&](int head, int qt, uint32_t to) {
+      TL::copy(qb + (size_t)head * D * sizeof(TS), qstride, qt * kTile, T1, to, wave, lane);
+      TL::copy(gb + (size_t)head * D * sizeof(TS), gstride, qt * kTile, T1, to + TL::kBytes, wave, lane);
+      const int64_t r = (int64_t)qt * kTile + lane;
+      const void* p = wave == 0   ? (const void*)(a.lsep + (int64_t)head * a.Tp + r)
+                      : wave == 1 ? (const void*)(a.delta + (int64_t)head * a.Tp + r)
+                      : wave == 2 ? (const void*)(a.lo + r)
+                                  : (const void*)(a.hi + r);
+      lds_dma4(p, to + ST::kRows + wave * 256);
+    };
+    // the tile behind (head, qt) that is to be taken; head == head0 + mine: none
+    auto advance = [&](int& head, int& qt, int4& e) {
+      do {
+        if (++qt > upto) {
+          qt = from;
+          ++head;
+        }
+        e = a.range[qt];
+      } while (head < head0 + mine && !sees(e));
+    };
+    int head = head0, qt = from, stage = 0;
+    int4 e = a.range[qt];
+    copy(head, qt, at);
+    while (head < head0 + mine) {
+      int nhead = head, nqt = qt;
+      int4 ne;
+      advance(nhead, nqt, ne);      // (loads of its own stand before the copies, which a wait for them would wait for)
+      Score sc;
+      sc.init(a, head);
+      wait_vm<0>();
+      lds_barrier();
+      unsigned char* Q = lds + stage * ST::kBytes;
+      unsigned char* G = Q + TL::kBytes;
+      stage ^= 1;
+      if (nhead < head0 + mine) copy(nhead, nqt, at + stage * ST::kBytes);
+      const bool cut = e.z > j0 || e.w < j0 + 128;
+      uint64_t bad = 0;
+      if (cut) bad = TL::clean(Q, bits, wave, lane) | TL::clean(G, bits + 4, wave, lane);
+      const float* rows = reinterpret_cast<const float*>(Q + ST::kRows) + 4 * (lane / 32);
+      const float d0 = (float)(qt * kTile + 4 * (lane / 32) - key);
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          Frag<TS> q, go;
+          TL::row_frag(Q, rb, ks, lane, q);
+          s = mfma32(q, kf[ks], s);
+          TL::row_frag(G, rb, ks, lane, go);
+          dp = mfma32(go, vf[ks], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 lse = *reinterpret_cast<const float4*>(rows + 32 * rb + 8 * i);
+          const float4 del = *reinterpret_cast<const float4*>(rows + 64 + 32 * rb + 8 * i);
+          const float L[4] = {lse.x, lse.y, lse.z, lse.w}, E[4] = {del.x, del.y, del.z, del.w};
+#pragma unroll
+          for (int e4 = 0; e4 < 4; ++e4) {
+            const int r = 4 * i + e4;
+            if (a.slopes || a.cap > 0.f) {
+              float x = s[r], y = dp[r];
+              reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 + (float)(32 * rb + sum_row(r))), L[e4],
+                                E[e4]);
+              s[r] = x;
+              dp[r] = y;
+            } else {
+              s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.mul, -L[e4]));
+              dp[r] = s[r] * (dp[r] - E[e4]);
+            }
+          }
+        }
+        if (cut) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int4 lo = *reinterpret_cast<const int4*>(rows + 128 + 32 * rb + 8 * i);
+            const int4 hi = *reinterpret_cast<const int4*>(rows + 192 + 32 * rb + 8 * i);
+            const int L[4] = {lo.x, lo.y, lo.z, lo.w}, U[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+              const int r = 4 * i + e4;
+              const bool seen = key >= L[e4] && key < U[e4];
+              if (bad && ((bad >> (32 * rb + sum_row(r) + 4 * (lane / 32))) & 1))
+                s[r] = dp[r] = __builtin_nanf("");
+              if (!seen) s[r] = dp[r] = 0.f;
+            }
+          }
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          Frag<TS> p, ds;
+          sums_frag(s, st, p);
+          sums_frag(dp, st, ds);
+#pragma unroll
+          for (int f = 0; f < F; ++f) {
+            Frag<TS> x;
+            TL::col_frag(G, f, 2 * rb + st, lane, x);
+            dv[f] = mfma32(x, p, dv[f]);
+            TL::col_frag(Q, f, 2 * rb + st, lane, x);
+            dk[f] = mfma32(x, ds, dk[f]);
+          }
+        }
+      }
+      head = nhead;
+      qt = nqt;
+      e = ne;
+    }
+  }
+  if (a.parts == 1) {
+    TS* p = reinterpret_cast<TS*>(a.dqkv) + ((int64_t)key * H + a.Hq + kvh) * D;
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      store_sums<TS>(dk[f], a.scale, p + 32 * f, row, lane);
+      store_sums<TS>(dv[f], 1.f, p + (int64_t)a.Hkv * D + 32 * f, row, lane);
+    }
+  } else {
+    float* p = a.part + (((int64_t)part * a.T + key) * 2 * a.Hkv + kvh) * D;
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      store_sums<float>(dk[f], a.scale, p + 32 * f, row, lane);
+      store_sums<float>(dv[f], 1.f, p + (int64_t)a.Hkv * D + 32 * f, row, lane);
+    }
+  }
+}
+
+// dk and dv from the parts, added in order; `row` = 2 Hkv D elements a token
+template <typename TS>
+__global__ __launch_bounds__(256) void k_attn_join(int64_t T, int row, int parts, const float* part, int H, int Hq, int D,
+                                                   TS* dqkv) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= T * row) return;
+  const int64_t t = i / row;
+  float s[8];
+  Vec8<float>::load(part + i, s);
+  for (int p = 1; p < parts; ++p) {
+    float x[8];
+    Vec8<float>::load(part + (int64_t)p * T * row + i, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += x[e];
+  }
+  Vec8<TS>::store(dqkv + (t * H + Hq) * D + (i - t * row), s);
+}
+
+constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+// Parts of a group's heads for dk and dv: 512 workgroups fill the chip's 256 CUs
+// twice over; with fewer, a group's heads are divided among several, whose sums
+// are then added.
+int parts_of(int64_t T, int Hq, int Hkv) {
+  const int64_t wg = (T + 127) / 128 * Hkv;
+  const int g = Hq / Hkv;
+  for (int p = 1; p < g; ++p)
+    if (g % p == 0 && wg * p >= 512) return p;
+  return g;
+}
+
+template <typename TS, int D> hipError_t run_bwd(AttnArgs a, char* ws, hipStream_t s) {
+  const size_t heads = up((size_t)a.Tp * a.Hq * 4), rows = up((size_t)a.Tp * 4);
+  float* lsep = reinterpret_cast<float*>(ws);
+  float* delta = reinterpret_cast<float*>(ws + heads);
+  int* lo = reinterpret_cast<int*>(ws + 2 * heads);
+  int* hi = reinterpret_cast<int*>(ws + 2 * heads + rows);
+  int4* range = reinterpret_cast<int4*>(ws + 2 * heads + 2 * rows);
+  a.part = reinterpret_cast<float*>(ws + 2 * heads + 2 * rows + up((size_t)a.Tp / kTile * 16));
+  k_attn_prep<TS, D><<<dim3((unsigned)(a.Tp / kTile), a.Hq + 1), dim3(256), 0, s>>>(a, lsep, delta, lo, hi, range);
+  a.lsep = lsep, a.delta = delta, a.lo = lo, a.hi = hi, a.range = range;
+  const unsigned tiles = (unsigned)((a.T + 127) / 128);
+  k_attn_dkv<TS, D><<<dim3(tiles * a.Hkv * a.parts), dim3(64 * kAttnWaves), 0, s>>>(a);
+  if (a.parts > 1) {
+    const int row = 2 * a.Hkv * D;
+    k_attn_join<TS><<<dim3((unsigned)((a.T * row / 8 + 255) / 256)), dim3(256), 0, s>>>(
+        a.T, row, a.parts, a.part, a.Hq + 2 * a.Hkv, a.Hq, D, static_cast<TS*>(a.dqkv));
+  }
+  k_attn_dq<TS, D><<<dim3(tiles * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename TS> hipError_t run_bwd_of(int D, const AttnArgs& a, char* ws, hipStream_t s) {
+  switch (D) {
+    case 32: return run_bwd<TS, 32>(a, ws, s);
+    case 64: return run_bwd<TS, 64>(a, ws, s);
+    case 96: return run_bwd<TS, 96>(a, ws, s);
+    default: return run_bwd<TS, 128>(a, ws, s);
+  }
+}
+
+}  // namespace
+
+size_t attn_bwd_ws_bytes(int64_t T, int Hq, int Hkv, int D) {
+  const int64_t Tp = (T + kTile - 1) / kTile * kTile;
+  const int parts = parts_of(T, Hq, Hkv);
+  return 2 * up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) +
+         (parts > 1 ? (size_t)parts * T * 2 * Hkv * D * 4 : 0);
+}
+
+hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
+                           const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                           void* ws, hipStream_t s) {
+  AttnArgs a{};
+  a.qkv = qkv;
+  a.span = reinterpret_cast<const int2*>(span);
+  a.slopes = slopes;
+  a.out = const_cast<void*>(out);
+  a.lse = const_cast<float*>(lse);
+  a.dout = dout;
+  a.dqkv = dqkv;
+  a.T = d->T, a.S = d->S, a.Tp = (d->T + kTile - 1) / kTile * kTile;
+  a.Hq = h->Hq, a.Hkv = h->Hkv, a.window = h->window;
+  a.parts = parts_of(d->T, h->Hq, h->Hkv);
+  a.scale = h->scale, a.cap = h->cap;
+  return d->state_dtype == XHC_BF16 ? run_bwd_of<uint16_t>(h->D, a, static_cast<char*>(ws), s)
+                                    : run_bwd_of<float>(h->D, a, static_cast<char*>(ws), s);
+}
+
+}  // namespace xhc

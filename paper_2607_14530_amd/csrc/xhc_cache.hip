@@ -1,0 +1,800 @@
+// A paged cache of keys and values in 4 bits, and attention over it.
+//
+// A page holds, for each key and value head, blocks of 32 tokens, and a block
+// the four operands of its products as the matrix instructions take them, so
+// that attention reads runs and unpacks in place:
+//
+//   keys    [half of 16 tokens][lane][D / 32 words]: lane l has channels 32 g +
+//           8 (l / 16) + 0 .. 7 of token l % 16 in word g, an operand of scores^T
+//           = K Q^T over the 32 channels of group g
+//   values  [lane][D / 16 words] in pieces of four words: lane l has channel 16 n
+//           + l % 16 of tokens 16 (j / 4) + 4 (l / 16) + j % 4, j = 0 .. 7, in word
+//           n: the order in which a lane holds the probabilities of its query
+//   scales  of keys, of values: [l / 16][half][group][4 tokens] bf16: lane l
+//           loads a word of its row of 16 lanes, which takes it from there (a DPP
+//           broadcast within the row, part of the instruction that multiplies)
+//
+// A group's scale is a factor of its share of a score, and of a probability
+// before it is rounded as an operand of the product with the values.
+#include "xhc_attn.h"
+
+namespace xhc {
+
+namespace {
+
+constexpr int kBlock = 32;                       // tokens of a block
+
+struct CacheArgs {
+  const void* qkv;        // append: [T][Hq + 2 Hkv][D]
+  const float* table;
+  const int *starts, *lens, *pages;
+  unsigned char* pool;
+  void *q, *k, *v;        // append's q, read's k and v; attend: q in, out in k
+  const float* slopes;
+  int64_t T;
+  int Hq, Hkv, R, pairs, window, page, npages, B, per_seq;
+  int rows;               // append: tokens that a workgroup looks after
+  int tokens;             // append: of which it rotates the queries
+  unsigned qblocks;       // append: workgroups that rotate queries
+  float scale, cap;
+  // attend
+  float* part;            // [2 grid][16 RT][D]
+  float2* ml;             // [2 grid][16 RT]: maximum and sum
+  int64_t* where;         // [B][2]: first unit of a sequence, units of its segments; [2 B]: units of a workgroup
+};
+
+template <int D> struct Block {
+  static constexpr int G = D / 32, W = D / 16;
+  static constexpr int kCodes = 16 * D, kScales = 2 * D, kBytes = 2 * kCodes + 2 * kScales;
+  static constexpr int kKeys = 0, kValues = kCodes, kKeyScales = 2 * kCodes, kValueScales = 2 * kCodes + kScales;
+  // byte of the word of channels 8 c .. 8 c + 7 of a token's key
+  static __device__ __forceinline__ int key_word(int tok, int c) {
+    return kKeys + ((tok / 16 * 64 + c % 4 * 16 + tok % 16) * G + c / 4) * 4;
+  }
+  // byte of word n of a lane's values
+  static __device__ __forceinline__ int value_word(int lane, int n) {
+    const int at = n / 4 * 4, wide = W - at < 4 ? W - at : 4;
+    return kValues + (at * 64 + lane * wide + n % 4) * 4;
+  }
+  static __device__ __forceinline__ int value_lane(int tok, int ch) { return tok % 16 / 4 * 16 + ch % 16; }
+  static __device__ __forceinline__ int value_slot(int tok) { return tok / 16 * 4 + tok % 4; }
+  // byte of a token's scale of group g, from the first of the keys' or values'
+  static __device__ __forceinline__ int scale_at(int tok, int g) {
+    return ((tok % 16 / 4 * 2 + tok / 16) * G + g) * 8 + tok % 4 * 2;
+  }
+};
+
+template <int D> __device__ __forceinline__ unsigned char* block_at(const CacheArgs& a, int page, int head, int tok) {
+  return a.pool + (((int64_t)page * a.Hkv + head) * (a.page / kBlock) + tok / kBlock) * Block<D>::kBytes;
+}
+
+// The sequence that token t of a call belongs to: the last b with starts[b] <=
+// t, or -1.  All lanes of the wave ask for the same t; a step looks at 64 places.
+__device__ __forceinline__ int sequence_of(const int* starts, int B, int64_t t, int lane) {
+  int first = 0, n = B;
+  do {
+    const int step = (n + 63) / 64, i = lane * step;
+    const int c = __popcll(__ballot(i < n && starts[first + i] <= t));
+    if (c == 0) return -1;
+    first += (c - 1) * step;
+    n = n - (c - 1) * step < step ? n - (c - 1) * step : step;
+  } while (n > 1);
+  return __builtin_amdgcn_readfirstlane(first);
+}
+
+// Eight consecutive channels from channel c of a head, rotated at the position
+// whose table row is cs.
+template <typename TS>
+__device__ __forceinline__ void rotated8(const TS* head, int c, const float* cs, int R, int pairs, float (&x)[8]) {
+  Vec8<TS>::load(head + c, x);
+  if (c >= R) return;
+  if (pairs) {
+    float w[8], a[4], b[4];
+    Vec8<float>::load(cs + c, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = x[2 * i], b[i] = x[2 * i + 1];
+    turn<4>(a, b, w, 1.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = a[i], x[2 * i + 1] = b[i];
+  } else {
+    const bool low = c < R / 2;
+    float w[16], y[8];
+    Vec8<float>::load(cs + 2 * (low ? c : c - R / 2), *reinterpret_cast<float(*)[8]>(w));
+    Vec8<float>::load(cs + 2 * (low ? c : c - R / 2) + 8, *reinterpret_cast<float(*)[8]>(w + 8));
+    Vec8<TS>::load(head + (low ? c + R / 2 : c - R / 2), y);
+    if (low) {
+      turn<8>(x, y, w, 1.f);
+    } else {
+      turn<8>(y, x, w, 1.f);
+    }
+  }
+}
+
+// Codes of eight channels of a group that four neighbouring lanes share, and
+// its scale (bf16 bits): the largest magnitude / 6, rounded; divisions rounded
+// to the nearest, so that the codes are the definition's to the bit.
+__device__ __forceinline__ uint32_t hold8(const float (&x)[8], uint32_t& bits) {
+  uint32_t top = 0;                              // magnitudes order as their bits do, NaN above all
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  bits = top >= 0x7f800000u              ? 0x7fc0u
+         : top < (27u << 23)             ? 0u               // below 2^-100
+                                         : f2bf(__uint_as_float(top) / 6.f);
+  const float s = __uint_as_float(bits << 16);
+  uint32_t w = 0;
+  if (bits != 0 && bits != 0x7fc0u) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float m = fabsf(x[i]) / s;
+      uint32_t c = (m > 0.25f) + (m >= 0.75f) + (m > 1.25f) + (m >= 1.75f) + (m > 2.5f) + (m >= 3.5f) + (m > 5.f);
+      c |= __float_as_uint(x[i]) >> 31 << 3;
+      w |= c << (4 * i);
+    }
+  }
+  return w;
+}
+
+// The first workgroups rotate the queries, a few tokens each.  Each of the
+// others looks after `rows` tokens for one head: it stores the block of each
+// token that is the call's first in its block, which may go on behind them;
+// so no two workgroups write to a block.  Tokens that were there before keep
+// their bits.
+template <typename TS, int D>
+__global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
+  using BL = Block<D>;
+  constexpr int P = D / 8;                       // threads of a head
+  __shared__ uint8_t codes[kBlock][D + 4];
+  __shared__ int64_t pos[256];
+  const int tid = threadIdx.x, lane = tid % 64, H = a.Hq + 2 * a.Hkv;
+  const int64_t cap = (int64_t)a.per_seq * a.page;
+  const TS* qkv = static_cast<const TS*>(a.qkv);
+  if (blockIdx.x < a.qblocks) {
+    const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
+    for (int i = tid / 64; i < a.tokens; i += 4) {
+      const int64_t t = t0 + i;
+      const int b = t < a.T ? sequence_of(a.starts, a.B, t, lane) : -1;
+      int64_t p = -1;
+      if (b >= 0 && t < a.starts[b + 1]) p = a.lens[b] - (a.starts[b + 1] - t);
+      if (lane == 0) pos[i] = p < cap ? p : -1;
+    }
+    __syncthreads();
+    TS* q = static_cast<TS*>(a.q);
+    const int all = a.tokens * a.Hq * P;
+    for (int u = tid; u < all; u += 256) {
+      const int c = u % P * 8, hd = u / P % a.Hq, i = u / P / a.Hq;
+      if (pos[i] < 0) continue;
+      float x[8];
+      rotated8<TS>(qkv + ((t0 + i) * H + hd) * D, c, a.table + pos[i] * a.R, a.R, a.pairs, x);
+      Vec8<TS>::store(q + ((t0 + i) * a.Hq + hd) * D + c, x);
+    }
+    return;
+  }
+  const unsigned mine = blockIdx.x - a.qblocks;
+  const int head = mine % a.Hkv;
+  int64_t t = (int64_t)(mine / a.Hkv) * a.rows;
+  const int64_t behind = t + a.rows < a.T ? t + a.rows : a.T;
+  while (t < behind) {
+    const int b = sequence_of(a.starts, a.B, t, lane);
+    if (b < 0) {                                 // in front of the first sequence
+      const int64_t s = a.starts[0];
+      if (s >= behind) return;
+      t = s;
+      continue;
+    }
+    const int64_t first = a.starts[b] > 0 ? a.starts[b] : 0, after = a.starts[b + 1], end = after < a.T ? after : a.T;
+    if (t >= end) return;                        // behind the last (starts ascend)
+    const int64_t p = a.lens[b] - (after - t);
+    if (p < 0 || p >= cap) {
+      t = p < 0 && t - p < end ? t - p : end;
+      continue;
+    }
+    const int64_t next = t + kBlock - p % kBlock < end ? t + kBlock - p % kBlock : end;
+    const int idx = a.pages[(int64_t)b * a.per_seq + p / a.page];
+    // the block's first token of this call: where it begins, or where the call's tokens of the sequence do
+    if ((p % kBlock == 0 || t == first) && idx >= 0 && idx < a.npages) {
+      unsigned char* to = block_at<D>(a, idx, head, (int)(p % a.page));
+      const int at = (int)(p % kBlock), n = (int)(next - t);     // tokens at .. at + n - 1 of the block are new
+      for (int u = tid; u < n * P * 2; u += 256) {
+        const int c = u % P, i = u / P % n, val = u / P / n, tok = at + i;
+        const TS* src = qkv + ((t + i) * H + a.Hq + (val ? a.Hkv : 0) + head) * D;
+        float x[8];
+        if (val)
+          Vec8<TS>::load(src + 8 * c, x);
+        else
+          rotated8<TS>(src, 8 * c, a.table + (p + i) * a.R, a.R, a.pairs, x);
+        uint32_t bits;
+        const uint32_t w = hold8(x, bits);
+        if (c % 4 == 0)
+          *reinterpret_cast<uint16_t*>(to + (val ? BL::kValueScales : BL::kKeyScales) + BL::scale_at(tok, c / 4)) =
+              (uint16_t)bits;
+        if (val) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) codes[tok][8 * c + e] = (uint8_t)(w >> (4 * e) & 15);
+        } else {
+          *reinterpret_cast<uint32_t*>(to + BL::key_word(tok, c)) = w;
+        }
+      }
+      __syncthreads();
+      for (int u = tid; u < 64 * BL::W; u += 256) {
+        const int l = u % 64, word = u / 64, ch = 16 * word + l % 16;
+        uint32_t w = 0, keep = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int tok = 16 * (j / 4) + 4 * (l / 16) + j % 4;
+          if (tok >= at && tok < at + n)
+            w |= (uint32_t)codes[tok][ch] << (4 * j);
+          else
+            keep |= 15u << (4 * j);
+        }
+        if (keep == 0xffffffffu) continue;
+        uint32_t* p32 = reinterpret_cast<uint32_t*>(to + BL::value_word(l, word));
+        *p32 = keep ? (*p32 & keep) | w : w;
+      }
+      __syncthreads();
+    }
+    t = next;
+  }
+}
+
+__device__ __forceinline__ float held_value(uint32_t code) {
+  const float m = (float)(0xc8643210u >> (4 * (code & 7)) & 15) * 0.5f;
+  return code & 8 ? -m : m;
+}
+
+template <typename TS, int D>
+__global__ __launch_bounds__(256) void k_cache_read(CacheArgs a) {
+  using BL = Block<D>;
+  constexpr int P = D / 8;
+  const int64_t t = blockIdx.x;
+  const int lane = threadIdx.x % 64;
+  const int b = sequence_of(a.starts, a.B, t, lane);
+  if (b < 0 || t >= a.starts[b + 1]) return;
+  const int64_t p = a.lens[b] - (a.starts[b + 1] - t), cap = (int64_t)a.per_seq * a.page;
+  if (p < 0 || p >= cap) return;
+  const int idx = a.pages[(int64_t)b * a.per_seq + p / a.page];
+  if (idx < 0 || idx >= a.npages) return;
+  const int tok = (int)(p % kBlock);
+  for (int u = threadIdx.x; u < a.Hkv * P * 2; u += 256) {
+    const int c = u % P, head = u / P % a.Hkv, val = u / P / a.Hkv;
+    const unsigned char* from = block_at<D>(a, idx, head, (int)(p % a.page));
+    const uint16_t bits = *reinterpret_cast<const uint16_t*>(from + (val ? BL::kValueScales : BL::kKeyScales) +
+                                                             BL::scale_at(tok, c / 4));
+    uint32_t w = 0;
+    if (val) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int ch = 8 * c + e;
+        const uint32_t word = *reinterpret_cast<const uint32_t*>(from + BL::value_word(BL::value_lane(tok, ch), ch / 16));
+        w |= (word >> (4 * BL::value_slot(tok)) & 15) << (4 * e);
+      }
+    } else {
+      w = *reinterpret_cast<const uint32_t*>(from + BL::key_word(tok, c));
+    }
+    const float s = __uint_as_float((uint32_t)bits << 16);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = held_value(w >> (4 * e) & 15) * s;
+    Vec8<TS>::store(static_cast<TS*>(val ? a.v : a.k) + (t * a.Hkv + head) * D + 8 * c, x);
+  }
+}
+
+// ---------------------------------------------------------------- attention over the cache
+
+__device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, f32x4 c) { return mfma_16x16x32(a, b, c); }
+__device__ __forceinline__ f32x4 mfma16(const Frag32& a, const Frag32& b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+  return c;
+}
+// a word's eight codes, exact in either type
+__device__ __forceinline__ void unpack_codes(uint32_t w, uint4& f) {
+  f.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0));
+  f.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1));
+  f.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2));
+  f.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3));
+}
+__device__ __forceinline__ void unpack_codes(uint32_t w, Frag32& f) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1),
+              c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+  f = Frag32{{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y}};
+}
+__device__ __forceinline__ void pack_frag(const float (&x)[8], uint4& f) { f = pack8(x); }
+__device__ __forceinline__ void pack_frag(const float (&x)[8], Frag32& f) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.v[j] = x[j];
+}
+// lane K of this lane's row of 16
+template <int K> __device__ __forceinline__ float row_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + K, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float max_quarters(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+// A block of keys and values of one head, on its way.
+template <int D> struct Raw {
+  uint32_t k[2][D / 32], v[D / 16], ks, vs;
+  template <int N> static __device__ __forceinline__ void words(const unsigned char* p, uint32_t* w) {
+    if constexpr (N == 4) {
+      const uint4 x = *reinterpret_cast<const uint4*>(p);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else if constexpr (N == 2) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      w[0] = x.x, w[1] = x.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+  }
+  __device__ __forceinline__ void load(const unsigned char* p, int lane) {
+    using BL = Block<D>;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) words<BL::G>(p + BL::kKeys + (h * 64 + lane) * BL::G * 4, k[h]);
+#pragma unroll
+    for (int at = 0; at < BL::W; at += 4) {
+      if (BL::W - at >= 4)
+        words<4>(p + BL::kValues + (at * 64 + lane * 4) * 4, v + at);
+      else
+        words<2>(p + BL::kValues + (at * 64 + lane * 2) * 4, v + at);
+    }
+    // of a row of 16 lanes the first 4 G have a word each
+    const int s = (lane / 16 * 4 * BL::G + (lane % 16 < 4 * BL::G ? lane % 16 : 0)) * 4;
+    ks = *reinterpret_cast<const uint32_t*>(p + BL::kKeyScales + s);
+    vs = *reinterpret_cast<const uint32_t*>(p + BL::kValueScales + s);
+  }
+};
+
+struct Sequence {
+  int64_t first, end, after;   // its tokens of the call (within 0 .. T), and starts[b + 1]
+  int64_t len, upto;           // its tokens, and those that its row of the table has room for
+  int blocks, block0;          // of 32 keys that its tokens see, the first of them
+  int tiles;                   // of its rows
+};
+__device__ __forceinline__ Sequence sequence(const CacheArgs& a, int b, int rows) {
+  Sequence s;
+  s.first = a.starts[b] > 0 ? a.starts[b] : 0;
+  s.after = a.starts[b + 1];
+  s.end = s.after < a.T ? s.after : a.T;
+  s.len = a.lens[b];
+  const int64_t cap = (int64_t)a.per_seq * a.page;
+  s.upto = s.len < cap ? s.len : cap;
+  const int64_t p = s.len - (s.after - s.first);
+  const int64_t lo = a.window > 0 && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+  const bool some = s.end > s.first && s.upto > lo;
+  s.block0 = (int)(some ? lo / kBlock : 0);
+  s.blocks = some ? (int)((s.upto + kBlock - 1) / kBlock) - s.block0 : 0;
+  s.tiles = some ? (int)(((s.end - s.first) * (a.Hq / a.Hkv) + rows - 1) / rows) : 0;
+  return s;
+}
+
+// The work in units of one block of one head and tile of rows, in the order
+// sequence, tile, head, block, is cut into equal runs, one for each workgroup:
+// lengths need not be alike, nor known to the host.  A run takes the end of a
+// segment (a sequence's tile and head), whole segments, and the beginning of
+// another; what it has of a segment that it does not have whole goes to one of
+// its two places, and k_cache_join adds those up in order.
+//
+// Within a run a segment's blocks go around the four waves, each with the
+// running maximum and sum of its rows; a block's loads are under way while the
+// one before is worked on.  16 RT rows (tokens times the query heads of the
+// group) are the columns of 16x16x32 products.
+constexpr int attend_wgs(bool f32, int rows) { return rows == 16 ? (f32 ? 2 : 3) : (f32 ? 1 : 2); }   // of a CU
+
+template <typename TS, int D, int RT>
+__global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_cache_attend(CacheArgs a) {
+  using BL = Block<D>;
+  constexpr int G = BL::G, W = BL::W, ROWS = 16 * RT, LD = D + 4;
+  __shared__ __align__(16) float sums[4][16][LD];
+  __shared__ float2 mls[4][16];
+  __shared__ int64_t scan[256];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int g = a.Hq / a.Hkv, r16 = lane % 16;
+
+  // units in front of each thread's share of the sequences, and of all
+  const int share = (a.B + 255) / 256, b0 = tid * share, b1 = min(a.B, b0 + share);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Sequence s = sequence(a, b, ROWS);
+    mine += (int64_t)s.tiles * a.Hkv * s.blocks;
+  }
+  scan[tid] = mine;
+  __syncthreads();
+  for (int d = 1; d < 256; d *= 2) {
+    const int64_t x = tid >= d ? scan[tid - d] : 0;
+    __syncthreads();
+    scan[tid] += x;
+    __syncthreads();
+  }
+  const int64_t all = scan[255];
+  // at least four blocks a workgroup, one for each wave
+  int64_t run = (all + gridDim.x - 1) / gridDim.x;
+  if (run < 4) run = 4;
+  if (blockIdx.x == 0) {
+    int64_t at = scan[tid] - mine;
+    for (int b = b0; b < b1; ++b) {
+      const Sequence s = sequence(a, b, ROWS);
+      a.where[2 * b] = at;
+      a.where[2 * b + 1] = s.blocks;
+      at += (int64_t)s.tiles * a.Hkv * s.blocks;
+    }
+    if (tid == 0) a.where[2 * (int64_t)a.B] = run;
+  }
+  const int64_t u0 = (int64_t)blockIdx.x * run, u1 = u0 + run < all ? u0 + run : all;
+  if (u0 >= u1) return;
+  // the sequence of unit u0, and the units in front of it
+  int owner = 0;                                 // the first thread whose share ends behind u0
+  for (int upto = 255; owner < upto;) {
+    const int c = (owner + upto) / 2;
+    if (scan[c] > u0)
+      upto = c;
+    else
+      owner = c + 1;
+  }
+  int64_t before = owner > 0 ? scan[owner - 1] : 0;
+  int b = owner * share;
+  Sequence sq = sequence(a, b, ROWS);
+  for (;;) {
+    const int64_t n = (int64_t)sq.tiles * a.Hkv * sq.blocks;
+    if (before + n > u0) break;
+    before += n;
+    sq = sequence(a, ++b, ROWS);
+  }
+
+  for (int64_t u = u0; u < u1;) {
+    while (u >= before + (int64_t)sq.tiles * a.Hkv * sq.blocks) {
+      before += (int64_t)sq.tiles * a.Hkv * sq.blocks;
+      sq = sequence(a, ++b, ROWS);
+    }
+    const int64_t seg = (u - before) / sq.blocks, seg0 = before + seg * sq.blocks;
+    const int head = (int)(seg % a.Hkv), tile = (int)(seg / a.Hkv);
+    const int from = (int)(u - seg0);
+    const int64_t last = u1 < seg0 + sq.blocks ? u1 : seg0 + sq.blocks;
+    const int upto = (int)(last - seg0);         // blocks from .. upto - 1 of the segment are taken here
+
+    // this lane's rows: row r16 of each of the RT tiles
+    Frag<TS> q[RT][G];
+    int see[RT], low[RT];                        // the row sees low .. see - 1
+    float m[RT], l[RT], slope[RT];
+    f32x4 o[RT][W];
+    int least = INT32_MAX, most = 0;             // every row sees most .. least - 1
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int64_t row = (int64_t)tile * ROWS + rt * 16 + r16, i = row / g;
+      const int64_t t = sq.first + i, p = sq.len - (sq.after - t);
+      const bool is = t < sq.end && p >= 0 && p < (int64_t)a.per_seq * a.page;
+      const int qh = head * g + (int)(row % g);
+      see[rt] = is ? (int)p + 1 : 0;
+      low[rt] = is && a.window > 0 && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
+      slope[rt] = a.slopes ? a.slopes[qh] * kLog2e : 0.f;
+      if (is) {                                  // (what the other rows give is not used)
+        least = min(least, see[rt]);
+        most = max(most, low[rt]);
+      }
+      const TS* qp = static_cast<const TS*>(a.q) + ((is ? t : sq.first) * a.Hq + qh) * D + 8 * (lane / 16);
+#pragma unroll
+      for (int k = 0; k < G; ++k) load_frag(qp + 32 * k, q[rt][k]);
+      m[rt] = -__builtin_huge_valf();
+      l[rt] = 0.f;
+#pragma unroll
+      for (int n = 0; n < W; ++n) o[rt][n] = f32x4{};
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) {
+      least = min(least, __shfl_xor(least, d));
+      most = max(most, __shfl_xor(most, d));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+    const float mul = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e, cap = a.cap * kLog2e;
+
+    const int count = (upto - from - wave + 3) / 4;          // this wave's blocks: from + wave + 4 i
+    const int* pages = a.pages + (int64_t)b * a.per_seq;
+    auto token0 = [&](int i) { return (sq.block0 + from + wave + 4 * i) * kBlock; };
+    for (int i0 = 0; i0 < count; i0 += 64) {
+      const int n = min(64, count - i0);
+      int mypage = -1;
+      if (lane < n) mypage = pages[token0(i0 + lane) / a.page];
+      // the blocks that are there, one bit each
+      uint64_t left = __ballot(mypage >= 0 && mypage < a.npages);
+      Raw<D> raw, nextraw;
+      auto fetch = [&](Raw<D>& r, int i) {
+        const int pg = __builtin_amdgcn_readlane(mypage, i);
+        r.load(block_at<D>(a, pg, head, token0(i0 + i) % a.page), lane);
+      };
+      if (left) fetch(raw, __builtin_ctzll(left));
+      while (left) {
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        if (left) fetch(nextraw, __builtin_ctzll(left));
+        const int j0 = token0(i0 + i);
+        const bool cut = j0 + kBlock > least || j0 < most;   // some row does not see all of the block
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{};
+        const float kl = bf_lo(raw.ks), kh = bf_hi(raw.ks), vl = bf_lo(raw.vs), vh = bf_hi(raw.vs);
+        unroll<2 * G>([&](auto hg) {
+          constexpr int h = hg.value / G, k = hg.value % G;
+          Frag<TS> x;
+          unpack_codes(raw.k[h][k], x);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const f32x4 part = mfma16(x, q[rt][k], f32x4{});
+            constexpr int W0 = (h * G + k) * 2;  // words of the row of lanes: tokens 0, 1 and 2, 3 of the four
+            s[rt][h][0] = fmaf(row_lane<W0>(kl), part[0], s[rt][h][0]);
+            s[rt][h][1] = fmaf(row_lane<W0>(kh), part[1], s[rt][h][1]);
+            s[rt][h][2] = fmaf(row_lane<W0 + 1>(kl), part[2], s[rt][h][2]);
+            s[rt][h][3] = fmaf(row_lane<W0 + 1>(kh), part[3], s[rt][h][3]);
+          }
+        });
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float top = -__builtin_huge_valf();
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float x = s[rt][e / 4][e % 4];
+            x = a.cap > 0.f ? cap * tanh_of<TS>(x * mul) : x * mul;
+            const int j = j0 + 16 * (e / 4) + 4 * (lane / 16) + e % 4;
+            if (a.slopes) x = fmaf(-slope[rt], (float)(see[rt] - 1 - j), x);
+            if (cut && !(j < see[rt] && j >= low[rt])) x = -__builtin_huge_valf();
+            s[rt][e / 4][e % 4] = x;
+            top = fmaxf(top, x);
+          }
+          top = max_quarters(top);
+          if (__any(top > m[rt] + 8.f)) {        // (as in the attention of token rows)
+            const float to = top > m[rt] + 8.f ? top : m[rt];
+            const float c = m[rt] == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(m[rt] - to);
+            m[rt] = to;
+            l[rt] *= c;
+#pragma unroll
+            for (int n2 = 0; n2 < W; ++n2)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[rt][n2][e] *= c;
+          }
+          const float ref = m[rt] == -__builtin_huge_valf() ? 0.f : m[rt];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x = __builtin_amdgcn_exp2f(s[rt][e / 4][e % 4] - ref);
+            s[rt][e / 4][e % 4] = x;
+            l[rt] += x;
+          }
+        }
+        unroll<G>([&](auto kk) {
+          constexpr int k = kk.value;
+          Frag<TS> x0, x1;
+          unpack_codes(raw.v[2 * k], x0);
+          unpack_codes(raw.v[2 * k + 1], x1);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float p[8];
+            unroll<2>([&](auto hh) {
+              constexpr int h = hh.value, W0 = (h * G + k) * 2;
+              p[4 * h] = row_lane<W0>(vl) * s[rt][h][0];
+              p[4 * h + 1] = row_lane<W0>(vh) * s[rt][h][1];
+              p[4 * h + 2] = row_lane<W0 + 1>(vl) * s[rt][h][2];
+              p[4 * h + 3] = row_lane<W0 + 1>(vh) * s[rt][h][3];
+            });
+            if (cut) {                           // what is not seen may have any scale, NaN too
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int j = j0 + 16 * (e / 4) + 4 * (lane / 16) + e % 4;
+                if (!(j < see[rt] && j >= low[rt])) p[e] = 0.f;
+              }
+            }
+            Frag<TS> pf;
+            pack_frag(p, pf);
+            o[rt][2 * k] = mfma16(x0, pf, o[rt][2 * k]);
+            o[rt][2 * k + 1] = mfma16(x1, pf, o[rt][2 * k + 1]);
+          }
+        });
+        raw = nextraw;
+      }
+    }
+
+    // the waves' sums of each 16 rows, added in order
+    const bool whole = from == 0 && upto == sq.blocks;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (from == 0 ? 1 : 0);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[rt]), __float_as_uint(l[rt]), false, false);
+      float ls = __uint_as_float(s16[0]) + __uint_as_float(s16[1]);
+      ls = swap32_add(ls);
+      __syncthreads();
+      if (lane < 16) mls[wave][lane] = make_float2(m[rt], ls);
+#pragma unroll
+      for (int n = 0; n < W; ++n)
+        *reinterpret_cast<f32x4*>(&sums[wave][r16][16 * n + 4 * (lane / 16)]) = o[rt][n];
+      __syncthreads();
+      for (int i = tid; i < 16 * (D / 8); i += 256) {
+        const int row = i / (D / 8), c = i % (D / 8) * 8;
+        const int64_t ri = (int64_t)tile * ROWS + rt * 16 + row, t = sq.first + ri / g, p = sq.len - (sq.after - t);
+        if (t >= sq.end || p < 0 || p >= (int64_t)a.per_seq * a.page) continue;
+        float top = mls[0][row].x;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, mls[w][row].x);
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+        const float ref = top == -__builtin_huge_valf() ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float2 ml = mls[w][row];
+          const float c2 = __builtin_amdgcn_exp2f(ml.x - ref);
+          sum = fmaf(c2, ml.y, sum);
+          float y[8];
+          Vec8<float>::load(&sums[w][row][c], y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = fmaf(c2, y[e], x[e]);
+        }
+        if (whole) {
+          const float inv = top == -__builtin_huge_valf() && sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= inv;
+          Vec8<TS>::store(static_cast<TS*>(a.k) + (t * a.Hq + head * g + ri % g) * D + c, x);
+        } else {
+          const int64_t to = slot * ROWS + rt * 16 + row;
+          Vec8<float>::store(a.part + to * D + c, x);
+          if (c == 0) a.ml[to] = make_float2(top, sum);
+        }
+      }
+    }
+    u = last;
+  }
+}
+
+// A row of the output from the places of its segment's runs, where there are
+// several.
+template <typename TS, int D>
+__global__ __launch_bounds__(256) void k_cache_join(CacheArgs a, int ROWS, int64_t wgs) {
+  constexpr int P = D / 8;
+  const int lane = threadIdx.x % 64, g = a.Hq / a.Hkv;
+  const int64_t t = blockIdx.x;
+  const int b = sequence_of(a.starts, a.B, t, lane);
+  if (b < 0 || t >= a.starts[b + 1]) return;
+  const int64_t first = a.starts[b] > 0 ? a.starts[b] : 0;
+  const int64_t p = a.lens[b] - (a.starts[b + 1] - t);
+  if (p < 0 || p >= (int64_t)a.per_seq * a.page) return;
+  const int64_t before = a.where[2 * b], blocks = a.where[2 * b + 1], run = a.where[2 * (int64_t)a.B];
+  for (int u = threadIdx.x; u < a.Hq * P; u += 256) {
+    const int qh = u / P, c = u % P * 8;
+    const int64_t row = (t - first) * g + qh % g, tile = row / ROWS;
+    const int64_t seg0 = before + (tile * a.Hkv + qh / g) * blocks;
+    const int64_t w0 = seg0 / run, w1 = (seg0 + blocks - 1) / run;
+    if (w0 == w1 || w1 >= wgs) continue;         // (>=: only where starts do not ascend)
+    auto place = [&](int64_t w) { return (2 * w + (w == w0 ? 1 : 0)) * ROWS + row % ROWS; };
+    float top = -__builtin_huge_valf();
+    for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, a.ml[place(w)].x);
+    const float ref = top == -__builtin_huge_valf() ? 0.f : top;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+    for (int64_t w = w0; w <= w1; ++w) {
+      const float2 ml = a.ml[place(w)];
+      const float c2 = __builtin_amdgcn_exp2f(ml.x - ref);
+      sum = fmaf(c2, ml.y, sum);
+      float y[8];
+      Vec8<float>::load(a.part + place(w) * D + c, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = fmaf(c2, y[e], x[e]);
+    }
+    const float inv = top == -__builtin_huge_valf() && sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    Vec8<TS>::store(static_cast<TS*>(a.k) + (t * a.Hq + qh) * D + c, x);
+  }
+}
+
+CacheArgs args_of(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const int32_t* starts,
+                  const int32_t* lens, const int32_t* pages, const void* pool) {
+  CacheArgs a{};
+  a.starts = starts, a.lens = lens, a.pages = pages;
+  a.pool = static_cast<unsigned char*>(const_cast<void*>(pool));
+  a.T = d->T;
+  a.Hq = h->Hq, a.Hkv = h->Hkv, a.R = h->R, a.pairs = h->pairs, a.window = h->window;
+  a.page = c->page, a.npages = c->npages, a.B = c->B, a.per_seq = c->per_seq;
+  a.scale = h->scale, a.cap = h->cap;
+  return a;
+}
+
+template <class F> void with_width(int D, F&& f) {
+  switch (D) {
+    case 32: return f(Int<32>{});
+    case 64: return f(Int<64>{});
+    case 96: return f(Int<96>{});
+    default: return f(Int<128>{});
+  }
+}
+
+// rows of a tile: 32 where the sequences have more than 16 on average
+int tile_rows(int64_t T, int B, int g) { return T * g > 16 * (int64_t)B ? 32 : 16; }
+
+// Workgroups: what the chip holds at a time, or one for each four blocks there can be.
+int64_t attend_grid(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c) {
+  const int rows = tile_rows(d->T, c->B, h->Hq / h->Hkv);
+  const int64_t tiles = d->T * (h->Hq / h->Hkv) / rows + (c->B < d->T ? c->B : d->T);
+  const int64_t blocks = (int64_t)c->per_seq * c->page / kBlock;
+  const int64_t full = 256 * attend_wgs(d->state_dtype == XHC_F32, rows);
+  const int64_t units = tiles * h->Hkv;
+  if (units >= 4 * full || blocks >= 4 * full) return full;
+  const int64_t need = (units * blocks + 3) / 4;
+  return need < full ? need : full;
+}
+
+constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t cache_bytes(const xhc_heads* h, const xhc_cache* c) {
+  return (size_t)c->npages * h->Hkv * (c->page / kBlock) * (36 * h->D);
+}
+
+size_t cache_attend_ws_bytes(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c) {
+  const size_t slots = 2 * (size_t)attend_grid(d, h, c) * tile_rows(d->T, c->B, h->Hq / h->Hkv);
+  return up(slots * h->D * 4) + up(slots * 8) + up((2 * (size_t)c->B + 1) * 8);
+}
+
+hipError_t launch_cache_append(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* qkv,
+                               const float* table, const int32_t* starts, const int32_t* lens, const int32_t* pages,
+                               void* pool, void* q, hipStream_t s) {
+  CacheArgs a = args_of(d, h, c, starts, lens, pages, pool);
+  a.qkv = qkv, a.table = table, a.q = q;
+  const int64_t mean = d->T / c->B, per = h->Hq * (h->D / 8);
+  a.rows = (int)(mean < 1 ? 1 : mean > kBlock ? kBlock : mean);
+  while ((d->T + a.rows - 1) / a.rows * h->Hkv > (1 << 22)) a.rows *= 2;   // (a launch's threads stay below 2^32)
+  a.tokens = per >= 256 ? 1 : (int)(256 / per);
+  a.qblocks = q ? (unsigned)((d->T + a.tokens - 1) / a.tokens) : 0;
+  const dim3 grid((unsigned)(a.qblocks + (d->T + a.rows - 1) / a.rows * h->Hkv)), block(256);
+  with_width(h->D, [&](auto D) {
+    if (d->state_dtype == XHC_BF16)
+      k_cache_append<uint16_t, D.value><<<grid, block, 0, s>>>(a);
+    else
+      k_cache_append<float, D.value><<<grid, block, 0, s>>>(a);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const int32_t* starts,
+                             const int32_t* lens, const int32_t* pages, const void* pool, void* k, void* v,
+                             hipStream_t s) {
+  CacheArgs a = args_of(d, h, c, starts, lens, pages, pool);
+  a.k = k, a.v = v;
+  const dim3 grid((unsigned)d->T), block(256);
+  with_width(h->D, [&](auto D) {
+    if (d->state_dtype == XHC_BF16)
+      k_cache_read<uint16_t, D.value><<<grid, block, 0, s>>>(a);
+    else
+      k_cache_read<float, D.value><<<grid, block, 0, s>>>(a);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_attend(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* q,
+                               const float* slopes, const int32_t* starts, const int32_t* lens, const int32_t* pages,
+                               const void* pool, void* out, void* ws, hipStream_t s) {
+  CacheArgs a = args_of(d, h, c, starts, lens, pages, pool);
+  a.q = const_cast<void*>(q), a.k = out, a.slopes = slopes;
+  const int rows = tile_rows(d->T, c->B, h->Hq / h->Hkv);
+  const int64_t wgs = attend_grid(d, h, c);
+  const size_t slots = 2 * (size_t)wgs * rows;
+  char* p = static_cast<char*>(ws);
+  a.part = reinterpret_cast<float*>(p);
+  a.ml = reinterpret_cast<float2*>(p + up(slots * h->D * 4));
+  a.where = reinterpret_cast<int64_t*>(p + up(slots * h->D * 4) + up(slots * 8));
+  const dim3 grid((unsigned)wgs), block(256), tokens((unsigned)d->T);
+  with_width(h->D, [&](auto D) {
+    if (d->state_dtype == XHC_BF16) {
+      if (rows == 16)
+        k_cache_attend<uint16_t, D.value, 1><<<grid, block, 0, s>>>(a);
+      else
+        k_cache_attend<uint16_t, D.value, 2><<<grid, block, 0, s>>>(a);
+      k_cache_join<uint16_t, D.value><<<tokens, block, 0, s>>>(a, rows, wgs);
+    } else {
+      if (rows == 16)
+        k_cache_attend<float, D.value, 1><<<grid, block, 0, s>>>(a);
+      else
+        k_cache_attend<float, D.value, 2><<<grid, block, 0, s>>>(a);
+      k_cache_join<float, D.value><<<tokens, block, 0, s>>>(a, rows, wgs);
+    }
+  });
+  return hipGetLastError();
+}
+
+}  // namespace xhc

@@ -323,6 +323,35 @@ size_t grad_ws_bytes(int n);
 hipError_t launch_grad_clip(int n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
                             float max_norm, void* const* outs, float* norm, void* ws, hipStream_t s);
 
+// ---- an attention-type sublayer's own function: rotation, attention, paged cache
+constexpr int64_t kMaxAttnT = (int64_t)1 << 23;      // tokens, and heads of all of them: a launch's threads stay
+constexpr int64_t kMaxAttnHeads = (int64_t)1 << 29;  // below 2^32
+constexpr int kMaxHeads = 1024;                      // of a token
+hipError_t launch_rotate(const xhc_dims* d, const xhc_heads* h, const void* src, const int32_t* pos,
+                         const float* table, int64_t positions, bool inverse, void* dst, hipStream_t s);
+hipError_t launch_attn_spans(int64_t T, int64_t S, int window, int n, const int32_t* starts, const int32_t* prefix,
+                             int32_t* span, hipStream_t s);
+hipError_t launch_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
+                       const float* slopes, void* out, float* lse, hipStream_t s);
+size_t attn_bwd_ws_bytes(int64_t T, int Hq, int Hkv, int D);
+hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
+                           const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                           void* ws, hipStream_t s);
+
+constexpr int64_t kMaxCached = (int64_t)1 << 24;     // tokens that a sequence's row of the page table has room for
+constexpr int kMaxSequences = 1 << 16;
+size_t cache_bytes(const xhc_heads* h, const xhc_cache* c);
+size_t cache_attend_ws_bytes(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c);
+hipError_t launch_cache_append(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* qkv,
+                               const float* table, const int32_t* starts, const int32_t* lens, const int32_t* pages,
+                               void* pool, void* q, hipStream_t s);
+hipError_t launch_cache_read(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const int32_t* starts,
+                             const int32_t* lens, const int32_t* pages, const void* pool, void* k, void* v,
+                             hipStream_t s);
+hipError_t launch_cache_attend(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const void* q,
+                               const float* slopes, const int32_t* starts, const int32_t* lens, const int32_t* pages,
+                               const void* pool, void* out, void* ws, hipStream_t s);
+
 // per-token values xhc_pre saves for the backward: [z_r (N) | z_pre (N) |
 // z_post, z_res (k*Kr + k*k) | mu | nu | nu_a | pad], z = normalised logits
 __host__ __device__ inline int saved_floats(int N, int k, int Kr) { return 2 * N + k * Kr + k * k + 4; }

@@ -32,6 +32,7 @@ XHC_BF16, XHC_F32 = 0, 1
 XHC_IMPL_AUTO, XHC_IMPL_MULTI, XHC_IMPL_FUSED = 0, 1, 2
 XHC_ROUTER_SIGMOID, XHC_ROUTER_SOFTMAX = 0, 1
 XHC_ACT_SILU, XHC_ACT_GELU = 0, 1
+XHC_PAIRS_HALVES, XHC_PAIRS_NEIGHBOURS = 0, 1
 (XHC_OP_PRE, XHC_OP_POST, XHC_OP_FLASH_PRE, XHC_OP_FLASH_POST, XHC_OP_POST_BWD, XHC_OP_PRE_BWD,
  XHC_OP_FLASH_POST_BWD, XHC_OP_FLASH_PRE_BWD) = range(8)
 
@@ -70,6 +71,28 @@ def make_dims(T, N, k, m, C, Kr=1, S=None, kappa=(4, 8, 12), sinkhorn_iters=20, 
     return d
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [
+        ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("R", ctypes.c_int32),
+        ("pairs", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+    ]
+
+
+def make_heads(Hq, Hkv, D, rotary=None, pairing="halves", window=0, scale=None, cap=0.0) -> Heads:
+    """Heads of an attention-type sublayer: rotary is the number of channels that are rotated (all of a head's unless
+    given), pairing "halves" or "neighbours", scale D^-1/2 unless given; window and cap 0 for none."""
+    if pairing not in ("halves", "neighbours"):
+        raise ValueError(f"pairing is 'halves' or 'neighbours', got {pairing!r}")
+    return Heads(Hq, Hkv, D, D if rotary is None else rotary,
+                 XHC_PAIRS_HALVES if pairing == "halves" else XHC_PAIRS_NEIGHBOURS, window,
+                 D ** -0.5 if scale is None else scale, cap)
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("page", ctypes.c_int32), ("npages", ctypes.c_int32), ("B", ctypes.c_int32),
+                ("per_seq", ctypes.c_int32)]
+
+
 def dims_for(w, **kw) -> Dims:
     """Dims of a synth.Workload."""
     kw.setdefault("router", getattr(w, "router", "sigmoid"))
@@ -81,6 +104,8 @@ def dims_for(w, **kw) -> Dims:
 _lib = None
 _P = ctypes.c_void_p
 _D = ctypes.POINTER(Dims)
+_H = ctypes.POINTER(Heads)
+_C = ctypes.POINTER(Cache)
 _SIGS = {
     "xhc_packed_full_bytes": (ctypes.c_size_t, [_D, ctypes.c_int32]),
     "xhc_packed_active_bytes": (ctypes.c_size_t, [_D, ctypes.c_int32, ctypes.c_int32]),
@@ -109,6 +134,16 @@ _SIGS = {
     "xhc_pack_ffn": (ctypes.c_int, [_D, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P, _P]),
     "xhc_ffn": (ctypes.c_int, [_D, ctypes.c_int32, ctypes.c_int32] + [_P] * 5 + [ctypes.c_size_t, _P]),
     "xhc_ffn_bwd": (ctypes.c_int, [_D, ctypes.c_int32, ctypes.c_int32] + [_P] * 9 + [ctypes.c_size_t, _P]),
+    "xhc_rotate": (ctypes.c_int, [_D, _H] + [_P] * 3 + [ctypes.c_int64, ctypes.c_int32, _P, _P]),
+    "xhc_attn_spans": (ctypes.c_int, [_D, _H, ctypes.c_int32] + [_P] * 4),
+    "xhc_attn": (ctypes.c_int, [_D, _H] + [_P] * 6),
+    "xhc_attn_workspace_bytes": (ctypes.c_size_t, [_D, _H]),
+    "xhc_attn_bwd": (ctypes.c_int, [_D, _H] + [_P] * 8 + [ctypes.c_size_t, _P]),
+    "xhc_cache_bytes": (ctypes.c_size_t, [_H, _C]),
+    "xhc_attn_cache_workspace_bytes": (ctypes.c_size_t, [_D, _H, _C]),
+    "xhc_cache_append": (ctypes.c_int, [_D, _H, _C, _P, _P, ctypes.c_int64] + [_P] * 6),
+    "xhc_cache_read": (ctypes.c_int, [_D, _H, _C] + [_P] * 7),
+    "xhc_attn_cache": (ctypes.c_int, [_D, _H, _C] + [_P] * 8 + [ctypes.c_size_t, _P]),
     "xhc_grad_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32]),
     "xhc_grad_norm": (ctypes.c_int, [ctypes.c_int32] + [_P] * 5 + [ctypes.c_size_t, _P]),
     "xhc_grad_clip": (ctypes.c_int, [ctypes.c_int32] + [_P] * 3 + [ctypes.c_float] + [_P] * 3 + [ctypes.c_size_t, _P]),
@@ -328,6 +363,53 @@ def xhc_ffn(d, H, act, input, packed, F, saved, workspace, stream=None):
 def xhc_ffn_bwd(d, H, act, input, packed, saved, dF, d_input, dW_gate, dW_up, dW_down, workspace, stream=None):
     _call("xhc_ffn_bwd", ctypes.byref(d), H, act, _ptr(input), _ptr(packed), _ptr(saved), _ptr(dF), _ptr(d_input),
           _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def xhc_rotate(d, h, in_, pos, table, positions, inverse, out, stream=None):
+    _call("xhc_rotate", ctypes.byref(d), ctypes.byref(h), _ptr(in_), _ptr(pos), _ptr(table), positions,
+          int(bool(inverse)), _ptr(out), _stream(stream))
+
+
+def xhc_attn_spans(d, h, n, starts, prefix, span, stream=None):
+    _call("xhc_attn_spans", ctypes.byref(d), ctypes.byref(h), n, _ptr(starts), _ptr(prefix), _ptr(span),
+          _stream(stream))
+
+
+def xhc_attn(d, h, qkv, span, slopes, out, lse, stream=None):
+    _call("xhc_attn", ctypes.byref(d), ctypes.byref(h), _ptr(qkv), _ptr(span), _ptr(slopes), _ptr(out), _ptr(lse),
+          _stream(stream))
+
+
+def xhc_attn_workspace_bytes(d, h):
+    return lib().xhc_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(h))
+
+
+def xhc_attn_bwd(d, h, qkv, span, slopes, out, lse, dout, dqkv, workspace, stream=None):
+    _call("xhc_attn_bwd", ctypes.byref(d), ctypes.byref(h), _ptr(qkv), _ptr(span), _ptr(slopes), _ptr(out), _ptr(lse),
+          _ptr(dout), _ptr(dqkv), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def xhc_cache_bytes(h, c):
+    return lib().xhc_cache_bytes(ctypes.byref(h), ctypes.byref(c))
+
+
+def xhc_attn_cache_workspace_bytes(d, h, c):
+    return lib().xhc_attn_cache_workspace_bytes(ctypes.byref(d), ctypes.byref(h), ctypes.byref(c))
+
+
+def xhc_cache_append(d, h, c, qkv, table, positions, starts, lens, pages, pool, q, stream=None):
+    _call("xhc_cache_append", ctypes.byref(d), ctypes.byref(h), ctypes.byref(c), _ptr(qkv), _ptr(table), positions,
+          _ptr(starts), _ptr(lens), _ptr(pages), _ptr(pool), _ptr(q), _stream(stream))
+
+
+def xhc_cache_read(d, h, c, starts, lens, pages, pool, k, v, stream=None):
+    _call("xhc_cache_read", ctypes.byref(d), ctypes.byref(h), ctypes.byref(c), _ptr(starts), _ptr(lens), _ptr(pages),
+          _ptr(pool), _ptr(k), _ptr(v), _stream(stream))
+
+
+def xhc_attn_cache(d, h, c, q, slopes, starts, lens, pages, pool, out, workspace, stream=None):
+    _call("xhc_attn_cache", ctypes.byref(d), ctypes.byref(h), ctypes.byref(c), _ptr(q), _ptr(slopes), _ptr(starts),
+          _ptr(lens), _ptr(pages), _ptr(pool), _ptr(out), _ptr(workspace), _nbytes(workspace), _stream(stream))
 
 
 _GRAD_DTYPES = {torch.bfloat16: XHC_BF16, torch.float32: XHC_F32}
@@ -854,6 +936,197 @@ class TrainableFeedForward(FeedForward):
         xhc_ffn_bwd(self.d, self.H, self.act, self.x, self.packed, self.saved, dF, self.d_input, g["W_gate"],
                     g["W_up"], g["W_down"], self.ws_bwd, stream)
         return self.d_input
+
+
+def rotation_table(positions, R, base=10000.0, device="cuda"):
+    """Cosines and sines [positions, R / 2, 2] of the angles p base^(-2 i / R), formed in 64 bits (the angles of far
+    positions need them) and rounded to fp32.  A table of other frequencies is as good."""
+    f = base ** (-2.0 * torch.arange(R // 2, dtype=torch.float64, device=device) / max(R, 1))
+    a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * f
+    return torch.stack([torch.cos(a), torch.sin(a)], -1).float()
+
+
+def _table(h, table, device):
+    if h.R == 0:
+        return None, 0
+    _expect(table, torch.float32, (table.shape[0], h.R // 2, 2), "table")
+    return table.to(device).contiguous(), table.shape[0]
+
+
+def _slopes(h, slopes, device):
+    if slopes is None:
+        return None
+    _expect(slopes, torch.float32, (h.Hq,), "slopes")
+    return slopes.to(device).contiguous()
+
+
+def _expect_ints(t, shape, dev, name):
+    if t is not None:
+        _expect(t, torch.int32, shape, name)
+        _on(t, dev, name)
+
+
+class Rotation:
+    """Position rotation of the query and key heads of qkv [T, Hq + 2 Hkv, D] by a table of cosines and sines
+    (rotation_table).  Positions are t % d.S unless given (pos [T] int32).  Forward and backward each have a buffer
+    of this object for their output, overwritten by their next call; with ``out``, which may be the input itself, it
+    goes there."""
+
+    def __init__(self, d: Dims, h: Heads, table, device="cuda"):
+        self.d, self.h, self.device = d, h, _here(device)
+        self.table, self.positions = _table(h, table, self.device)
+        self.buffers = [None, None]    # of forward, of backward
+
+    def _run(self, x, pos, out, inverse, stream):
+        shape = (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D)
+        _expect(x, _state_dtype(self.d), shape, "the heads")
+        _on(x, self.device, "the heads")
+        _expect_ints(pos, (self.d.T,), self.device, "pos")
+        if out is None:
+            if self.buffers[inverse] is None:
+                with _within(stream):
+                    self.buffers[inverse] = torch.empty(shape, dtype=x.dtype, device=self.device)
+            out = self.buffers[inverse]
+        else:
+            _expect(out, x.dtype, shape, "out")
+            _on(out, self.device, "out")
+        xhc_rotate(self.d, self.h, x, pos, self.table, self.positions, inverse, out, stream)
+        return out
+
+    def forward(self, qkv, pos=None, out=None, stream=None):
+        return self._run(qkv, pos, out, 0, stream)
+
+    def backward(self, dqkv, pos=None, out=None, stream=None):
+        """The gradient of forward's input, given that of its output."""
+        return self._run(dqkv, pos, out, 1, stream)
+
+
+class Attention:
+    """Attention of qkv [T, Hq + 2 Hkv, D]: forward(qkv, span) returns [T, Hq, D].  Without a span a token sees the
+    tokens of its sequence (d.S) up to itself; spans() gives those of packed documents, also with prefixes that see
+    themselves both ways.  slopes [Hq] fp32: of a bias -slope |i - j|.  Outputs go to buffers of this object,
+    overwritten by its next call."""
+
+    def __init__(self, d: Dims, h: Heads, slopes=None, device="cuda"):
+        self.d, self.h, self.device = d, h, _here(device)
+        self.slopes = _slopes(h, slopes, self.device)
+        self.out = torch.empty(d.T, h.Hq, h.D, dtype=_state_dtype(d), device=self.device)
+        self.lse = None
+        self.span = None
+
+    def spans(self, starts=None, prefix=None, stream=None):
+        """span [T, 2] of documents: document i has the tokens starts[i] .. starts[i + 1] - 1 (int32 [n + 1]), its
+        first prefix[i] (int32 [n]) seen by all of it; without starts, of sequences."""
+        n = 0 if starts is None else starts.numel() - 1
+        if starts is not None:
+            if n < 0:
+                raise ValueError("starts holds one entry more than there are documents")
+            _expect_ints(starts, (n + 1,), self.device, "starts")
+        _expect_ints(prefix, (n,), self.device, "prefix")
+        _enqueues(self.device)
+        if self.span is None:
+            with _within(stream):
+                self.span = torch.empty(self.d.T, 2, dtype=torch.int32, device=self.device)
+        xhc_attn_spans(self.d, self.h, n, starts, prefix, self.span, stream)
+        return self.span
+
+    def forward(self, qkv, span=None, stream=None):
+        _expect(qkv, self.out.dtype, (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D), "qkv")
+        _on(qkv, self.device, "qkv")
+        _expect_ints(span, (self.d.T, 2), self.device, "span")
+        xhc_attn(self.d, self.h, qkv, span, self.slopes, self.out, self.lse, stream)
+        return self.out
+
+
+class TrainableAttention(Attention):
+    """An Attention that keeps what the backward needs and runs it: backward(dout) returns dL/dqkv of the last
+    forward's qkv and span (read again: they must still hold their values)."""
+
+    def __init__(self, d: Dims, h: Heads, slopes=None, device="cuda"):
+        super().__init__(d, h, slopes, device)
+        self.lse = torch.empty(d.T, h.Hq, dtype=torch.float32, device=self.device)
+        self.dqkv = torch.empty(d.T, h.Hq + 2 * h.Hkv, h.D, dtype=self.out.dtype, device=self.device)
+        self.ws = _bytes(xhc_attn_workspace_bytes(d, h), self.device)
+        self.seen = None
+
+    def forward(self, qkv, span=None, stream=None):
+        out = super().forward(qkv, span, stream)
+        self.seen = (qkv, span)        # (of a forward that ran: a refused one changes nothing)
+        return out
+
+    def backward(self, dout, stream=None):
+        if self.seen is None:
+            raise ValueError("backward without a forward")
+        _expect(dout, self.out.dtype, self.out.shape, "dout")
+        _on(dout, self.device, "dout")
+        qkv, span = self.seen
+        xhc_attn_bwd(self.d, self.h, qkv, span, self.slopes, self.out, self.lse, dout, self.dqkv, self.ws, stream)
+        return self.dqkv
+
+
+class KVCache:
+    """Paged cache of a layer's keys and values in 4 bits, for calls of d.T tokens.  ``sequences`` rows of a page table
+    of ``per_sequence`` entries name pages of a pool of ``npages``, ``page`` tokens each; an entry that is no page
+    (-1) is one that is not there.  Each call takes starts [sequences + 1], lens [sequences] and pages [sequences,
+    per_sequence], int32 on the device: sequence b's newest tokens are starts[b] .. starts[b + 1] - 1 of the call's,
+    the last of its lens[b].  ``pool``: that of another KVCache with the same heads, page and npages, for calls of
+    another number of tokens.  Outputs go to buffers of this object, overwritten by its next call."""
+
+    def __init__(self, d: Dims, h: Heads, table, sequences, per_sequence, page=64, npages=None, slopes=None,
+                 pool=None, device="cuda"):
+        self.d, self.h, self.device = d, h, _here(device)
+        self.c = Cache(page, sequences * per_sequence if npages is None else npages, sequences, per_sequence)
+        self.table, self.positions = _table(h, table, self.device)
+        self.slopes = _slopes(h, slopes, self.device)
+        n = xhc_cache_bytes(h, self.c)
+        if n == 0:
+            raise ValueError("a cache of these sizes is not supported")
+        if pool is None:
+            pool = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        _expect(pool, torch.uint8, (n,), "pool")
+        _on(pool, self.device, "pool")
+        self.pool = pool
+        sdt = _state_dtype(d)
+        self.q = torch.empty(d.T, h.Hq, h.D, dtype=sdt, device=self.device)
+        self.out = torch.empty_like(self.q)
+        self.k = self.v = None
+        self.ws = _bytes(xhc_attn_cache_workspace_bytes(d, h, self.c), self.device)
+
+    def _check(self, starts, lens, pages):
+        c = self.c
+        _expect_ints(starts, (c.B + 1,), self.device, "starts")
+        _expect_ints(lens, (c.B,), self.device, "lens")
+        _expect_ints(pages, (c.B, c.per_seq), self.device, "pages")
+        _enqueues(self.device)
+
+    def append(self, qkv, starts, lens, pages, stream=None):
+        """Stores the rotated key heads and the value heads of qkv [T, Hq + 2 Hkv, D]; returns the rotated query heads
+        [T, Hq, D]."""
+        _expect(qkv, self.q.dtype, (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D), "qkv")
+        _on(qkv, self.device, "qkv")
+        self._check(starts, lens, pages)
+        xhc_cache_append(self.d, self.h, self.c, qkv, self.table, self.positions, starts, lens, pages, self.pool,
+                         self.q, stream)
+        return self.q
+
+    def read(self, starts, lens, pages, stream=None):
+        """The keys and values [T, Hkv, D] held for the call's tokens (zeros until a token's have been read)."""
+        self._check(starts, lens, pages)
+        if self.k is None:
+            with _within(stream):
+                self.k, self.v = (torch.zeros(self.d.T, self.h.Hkv, self.h.D, dtype=self.q.dtype, device=self.device)
+                                  for _ in range(2))
+        xhc_cache_read(self.d, self.h, self.c, starts, lens, pages, self.pool, self.k, self.v, stream)
+        return self.k, self.v
+
+    def attend(self, q, starts, lens, pages, stream=None):
+        """Attention of q [T, Hq, D], the call's tokens (appended before), over their sequences up to themselves."""
+        _expect(q, self.q.dtype, self.q.shape, "q")
+        _on(q, self.device, "q")
+        self._check(starts, lens, pages)
+        xhc_attn_cache(self.d, self.h, self.c, q, self.slopes, starts, lens, pages, self.pool, self.out, self.ws,
+                       stream)
+        return self.out
 
 
 def grad_tensors(grads):

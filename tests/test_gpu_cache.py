@@ -1,0 +1,215 @@
+"""The paged 4-bit cache on the GPU: what it holds to the bit, attention over it
+against the formulas in 64 bits within bounds that count the roundings."""
+
+import pytest
+import torch
+
+from paper_2607_14530_amd import xhc as X
+from tests import attn_util as U
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+NAME = {BF: "bf16", F32: "f32"}
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Model:
+    """A cache and what it has to hold: k, v [sequence][position] in 64 bits, NaN where nothing is stored."""
+
+    def __init__(self, B, per_seq, page, Hq, Hkv, D, dtype, R=None, pairs="halves", seed=0, missing=(), **heads):
+        self.h = X.make_heads(Hq, Hkv, D, rotary=R, pairing=pairs, **heads)
+        self.B, self.per_seq, self.page, self.dtype = B, per_seq, page, dtype
+        self.R, self.pairs = self.h.R, pairs
+        self.g = torch.Generator().manual_seed(seed)
+        n = B * per_seq + 2
+        order = torch.randperm(n, generator=self.g)[:B * per_seq].view(B, per_seq)
+        for b, j, what in missing:
+            order[b, j] = what
+        self.pages, self.npages = order, n
+        self.table = X.rotation_table(per_seq * page + 1, self.R)
+        self.lens = [0] * B
+        self.k, self.v = (torch.full((B, per_seq * page, Hkv, D), float("nan"), dtype=U.F64) for _ in range(2))
+        self.pool = None
+
+    def there(self, b, p):
+        return 0 <= p < self.per_seq * self.page and 0 <= int(self.pages[b, p // self.page]) < self.npages
+
+    def bundle(self, T, slopes=None):
+        d = X.make_dims(T, 1, 1, 1, 32, S=1, state=NAME[self.dtype])
+        c = X.KVCache(d, self.h, self.table, self.B, self.per_seq, page=self.page, npages=self.npages, slopes=slopes,
+                      pool=self.pool)
+        if self.pool is None:
+            c.pool.fill_(255)                    # what is not stored: codes of -6 and scales of NaN
+            self.pool = c.pool
+        return c
+
+    def append(self, new, front=0, back=0, lens=None):
+        """new[b] tokens to each sequence; front, back: tokens of none."""
+        h = self.h
+        T = front + sum(new) + back
+        qkv = torch.randn(T, h.Hq + 2 * h.Hkv, h.D, generator=self.g).to(self.dtype)
+        starts = [front]
+        for n in new:
+            starts.append(starts[-1] + n)
+        self.lens = [a + b for a, b in zip(self.lens, new)] if lens is None else list(lens)
+        where = [(b, self.lens[b] - new[b] + i) for b in range(self.B) for i in range(new[b])]
+        c = self.bundle(T)
+        args = (i32(starts), i32(self.lens), self.pages.int().cuda())
+        c.q.fill_(7.0)
+        q = c.append(qkv.cuda(), *args)
+        cap = self.per_seq * self.page
+        at = torch.zeros(T, dtype=torch.long)
+        for i, (b, p) in enumerate(where):
+            at[front + i] = p if 0 <= p < cap else 0
+        cs = self.table.cpu()[at]
+        turned = U.rotated(qkv[:, :h.Hq + h.Hkv], cs, self.R, self.pairs)
+        ref_q = torch.full((T, h.Hq, h.D), 7.0, dtype=self.dtype)
+        ref_k, ref_v = (torch.zeros(T, h.Hkv, h.D, dtype=self.dtype) for _ in range(2))
+        hk, hv = U.held(turned[:, h.Hq:]), U.held(qkv[:, h.Hq + h.Hkv:])
+        for i, (b, p) in enumerate(where):
+            t = front + i
+            if 0 <= p < cap:
+                ref_q[t] = turned[t, :h.Hq].to(self.dtype)
+            if self.there(b, p):
+                self.k[b, p], self.v[b, p] = hk[t], hv[t]
+                ref_k[t], ref_v[t] = hk[t].to(self.dtype), hv[t].to(self.dtype)
+        assert torch.equal(q.cpu(), ref_q)
+        k, v = c.read(*args)
+        assert torch.equal(k.cpu(), ref_k) and torch.equal(v.cpu(), ref_v)
+        return args
+
+    def attend(self, new, slopes=None, front=0, back=0, q_scale=1.0):
+        """The newest new[b] tokens of each sequence."""
+        h = self.h
+        T = front + sum(new) + back
+        q = (torch.randn(T, h.Hq, h.D, generator=self.g) * q_scale).to(self.dtype)
+        starts = [front]
+        for n in new:
+            starts.append(starts[-1] + n)
+        sl = None if slopes is None else torch.tensor(slopes, dtype=F32, device="cuda")
+        c = self.bundle(T, sl)
+        c.out.fill_(7.0)
+        c.ws.fill_(255)
+        out = c.attend(q.cuda(), i32(starts), i32(self.lens), self.pages.int().cuda())
+        half = U.HALF[self.dtype]
+        ref, bound = torch.full((T, h.Hq, h.D), 7.0, dtype=U.F64), torch.zeros(T, h.Hq, h.D, dtype=U.F64)
+        for b in range(self.B):
+            n, L = new[b], min(self.lens[b], self.per_seq * self.page)
+            if n == 0 or L <= 0:
+                continue
+            pos = torch.arange(self.lens[b] - n, self.lens[b])
+            j = torch.arange(max(L, 0))
+            seen = (j[None] <= pos[:, None]) & torch.tensor([self.there(b, int(p)) for p in j], dtype=torch.bool)[None]
+            if h.window:
+                seen &= j[None] > pos[:, None] - h.window
+            rows = (pos >= 0) & (pos < self.per_seq * self.page)
+            dist = (pos[:, None] - j[None]).abs().to(U.F64)
+            t = slice(starts[b], starts[b] + n)
+            for hq in range(h.Hq):
+                kh = hq // (h.Hq // h.Hkv)
+                k, v = (torch.nan_to_num(z[b, :max(L, 0), kh]) for z in (self.k, self.v))
+                r, e = U.attention(q[t, hq].to(U.F64), k, v, seen, h.scale, h.cap,
+                                   0.0 if slopes is None else slopes[hq], dist, half if half > U.U else 0.0)["out"]
+                e = e + (8 * U.U if half == U.U else 0) * r.abs()
+                ref[t, hq] = torch.where(rows[:, None], r, ref[t, hq])
+                bound[t, hq] = torch.where(rows[:, None], e, bound[t, hq])
+        U.assert_within(out, (ref, bound), "out")
+        return out
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+@pytest.mark.parametrize("page,pairs", [(32, "halves"), (96, "neighbours")])
+def test_steps(D, page, pairs, dtype):
+    """Prompts of unlike lengths, then tokens one and several at a time across the borders of blocks and pages."""
+    m = Model(4, 200 // page + 1, page, 6, 2, D, dtype, pairs=pairs, seed=D + page)
+    m.append([1, 31, 100, 0])
+    m.attend([1, 31, 100, 0])
+    for new in ([1, 1, 1, 1], [1, 1, 1, 1], [5, 0, 31, 64], [1, 0, 0, 0], [2, 3, 4, 1]):
+        m.append(new)
+        m.attend(new)
+    m.attend([1, 1, 1, 1])                       # of tokens that were appended in other calls
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (16, 1), (17, 1), (40, 2), (8, 8)])
+def test_heads(Hq, Hkv, dtype):
+    m = Model(3, 3, 64, Hq, Hkv, 64, dtype, R=32, seed=Hq)
+    m.append([130, 64, 7])
+    m.attend([1, 1, 1])
+    m.attend([3, 1, 7])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_cap_bias_window(dtype):
+    for kw, slopes in ((dict(window=1), None), (dict(window=40, cap=3.0), [0.1, 0.0, 1.0, 0.01]),
+                       (dict(scale=0.5), [0.3, 0.2, 0.1, 0.0])):
+        m = Model(2, 4, 64, 4, 2, 128, dtype, seed=3, **kw)
+        m.append([250, 100])
+        m.attend([1, 1], slopes, q_scale=2.0)
+        m.attend([40, 9], slopes)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_pages_that_are_not_there(dtype):
+    """-1, one past the last, and a whole sequence without pages: nothing is stored, nothing seen; zeros where nothing
+    is seen."""
+    m = Model(3, 4, 32, 4, 2, 64, dtype, seed=5,
+              missing=[(0, 0, -1), (0, 2, 1 << 30), (1, 0, -5), (1, 1, -1), (1, 2, 3 * 4 + 2), (1, 3, -2 ** 31)])
+    m.append([100, 50, 128])
+    out = m.attend([1, 1, 1])
+    assert bool((out[1] == 0).all())
+    m.attend([60, 50, 20])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_tokens_of_no_sequence_and_positions_past_the_ends(dtype):
+    m = Model(3, 2, 64, 4, 2, 64, dtype, seed=6)
+    m.append([20, 0, 70], front=3, back=5)
+    m.attend([2, 0, 70], front=1, back=40)
+    m.append([10, 3, 80])                        # the last goes past its 128 positions
+    m.attend([10, 3, 80])
+    m.append([4, 4, 4], lens=[2, 0, -1])         # and positions below 0
+    m.attend([4, 4, 4])
+
+
+def test_one_long_sequence_and_many_short():
+    m = Model(1, 64, 256, 8, 2, 128, BF, seed=8)
+    m.append([16000])
+    m.attend([1])
+    m.append([1])
+    m.attend([1])
+    m = Model(300, 1, 32, 2, 1, 32, BF, seed=9)
+    m.append([b % 32 for b in range(300)])
+    m.attend([min(1, b % 32) for b in range(300)])
+
+
+def test_held_values_at_the_borders():
+    """Ties between codes, groups of zeros, tiny, huge and not finite values, signs."""
+    D, T = 64, 8
+    x = torch.zeros(T, D)
+    mid = torch.tensor([0.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    x[0, :9], x[0, 9:18] = mid, -mid             # scale 1: every tie
+    x[1, 32:] = 2.0 ** -101
+    x[2, :] = 2.0 ** -100
+    x[3, :32], x[3, 32:] = 3.0e38, -1e-30
+    x[4, 3], x[4, 40] = float("inf"), float("nan")
+    x[5] = torch.linspace(-1, 1, D)
+    x[6, 0] = 1e-45
+    x[7, 5] = float("-inf")
+    h = X.make_heads(1, 1, D, rotary=0)
+    d = X.make_dims(T, 1, 1, 1, 32, S=1, state="f32")
+    c = X.KVCache(d, h, None, 1, 1, page=32)
+    qkv = torch.stack([torch.zeros(T, D), x, x], 1)
+    args = (i32([0, T]), i32([T]), i32([[0]]))
+    c.append(qkv.cuda(), *args)
+    k, v = c.read(*args)
+    ref = U.held(x)
+    for z in (k, v):
+        z = z.cpu()[:, 0].to(U.F64)
+        assert torch.equal(torch.isnan(z), torch.isnan(ref))
+        assert torch.equal(torch.nan_to_num(z), torch.nan_to_num(ref))
