@@ -518,22 +518,22 @@ xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, cons
  *   span    [T,2] int32 as above, or any (cut to 0 .. T), or NULL: causal within
  *           sequences of S tokens, with h->window
  *   slopes  [Hq] fp32 or NULL
- *   lse     [T,Hq] fp32 or NULL: base-2 logarithm of the sum of exp, as
- *           xhc_attn_bwd needs it
- * A token that sees nothing gets zeros, and an lse of -infinity.  Tokens that
- * are not seen do not matter, whatever they hold; where a token that is seen
+ *   saved   NULL, or xhc_attn_saved_bytes(d, h) bytes that receive the rows'
+ *           sums, and what rounding out has left, for xhc_attn_bwd
+ * A token that sees nothing gets zeros.  Tokens that are not seen do not matter, whatever they hold; where a token that is seen
  * holds infinities or NaN, all of a row that sees it may become NaN.
  * xhc_attn_bwd - dqkv [T, Hq + 2 Hkv, D] from qkv, span, slopes as in the
- *   forward, its out and lse, and dout [T,Hq,D]; slopes get no gradient.
+ *   forward, its out and saved, and dout [T,Hq,D]; slopes get no gradient.
  *   workspace: xhc_attn_workspace_bytes(d, h) bytes.
  * Sums and softmax are fp32, in an order that the sizes fix.  bf16 state:
  * probabilities and the gradients of scores are rounded to bf16 as operands of
  * the next product; fp32 state: products are those of fp32 values in full.     */
+size_t xhc_attn_saved_bytes(const xhc_dims* d, const xhc_heads* h);
 size_t xhc_attn_workspace_bytes(const xhc_dims* d, const xhc_heads* h);
 xhc_status xhc_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span, const float* slopes,
-                    void* out, float* lse, void* stream);
+                    void* out, void* saved, void* stream);
 xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
-                        const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                        const float* slopes, const void* out, const void* saved, const void* dout, void* dqkv,
                         void* workspace, size_t workspace_bytes, void* stream);
 
 /* Paged cache of a layer: a pool of npages pages of `page` tokens, of which

@@ -1211,21 +1211,25 @@ xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, cons
 }
 
 xhc_status xhc_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span, const float* slopes,
-                    void* out, float* lse, void* stream) {
+                    void* out, void* saved, void* stream) {
   xhc_status st = check_heads(d, h);
   if (st != XHC_OK) return st;
   if (d->T == 0) return XHC_OK;
   if (!qkv || !out) return XHC_EINVAL;
-  if (!aligned16(qkv) || !aligned16(out) || !aligned(span, 8) || !aligned(slopes, 4) || !aligned(lse, 4))
+  if (!aligned16(qkv) || !aligned16(out) || !aligned(span, 8) || !aligned(slopes, 4) || !aligned16(saved))
     return XHC_EUNSUPPORTED;
   if (!buffers_apart({{qkv, heads_bytes(d, h, h->Hq + 2 * h->Hkv), false}, {span, (size_t)d->T * 8, false},
                       {slopes, (size_t)h->Hq * 4, false}, {out, heads_bytes(d, h, h->Hq), true},
-                      {lse, (size_t)d->T * h->Hq * 4, true}}))
+                      {saved, attn_saved_bytes(d->state_dtype, d->T, h->Hq, h->D), true}}))
     return XHC_EINVAL;
   clear_stale_error();
   hipError_t e = hipSuccess;
-  XHC_STEP("attn", launch_attn(d, h, qkv, span, slopes, out, lse, reinterpret_cast<hipStream_t>(stream)));
+  XHC_STEP("attn", launch_attn(d, h, qkv, span, slopes, out, saved, reinterpret_cast<hipStream_t>(stream)));
   return hip_status(e);
+}
+
+size_t xhc_attn_saved_bytes(const xhc_dims* d, const xhc_heads* h) {
+  return check_heads(d, h) == XHC_OK ? attn_saved_bytes(d->state_dtype, d->T, h->Hq, h->D) : 0;
 }
 
 size_t xhc_attn_workspace_bytes(const xhc_dims* d, const xhc_heads* h) {
@@ -1233,25 +1237,26 @@ size_t xhc_attn_workspace_bytes(const xhc_dims* d, const xhc_heads* h) {
 }
 
 xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
-                        const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                        const float* slopes, const void* out, const void* saved, const void* dout, void* dqkv,
                         void* workspace, size_t workspace_bytes, void* stream) {
   xhc_status st = check_heads(d, h);
   if (st != XHC_OK) return st;
   if (d->T == 0) return XHC_OK;
-  if (!qkv || !out || !lse || !dout || !dqkv || !workspace) return XHC_EINVAL;
-  for (const void* p : {qkv, out, dout, (const void*)dqkv, (const void*)workspace})
+  if (!qkv || !out || !saved || !dout || !dqkv || !workspace) return XHC_EINVAL;
+  for (const void* p : {qkv, out, saved, dout, (const void*)dqkv, (const void*)workspace})
     if (!aligned16(p)) return XHC_EUNSUPPORTED;
-  if (!aligned(span, 8) || !aligned(slopes, 4) || !aligned(lse, 4)) return XHC_EUNSUPPORTED;
+  if (!aligned(span, 8) || !aligned(slopes, 4)) return XHC_EUNSUPPORTED;
   const size_t need = attn_bwd_ws_bytes(d->T, h->Hq, h->Hkv, h->D);
   if (workspace_bytes < need) return XHC_EWORKSPACE;
   const size_t all = heads_bytes(d, h, h->Hq + 2 * h->Hkv), rows = heads_bytes(d, h, h->Hq);
   if (!buffers_apart({{qkv, all, false}, {span, (size_t)d->T * 8, false}, {slopes, (size_t)h->Hq * 4, false},
-                      {out, rows, false}, {lse, (size_t)d->T * h->Hq * 4, false}, {dout, rows, false},
+                      {out, rows, false}, {saved, attn_saved_bytes(d->state_dtype, d->T, h->Hq, h->D), false},
+                      {dout, rows, false},
                       {dqkv, all, true}, {workspace, need, true}}))
     return XHC_EINVAL;
   clear_stale_error();
   hipError_t e = hipSuccess;
-  XHC_STEP("attn_bwd", launch_attn_bwd(d, h, qkv, span, slopes, out, lse, dout, dqkv, workspace,
+  XHC_STEP("attn_bwd", launch_attn_bwd(d, h, qkv, span, slopes, out, saved, dout, dqkv, workspace,
                                        reinterpret_cast<hipStream_t>(stream)));
   return hip_status(e);
 }

@@ -159,17 +159,24 @@ struct Tile {
   }
 };
 
+// The same lane, which the compiler does not know to be: what follows from it is
+// formed where it is used, and not kept in registers over a loop.
+__device__ __forceinline__ int again(int lane) {
+  asm volatile("" : "+v"(lane));
+  return lane & 63;
+}
+
 // What an attention call is about, as its kernels take it.
 struct AttnArgs {
   const void* qkv;          // [T][Hq + 2 Hkv][D]
   const int2* span;         // [T]: the first key that a token sees, and one behind the last; null: causal
   const float* slopes;      // [Hq] or null
   void* out;                // [T][Hq][D]
-  float* lse;               // [T][Hq] or null: base-2 logarithms of the rows' sums
+  float* lse;               // [Hq][Tp] or null: base-2 logarithms of the rows' sums
+  uint16_t* low;            // [T][Hq][D], bf16 state: what out's rounding left, where lse is not null
   const void* dout;
   void* dqkv;
-  const float* lsep;        // [Hq][Tp]: of a backward
-  const float* delta;       // [Hq][Tp]
+  const float* delta;       // [Hq][Tp]: of a backward
   const int* lo;            // [Tp], [Tp]: spans, cut to 0 .. T, 0 .. 0 for rows behind the last
   const int* hi;
   const int4* range;        // [Tp / kTile]: of a tile's rows that see keys, min lo, max hi; of all, max lo, min hi
@@ -193,6 +200,11 @@ __device__ __forceinline__ int2 span_of(const AttnArgs& a, int t) {
   return make_int2(lo, t + 1);
 }
 
+// a value that all lanes have, in a scalar register
+__device__ __forceinline__ float scalar(float x) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x)));
+}
+
 // Scores in units of log2 e (their softmax then takes exp2), in place of the
 // raw products of one block of 32 keys x 32 queries or queries x keys:
 // (cap tanh(scale x / cap) - slope |i - j|) log2 e; der: d score / d (scale x),
@@ -200,9 +212,9 @@ __device__ __forceinline__ int2 span_of(const AttnArgs& a, int t) {
 struct Score {
   float mul, cap, slope;    // mul: scale log2 e, or 2 log2 e scale / cap
   __device__ __forceinline__ void init(const AttnArgs& a, int head) {
-    cap = a.cap * kLog2e;
-    mul = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e;
-    slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    cap = scalar(a.cap * kLog2e);
+    mul = scalar(a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e);
+    slope = a.slopes ? scalar(a.slopes[head] * kLog2e) : 0.f;
   }
 };
 template <typename TS> __device__ __forceinline__ float tanh_of(float x);
@@ -250,9 +262,10 @@ __device__ __forceinline__ int4 attn_extremes(int2 s, bool row, int4* red, int w
 
 // Sums of one 32-channel block of 32 tokens (a lane: token lane % 32, channels
 // 8 i + 4 (lane / 32) + 0 .. 3) times m, to row p of the lane's token: the two
-// halves exchange fours of channels, so that each writes runs of eight.
+// halves exchange fours of channels, so that each writes runs of eight.  low:
+// null, or where what the rounding leaves goes.
 template <typename TS>
-__device__ __forceinline__ void store_sums(const f32x16& x, float m, TS* p, bool row, int lane) {
+__device__ __forceinline__ void store_sums(const f32x16& x, float m, TS* p, bool row, int lane, TS* low = nullptr) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     float f[8];
@@ -264,7 +277,17 @@ __device__ __forceinline__ void store_sums(const f32x16& x, float m, TS* p, bool
       f[4 + e] = __uint_as_float(r[1]);
     }
     // the lower half now has channels 16 i + 0 .. 7, the upper 16 i + 8 .. 15
-    if (row) Vec8<TS>::store(p + 16 * i + 8 * (lane / 32), f);
+    const int at = 16 * i + 8 * (lane / 32);
+    if (row) Vec8<TS>::store(p + at, f);
+    if (sizeof(TS) == 2 && row && low) {
+      float g[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] = f[e];
+      Vec8<TS>::round(g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] -= g[e];
+      Vec8<TS>::store(low + at, f);
+    }
   }
 }
 

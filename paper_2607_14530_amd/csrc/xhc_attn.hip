@@ -14,7 +14,7 @@ namespace {
 
 constexpr float kNoKey = -__builtin_huge_valf();
 
-template <typename TS, int D>
+template <typename TS, int D, bool EX>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn(AttnArgs a) {
   using TL = Tile<TS, D>;
   constexpr int KS = D / 16, F = D / 32;
@@ -54,38 +54,40 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       wait_vm<0>();
       lds_barrier();
       if (kt + 1 < end) {
-        TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, lane);
-        TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, lane);
+        const int ln = again(lane);
+        TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, ln);
+        TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, ln);
       }
       unsigned char *K = lds + off, *V = K + TL::kBytes;
       const int j0 = kt * kTile;
       const bool cut = j0 < ex.z || j0 + kTile > ex.w;      // some row does not see all of the tile
       uint64_t bad = 0;
-      if (cut) bad = TL::clean(V, bits, wave, lane);
-      f32x16 s[2];
+      if (cut) bad = TL::clean(V, bits, wave, again(lane));
+      f32x16 s[2] = {f32x16{}, f32x16{}};
+      {
+        const int ln = again(lane);
+        Frag<TS> k[2];
+        TL::row_frag(K, 0, 0, ln, k[0]);
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        s[rb] = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          Frag<TS> k;
-          TL::row_frag(K, rb, ks, lane, k);
-          s[rb] = mfma32(k, q[ks], s[rb]);
+        for (int i = 0; i < 2 * KS; ++i) {       // a fragment is read while the one before is multiplied
+          if (i + 1 < 2 * KS) TL::row_frag(K, (i + 1) / KS, (i + 1) % KS, ln, k[(i + 1) % 2]);
+          s[i / KS] = mfma32(k[i % 2], q[i % KS], s[i / KS]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       // a lane's keys: j0 + 32 rb + sum_row(r) + 4 (lane / 32)
-      if (a.cap > 0.f) {
+      if (EX && a.cap > 0.f) {
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[rb][r] = sc.cap * tanh_of<TS>(s[rb][r] * sc.mul);
-      } else {
+      } else if (EX) {
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[rb][r] *= sc.mul;
       }
-      if (a.slopes) {
+      if (EX && a.slopes) {
         const float d0 = (float)(t - j0 - 4 * (lane / 32));
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
@@ -108,6 +110,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[rb][r]);
       top = max_halves(top);
+      if (!EX) top *= sc.mul;                               // (s: still the raw products, mul > 0)
       // The row's reference only follows its maximum when that is 2^8 above it:
       // probabilities up to 256 are as exact, and sums are rarely rescaled.
       if (__any(top > m + 8.f)) {
@@ -125,29 +128,32 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[rb][r] = __builtin_amdgcn_exp2f(s[rb][r] - ref);
+          s[rb][r] = __builtin_amdgcn_exp2f(EX ? s[rb][r] - ref : fmaf(s[rb][r], sc.mul, -ref));
           l += s[rb][r];
         }
       if (bad) {
-        const int lo = see.x - j0, hi = see.y - j0;
+        const int lo = see.x - j0 - 4 * (lane / 32), hi = see.y - j0 - 4 * (lane / 32);
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
+        for (int rb = 0; rb < 2; ++rb) {
+          const uint32_t keys = (uint32_t)(bad >> (32 * rb)) >> (4 * (lane / 32));
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int j = 32 * rb + sum_row(r) + 4 * (lane / 32);
-            if (((bad >> j) & 1) && j >= lo && j < hi) s[rb][r] = __builtin_nanf("");
+            const int j = 32 * rb + sum_row(r);
+            if ((keys >> sum_row(r) & 1) && j >= lo && j < hi) s[rb][r] = __builtin_nanf("");
           }
-      }
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        Frag<TS> p;
-        sums_frag(s[st / 2], st % 2, p);
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-          Frag<TS> v;
-          TL::col_frag(V, f, st, lane, v);
-          o[f] = mfma32(v, p, o[f]);
         }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const int ln = again(lane);
+      Frag<TS> v[2], p;
+      TL::col_frag(V, 0, 0, ln, v[0]);
+#pragma unroll
+      for (int i = 0; i < 4 * F; ++i) {
+        const int st = i / F, f = i % F;
+        if (f == 0) sums_frag(s[st / 2], st % 2, p);
+        if (i + 1 < 4 * F) TL::col_frag(V, (i + 1) % F, (i + 1) / F, ln, v[(i + 1) % 2]);
+        o[f] = mfma32(v[i % 2], p, o[f]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -156,9 +162,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   const float inv = see.x < see.y ? 1.f / l : 0.f;
   TS* op = reinterpret_cast<TS*>(a.out) + ((int64_t)t * a.Hq + head) * D;
 #pragma unroll
-  for (int f = 0; f < F; ++f) store_sums<TS>(o[f], inv, op + 32 * f, row, lane);
+  for (int f = 0; f < F; ++f)
+    store_sums<TS>(o[f], inv, op + 32 * f, row, lane,
+                   a.low ? reinterpret_cast<TS*>(a.low) + ((int64_t)t * a.Hq + head) * D + 32 * f : nullptr);
   if (a.lse && row && lane < 32)
-    a.lse[(int64_t)t * a.Hq + head] = see.x < see.y ? m + __builtin_amdgcn_logf(l) : kNoKey;
+    a.lse[(int64_t)head * a.Tp + t] = see.x < see.y ? m + __builtin_amdgcn_logf(l) : kNoKey;
 }
 
 // The spans of documents, by one thread each token.  Document i holds the
@@ -239,7 +247,11 @@ __global__ __launch_bounds__(256) void k_rotate(int64_t T, int64_t S, int H, int
 
 template <typename TS, int D> hipError_t run_attn(const AttnArgs& a, hipStream_t s) {
   const int64_t tiles = (a.T + 127) / 128;
-  k_attn<TS, D><<<dim3((unsigned)(tiles * a.Hq)), dim3(64 * kAttnWaves), 0, s>>>(a);
+  const dim3 grid((unsigned)(tiles * a.Hq)), block(64 * kAttnWaves);
+  if (a.cap > 0.f || a.slopes)
+    k_attn<TS, D, true><<<grid, block, 0, s>>>(a);
+  else
+    k_attn<TS, D, false><<<grid, block, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -252,17 +264,28 @@ template <typename TS> hipError_t run_attn_of(int D, const AttnArgs& a, hipStrea
   }
 }
 
+constexpr int64_t padded(int64_t T) { return (T + kTile - 1) / kTile * kTile; }
+
 }  // namespace
 
+size_t attn_lse_bytes(int64_t T, int Hq) { return ((size_t)padded(T) * Hq * 4 + 255) / 256 * 256; }
+size_t attn_saved_bytes(int state_dtype, int64_t T, int Hq, int D) {
+  return attn_lse_bytes(T, Hq) + (state_dtype == XHC_BF16 ? (size_t)T * Hq * D * 2 : 0);
+}
+
 hipError_t launch_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
-                       const float* slopes, void* out, float* lse, hipStream_t s) {
+                       const float* slopes, void* out, void* saved, hipStream_t s) {
   AttnArgs a{};
   a.qkv = qkv;
   a.span = reinterpret_cast<const int2*>(span);
   a.slopes = slopes;
   a.out = out;
-  a.lse = lse;
-  a.T = d->T, a.S = d->S;
+  a.T = d->T, a.S = d->S, a.Tp = padded(d->T);
+  if (saved) {
+    a.lse = static_cast<float*>(saved);
+    if (d->state_dtype == XHC_BF16)
+      a.low = reinterpret_cast<uint16_t*>(static_cast<char*>(saved) + attn_lse_bytes(d->T, h->Hq));
+  }
   a.Hq = h->Hq, a.Hkv = h->Hkv, a.window = h->window;
   a.scale = h->scale, a.cap = h->cap;
   return d->state_dtype == XHC_BF16 ? run_attn_of<uint16_t>(h->D, a, s) : run_attn_of<float>(h->D, a, s);

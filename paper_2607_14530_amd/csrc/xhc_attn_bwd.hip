@@ -15,12 +15,12 @@ namespace xhc {
 
 namespace {
 
-// Tile blockIdx.x of 64 rows: for head blockIdx.y < Hq the rows' delta and
-// lse, in the order in which k_attn_dkv reads them; in the last of them the
-// spans and what they have in common.
+// Tile blockIdx.x of 64 rows: for head blockIdx.y < Hq the rows' delta; in the
+// last of them the spans and what they have in common.  A bf16 out is taken
+// with what its rounding left, which the forward has saved: rounded, it raised
+// the error of dq and dk by a twentieth of theirs.
 template <typename TS, int D>
-__global__ __launch_bounds__(256) void k_attn_prep(AttnArgs a, float* lsep, float* delta, int* lo, int* hi,
-                                                   int4* range) {
+__global__ __launch_bounds__(256) void k_attn_prep(AttnArgs a, float* delta, int* lo, int* hi, int4* range) {
   constexpr int LP = D == 96 ? 16 : D / 8;       // lanes of a row
   const int tile = blockIdx.x, head = blockIdx.y, t0 = tile * kTile;
   if (head == a.Hq) {
@@ -51,16 +51,18 @@ __global__ __launch_bounds__(256) void k_attn_prep(AttnArgs a, float* lsep, floa
       float x[8], y[8];
       Vec8<TS>::load(reinterpret_cast<const TS*>(a.out) + at, x);
       Vec8<TS>::load(reinterpret_cast<const TS*>(a.dout) + at, y);
+      if (sizeof(TS) == 2) {
+        float z[8];
+        Vec8<uint16_t>::load(a.low + at, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += z[i];
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(x[i], y[i], sum);
     }
 #pragma unroll
     for (int d = 1; d < LP; d *= 2) sum += __shfl_xor(sum, d);
-    if (threadIdx.x % LP == 0) {
-      const int64_t to = (int64_t)head * a.Tp + t;
-      delta[to] = sum;
-      lsep[to] = t < a.T ? a.lse[(int64_t)t * a.Hq + head] : 0.f;
-    }
+    if (threadIdx.x % LP == 0) delta[(int64_t)head * a.Tp + t] = sum;
   }
 }
 
@@ -80,7 +82,7 @@ __device__ __forceinline__ void reverse_score(float& x, float& dp, const Score& 
   dp = x * (dp - delta) * der;
 }
 
-template <typename TS, int D>
+template <typename TS, int D, bool EX>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a) {
   using TL = Tile<TS, D>;
   constexpr int KS = D / 16, F = D / 32;
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     Score sc;
     sc.init(a, head);
     const int64_t tc = row ? t : T1;
-    const float lse = a.lsep[(int64_t)head * a.Tp + tc], delta = a.delta[(int64_t)head * a.Tp + tc];
+    const float lse = a.lse[(int64_t)head * a.Tp + tc], delta = a.delta[(int64_t)head * a.Tp + tc];
     Frag<TS> q[KS], go[KS];
     const TS* qp = reinterpret_cast<const TS*>(base) + tc * H * D + head * D;
     const TS* gp = reinterpret_cast<const TS*>(a.dout) + (tc * a.Hq + head) * D;
@@ -125,31 +127,37 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       wait_vm<0>();
       lds_barrier();
       if (kt + 1 < end) {
-        TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, lane);
-        TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, lane);
+        const int ln = again(lane);
+        TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, ln);
+        TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, ln);
       }
       unsigned char *K = lds + off, *V = K + TL::kBytes;
       const int j0 = kt * kTile;
       const bool cut = j0 < ex.z || j0 + kTile > ex.w;
       uint64_t bad = 0;
-      if (cut) bad = TL::clean(K, bits, wave, lane);
-      const float d0 = (float)(t - j0 - 4 * (lane / 32));
-#pragma unroll
+      if (cut) bad = TL::clean(K, bits, wave, again(lane));
+#pragma unroll 1
       for (int rb = 0; rb < 2; ++rb) {
+        const int ln = again(lane);
         f32x16 s = f32x16{}, dp = f32x16{};
+        Frag<TS> k[2];
+        TL::row_frag(K, rb, 0, ln, k[0]);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          Frag<TS> k, v;
-          TL::row_frag(K, rb, ks, lane, k);
-          s = mfma32(k, q[ks], s);
-          TL::row_frag(V, rb, ks, lane, v);
-          dp = mfma32(v, go[ks], dp);
+        for (int i = 0; i < 2 * KS; ++i) {       // a fragment is read while the one before is multiplied
+          if (i + 1 < 2 * KS) TL::row_frag(i + 1 < KS ? K : V, rb, (i + 1) % KS, ln, k[(i + 1) % 2]);
+          if (i < KS)
+            s = mfma32(k[i % 2], q[i % KS], s);
+          else
+            dp = mfma32(k[i % 2], go[i % KS], dp);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        if (a.slopes || a.cap > 0.f) {
+        const int j1 = j0 + 32 * rb + 4 * (ln / 32);         // this lane's keys: j1 + sum_row(r)
+        if constexpr (EX) {
+          const float d0 = (float)(t - j1);
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             float x = s[r], y = dp[r];
-            reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 - (float)(32 * rb + sum_row(r))), lse, delta);
+            reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 - (float)sum_row(r)), lse, delta);
             dp[r] = y;
           }
         } else {
@@ -157,26 +165,27 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
           for (int r = 0; r < 16; ++r)
             dp[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.mul, -lse)) * (dp[r] - delta);
         }
-        if (cut) {
-          const int lo = see.x - j0, hi = see.y - j0;
+        if (bad) {
+          const uint32_t keys = (uint32_t)(bad >> (32 * rb)) >> (4 * (ln / 32));
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = 32 * rb + sum_row(r) + 4 * (lane / 32);
-            const bool seen = j >= lo && j < hi;
-            if (bad && ((bad >> j) & 1)) dp[r] = __builtin_nanf("");
-            if (!seen) dp[r] = 0.f;
-          }
+          for (int r = 0; r < 16; ++r) dp[r] += keys >> sum_row(r) & 1 ? __builtin_nanf("") : 0.f;
         }
+        if (cut) {
+          const int lo = see.x - j1, hi = see.y - j1;
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          Frag<TS> ds;
-          sums_frag(dp, st, ds);
+          for (int r = 0; r < 16; ++r)
+            if (!(sum_row(r) >= lo && sum_row(r) < hi)) dp[r] = 0.f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        Frag<TS> x[2], ds;
+        TL::col_frag(K, 0, 2 * rb, ln, x[0]);
 #pragma unroll
-          for (int f = 0; f < F; ++f) {
-            Frag<TS> k;
-            TL::col_frag(K, f, 2 * rb + st, lane, k);
-            dq[f] = mfma32(k, ds, dq[f]);
-          }
+        for (int i = 0; i < 2 * F; ++i) {
+          const int st = i / F, f = i % F;
+          if (f == 0) sums_frag(dp, st, ds);
+          if (i + 1 < 2 * F) TL::col_frag(K, (i + 1) % F, 2 * rb + (i + 1) / F, ln, x[(i + 1) % 2]);
+          dq[f] = mfma32(x[i % 2], ds, dq[f]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
@@ -192,12 +201,16 @@ template <typename TL> struct QStage {
   static constexpr int kRows = 2 * TL::kBytes, kBytes = kRows + 1024;
 };
 
-template <typename TS, int D>
+template <typename TS, int D, bool EX>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dkv(AttnArgs a) {
   using TL = Tile<TS, D>;
   using ST = QStage<TL>;
   constexpr int KS = D / 16, F = D / 32;
-  __shared__ __align__(1024) unsigned char lds[2 * ST::kBytes];
+  // Of the fragments that a wave keeps, the values' last ones lie in LDS where
+  // the registers do not hold all (D = 128, bf16): two workgroups a CU have 256
+  // registers a lane and 80 KiB each.
+  constexpr int PARKED = sizeof(TS) == 2 && D == 128 ? 3 : 0;
+  __shared__ __align__(1024) unsigned char lds[2 * ST::kBytes + PARKED * kAttnWaves * 1024];
   __shared__ __align__(8) uint16_t bits[8];
   __shared__ int reach[2];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -245,15 +258,24 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       load_frag(kp + 16 * ks + 8 * (lane / 32), kf[ks]);
       load_frag(kp + (int64_t)a.Hkv * D + 16 * ks + 8 * (lane / 32), vf[ks]);
     }
+    Frag<TS>* parked = reinterpret_cast<Frag<TS>*>(lds + 2 * ST::kBytes) + wave * PARKED * 64;
+#pragma unroll
+    for (int i = 0; i < PARKED; ++i) parked[i * 64 + lane] = vf[KS - PARKED + i];
     auto copy = [&](int head, int qt, uint32_t to) {
-      TL::copy(qb + (size_t)head * D * sizeof(TS), qstride, qt * kTile, T1, to, wave, lane);
-      TL::copy(gb + (size_t)head * D * sizeof(TS), gstride, qt * kTile, T1, to + TL::kBytes, wave, lane);
-      const int64_t r = (int64_t)qt * kTile + lane;
-      const void* p = wave == 0   ? (const void*)(a.lsep + (int64_t)head * a.Tp + r)
+      const int ln = again(lane);
+      TL::copy(qb + (size_t)head * D * sizeof(TS), qstride, qt * kTile, T1, to, wave, ln);
+      TL::copy(gb + (size_t)head * D * sizeof(TS), gstride, qt * kTile, T1, to + TL::kBytes, wave, ln);
+      const int64_t r = (int64_t)qt * kTile + ln;
+      const void* p = wave == 0   ? (const void*)(a.lse + (int64_t)head * a.Tp + r)
                       : wave == 1 ? (const void*)(a.delta + (int64_t)head * a.Tp + r)
                       : wave == 2 ? (const void*)(a.lo + r)
                                   : (const void*)(a.hi + r);
       lds_dma4(p, to + ST::kRows + wave * 256);
+    };
+    auto range_of = [&](int i) {                 // (into scalar registers)
+      const int4 x = a.range[i];
+      return make_int4(__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y),
+                       __builtin_amdgcn_readfirstlane(x.z), __builtin_amdgcn_readfirstlane(x.w));
     };
     // the tile behind (head, qt) that is to be taken; head == head0 + mine: none
     auto advance = [&](int& head, int& qt, int4& e) {
@@ -262,11 +284,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
           qt = from;
           ++head;
         }
-        e = a.range[qt];
+        e = range_of(qt);
       } while (head < head0 + mine && !sees(e));
     };
     int head = head0, qt = from, stage = 0;
-    int4 e = a.range[qt];
+    int4 e = range_of(qt);
     copy(head, qt, at);
     while (head < head0 + mine) {
       int nhead = head, nqt = qt;
@@ -282,19 +304,27 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       if (nhead < head0 + mine) copy(nhead, nqt, at + stage * ST::kBytes);
       const bool cut = e.z > j0 || e.w < j0 + 128;
       uint64_t bad = 0;
-      if (cut) bad = TL::clean(Q, bits, wave, lane) | TL::clean(G, bits + 4, wave, lane);
-      const float* rows = reinterpret_cast<const float*>(Q + ST::kRows) + 4 * (lane / 32);
-      const float d0 = (float)(qt * kTile + 4 * (lane / 32) - key);
-#pragma unroll
+      if (cut) bad = TL::clean(Q, bits, wave, again(lane)) | TL::clean(G, bits + 4, wave, again(lane));
+#pragma unroll 1
       for (int rb = 0; rb < 2; ++rb) {
+        const int ln = again(lane);
+        const float* rows = reinterpret_cast<const float*>(Q + ST::kRows) + 4 * (ln / 32);
+        const float d0 = (float)(qt * kTile + 4 * (ln / 32) - key);
         f32x16 s = f32x16{}, dp = f32x16{};
+        // (one product after the other: few registers are left beside the sums and the keys' and values' fragments)
+        Frag<TS> q[2], v;
+        TL::row_frag(Q, rb, 0, ln, q[0]);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          Frag<TS> q, go;
-          TL::row_frag(Q, rb, ks, lane, q);
-          s = mfma32(q, kf[ks], s);
-          TL::row_frag(G, rb, ks, lane, go);
-          dp = mfma32(go, vf[ks], dp);
+        for (int i = 0; i < 2 * KS; ++i) {
+          if (i + 1 < 2 * KS) TL::row_frag(i + 1 < KS ? Q : G, rb, (i + 1) % KS, ln, q[(i + 1) % 2]);
+          if (i < KS) {
+            s = mfma32(q[i % 2], kf[i % KS], s);
+          } else {
+            if (i - KS < KS - PARKED) v = vf[i - KS];
+            dp = mfma32(q[i % 2], v, dp);
+          }
+          if (i + 1 >= 2 * KS - PARKED && i + 1 < 2 * KS) v = parked[(i + 1 - 2 * KS + PARKED) * 64 + ln];
+          __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -304,7 +334,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
           for (int e4 = 0; e4 < 4; ++e4) {
             const int r = 4 * i + e4;
-            if (a.slopes || a.cap > 0.f) {
+            if constexpr (EX) {
               float x = s[r], y = dp[r];
               reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 + (float)(32 * rb + sum_row(r))), L[e4],
                                 E[e4]);
@@ -315,10 +345,21 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
               dp[r] = s[r] * (dp[r] - E[e4]);
             }
           }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (bad) {
+          const uint32_t rows32 = (uint32_t)(bad >> (32 * rb)) >> (4 * (ln / 32));
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float nan = rows32 >> sum_row(r) & 1 ? __builtin_nanf("") : 0.f;
+            s[r] += nan;
+            dp[r] += nan;
+          }
         }
         if (cut) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
             const int4 lo = *reinterpret_cast<const int4*>(rows + 128 + 32 * rb + 8 * i);
             const int4 hi = *reinterpret_cast<const int4*>(rows + 192 + 32 * rb + 8 * i);
             const int L[4] = {lo.x, lo.y, lo.z, lo.w}, U[4] = {hi.x, hi.y, hi.z, hi.w};
@@ -326,25 +367,28 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
             for (int e4 = 0; e4 < 4; ++e4) {
               const int r = 4 * i + e4;
               const bool seen = key >= L[e4] && key < U[e4];
-              if (bad && ((bad >> (32 * rb + sum_row(r) + 4 * (lane / 32))) & 1))
-                s[r] = dp[r] = __builtin_nanf("");
               if (!seen) s[r] = dp[r] = 0.f;
             }
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        Frag<TS> x[2], y[2], p, ds;
+        TL::col_frag(G, 0, 2 * rb, ln, x[0]);
+        TL::col_frag(Q, 0, 2 * rb, ln, y[0]);
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          Frag<TS> p, ds;
-          sums_frag(s, st, p);
-          sums_frag(dp, st, ds);
-#pragma unroll
-          for (int f = 0; f < F; ++f) {
-            Frag<TS> x;
-            TL::col_frag(G, f, 2 * rb + st, lane, x);
-            dv[f] = mfma32(x, p, dv[f]);
-            TL::col_frag(Q, f, 2 * rb + st, lane, x);
-            dk[f] = mfma32(x, ds, dk[f]);
+        for (int i = 0; i < 2 * F; ++i) {
+          const int st = i / F, f = i % F;
+          if (f == 0) {
+            sums_frag(s, st, p);
+            sums_frag(dp, st, ds);
           }
+          if (i + 1 < 2 * F) {
+            TL::col_frag(G, (i + 1) % F, 2 * rb + (i + 1) / F, ln, x[(i + 1) % 2]);
+            TL::col_frag(Q, (i + 1) % F, 2 * rb + (i + 1) / F, ln, y[(i + 1) % 2]);
+          }
+          dv[f] = mfma32(x[i % 2], p, dv[f]);
+          dk[f] = mfma32(y[i % 2], ds, dk[f]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       head = nhead;
@@ -400,33 +444,33 @@ int parts_of(int64_t T, int Hq, int Hkv) {
   return g;
 }
 
-template <typename TS, int D> hipError_t run_bwd(AttnArgs a, char* ws, hipStream_t s) {
+template <typename TS, int D, bool EX> hipError_t run_bwd(AttnArgs a, char* ws, hipStream_t s) {
   const size_t heads = up((size_t)a.Tp * a.Hq * 4), rows = up((size_t)a.Tp * 4);
-  float* lsep = reinterpret_cast<float*>(ws);
-  float* delta = reinterpret_cast<float*>(ws + heads);
-  int* lo = reinterpret_cast<int*>(ws + 2 * heads);
-  int* hi = reinterpret_cast<int*>(ws + 2 * heads + rows);
-  int4* range = reinterpret_cast<int4*>(ws + 2 * heads + 2 * rows);
-  a.part = reinterpret_cast<float*>(ws + 2 * heads + 2 * rows + up((size_t)a.Tp / kTile * 16));
-  k_attn_prep<TS, D><<<dim3((unsigned)(a.Tp / kTile), a.Hq + 1), dim3(256), 0, s>>>(a, lsep, delta, lo, hi, range);
-  a.lsep = lsep, a.delta = delta, a.lo = lo, a.hi = hi, a.range = range;
+  float* delta = reinterpret_cast<float*>(ws);
+  int* lo = reinterpret_cast<int*>(ws + heads);
+  int* hi = reinterpret_cast<int*>(ws + heads + rows);
+  int4* range = reinterpret_cast<int4*>(ws + heads + 2 * rows);
+  a.part = reinterpret_cast<float*>(ws + heads + 2 * rows + up((size_t)a.Tp / kTile * 16));
+  k_attn_prep<TS, D><<<dim3((unsigned)(a.Tp / kTile), a.Hq + 1), dim3(256), 0, s>>>(a, delta, lo, hi, range);
+  a.delta = delta, a.lo = lo, a.hi = hi, a.range = range;
   const unsigned tiles = (unsigned)((a.T + 127) / 128);
-  k_attn_dkv<TS, D><<<dim3(tiles * a.Hkv * a.parts), dim3(64 * kAttnWaves), 0, s>>>(a);
+  k_attn_dkv<TS, D, EX><<<dim3(tiles * a.Hkv * a.parts), dim3(64 * kAttnWaves), 0, s>>>(a);
   if (a.parts > 1) {
     const int row = 2 * a.Hkv * D;
     k_attn_join<TS><<<dim3((unsigned)((a.T * row / 8 + 255) / 256)), dim3(256), 0, s>>>(
         a.T, row, a.parts, a.part, a.Hq + 2 * a.Hkv, a.Hq, D, static_cast<TS*>(a.dqkv));
   }
-  k_attn_dq<TS, D><<<dim3(tiles * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
+  k_attn_dq<TS, D, EX><<<dim3(tiles * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <typename TS> hipError_t run_bwd_of(int D, const AttnArgs& a, char* ws, hipStream_t s) {
+  const bool ex = a.cap > 0.f || a.slopes;
   switch (D) {
-    case 32: return run_bwd<TS, 32>(a, ws, s);
-    case 64: return run_bwd<TS, 64>(a, ws, s);
-    case 96: return run_bwd<TS, 96>(a, ws, s);
-    default: return run_bwd<TS, 128>(a, ws, s);
+    case 32: return ex ? run_bwd<TS, 32, true>(a, ws, s) : run_bwd<TS, 32, false>(a, ws, s);
+    case 64: return ex ? run_bwd<TS, 64, true>(a, ws, s) : run_bwd<TS, 64, false>(a, ws, s);
+    case 96: return ex ? run_bwd<TS, 96, true>(a, ws, s) : run_bwd<TS, 96, false>(a, ws, s);
+    default: return ex ? run_bwd<TS, 128, true>(a, ws, s) : run_bwd<TS, 128, false>(a, ws, s);
   }
 }
 
@@ -435,19 +479,20 @@ template <typename TS> hipError_t run_bwd_of(int D, const AttnArgs& a, char* ws,
 size_t attn_bwd_ws_bytes(int64_t T, int Hq, int Hkv, int D) {
   const int64_t Tp = (T + kTile - 1) / kTile * kTile;
   const int parts = parts_of(T, Hq, Hkv);
-  return 2 * up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) +
+  return up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) +
          (parts > 1 ? (size_t)parts * T * 2 * Hkv * D * 4 : 0);
 }
 
 hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
-                           const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                           const float* slopes, const void* out, const void* saved, const void* dout, void* dqkv,
                            void* ws, hipStream_t s) {
   AttnArgs a{};
   a.qkv = qkv;
   a.span = reinterpret_cast<const int2*>(span);
   a.slopes = slopes;
   a.out = const_cast<void*>(out);
-  a.lse = const_cast<float*>(lse);
+  a.lse = static_cast<float*>(const_cast<void*>(saved));
+  a.low = reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(a.lse) + attn_lse_bytes(d->T, h->Hq));
   a.dout = dout;
   a.dqkv = dqkv;
   a.T = d->T, a.S = d->S, a.Tp = (d->T + kTile - 1) / kTile * kTile;

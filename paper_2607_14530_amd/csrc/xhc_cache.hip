@@ -642,12 +642,14 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
   }
 }
 
-// A row of the output from the places of its segment's runs, where there are
-// several.
+// Rows of the output from the places of their segments' runs, where there are
+// several: a lane has eight channels of one, and its workgroup's four waves
+// share the runs.
 template <typename TS, int D>
 __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a, int ROWS, int64_t wgs) {
   constexpr int P = D / 8;
-  const int lane = threadIdx.x % 64, g = a.Hq / a.Hkv;
+  __shared__ float red[4][10][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = a.Hq / a.Hkv;
   const int64_t t = blockIdx.x;
   const int b = sequence_of(a.starts, a.B, t, lane);
   if (b < 0 || t >= a.starts[b + 1]) return;
@@ -655,31 +657,47 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a, int ROWS, int64
   const int64_t p = a.lens[b] - (a.starts[b + 1] - t);
   if (p < 0 || p >= (int64_t)a.per_seq * a.page) return;
   const int64_t before = a.where[2 * b], blocks = a.where[2 * b + 1], run = a.where[2 * (int64_t)a.B];
-  for (int u = threadIdx.x; u < a.Hq * P; u += 256) {
-    const int qh = u / P, c = u % P * 8;
-    const int64_t row = (t - first) * g + qh % g, tile = row / ROWS;
-    const int64_t seg0 = before + (tile * a.Hkv + qh / g) * blocks;
-    const int64_t w0 = seg0 / run, w1 = (seg0 + blocks - 1) / run;
-    if (w0 == w1 || w1 >= wgs) continue;         // (>=: only where starts do not ascend)
-    auto place = [&](int64_t w) { return (2 * w + (w == w0 ? 1 : 0)) * ROWS + row % ROWS; };
-    float top = -__builtin_huge_valf();
-    for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, a.ml[place(w)].x);
-    const float ref = top == -__builtin_huge_valf() ? 0.f : top;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-    for (int64_t w = w0; w <= w1; ++w) {
+  const int u = blockIdx.y * 64 + lane, qh = u / P, c = u % P * 8;
+  const int64_t row = (t - first) * g + qh % g, tile = row / ROWS;
+  const int64_t seg0 = before + (tile * a.Hkv + qh / g) * blocks;
+  const int64_t w0 = seg0 / run, w1 = (seg0 + blocks - 1) / run;
+  const bool is = u < a.Hq * P && w0 < w1 && w1 < wgs;       // (w1 >= wgs: only where starts do not ascend)
+  auto place = [&](int64_t w) { return (2 * w + (w == w0 ? 1 : 0)) * ROWS + row % ROWS; };
+  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, top = -__builtin_huge_valf(), sum = 0.f;
+  // adds (m, l, y) to what there is: the larger maximum is the reference
+  auto add = [&](float m, float l, const float (&y)[8]) {
+    const float to = fmaxf(top, m), ref = to == -__builtin_huge_valf() ? 0.f : to;
+    const float c0 = __builtin_amdgcn_exp2f(top - ref), c1 = __builtin_amdgcn_exp2f(m - ref);
+    sum = sum * c0 + l * c1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = x[e] * c0 + y[e] * c1;
+    top = to;
+  };
+  if (is) {
+#pragma unroll 4
+    for (int64_t w = w0 + wave; w <= w1; w += 4) {
       const float2 ml = a.ml[place(w)];
-      const float c2 = __builtin_amdgcn_exp2f(ml.x - ref);
-      sum = fmaf(c2, ml.y, sum);
       float y[8];
       Vec8<float>::load(a.part + place(w) * D + c, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = fmaf(c2, y[e], x[e]);
+      add(ml.x, ml.y, y);
     }
-    const float inv = top == -__builtin_huge_valf() && sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= inv;
-    Vec8<TS>::store(static_cast<TS*>(a.k) + (t * a.Hq + qh) * D + c, x);
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) red[wave][e][lane] = x[e];
+  red[wave][8][lane] = top;
+  red[wave][9][lane] = sum;
+  __syncthreads();
+  if (wave != 0 || !is) return;
+  for (int w = 1; w < 4; ++w) {
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = red[w][e][lane];
+    add(red[w][8][lane], red[w][9][lane], y);
+  }
+  const float inv = top == -__builtin_huge_valf() && sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= inv;
+  Vec8<TS>::store(static_cast<TS*>(a.k) + (t * a.Hq + qh) * D + c, x);
 }
 
 CacheArgs args_of(const xhc_dims* d, const xhc_heads* h, const xhc_cache* c, const int32_t* starts,
@@ -778,7 +796,7 @@ hipError_t launch_cache_attend(const xhc_dims* d, const xhc_heads* h, const xhc_
   a.part = reinterpret_cast<float*>(p);
   a.ml = reinterpret_cast<float2*>(p + up(slots * h->D * 4));
   a.where = reinterpret_cast<int64_t*>(p + up(slots * h->D * 4) + up(slots * 8));
-  const dim3 grid((unsigned)wgs), block(256), tokens((unsigned)d->T);
+  const dim3 grid((unsigned)wgs), block(256), tokens((unsigned)d->T, (unsigned)((h->Hq * (h->D / 8) + 63) / 64));
   with_width(h->D, [&](auto D) {
     if (d->state_dtype == XHC_BF16) {
       if (rows == 16)

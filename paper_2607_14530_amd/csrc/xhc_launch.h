@@ -332,10 +332,12 @@ hipError_t launch_rotate(const xhc_dims* d, const xhc_heads* h, const void* src,
 hipError_t launch_attn_spans(int64_t T, int64_t S, int window, int n, const int32_t* starts, const int32_t* prefix,
                              int32_t* span, hipStream_t s);
 hipError_t launch_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
-                       const float* slopes, void* out, float* lse, hipStream_t s);
+                       const float* slopes, void* out, void* saved, hipStream_t s);
+size_t attn_lse_bytes(int64_t T, int Hq);
+size_t attn_saved_bytes(int state_dtype, int64_t T, int Hq, int D);
 size_t attn_bwd_ws_bytes(int64_t T, int Hq, int Hkv, int D);
 hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
-                           const float* slopes, const void* out, const float* lse, const void* dout, void* dqkv,
+                           const float* slopes, const void* out, const void* saved, const void* dout, void* dqkv,
                            void* ws, hipStream_t s);
 
 constexpr int64_t kMaxCached = (int64_t)1 << 24;     // tokens that a sequence's row of the page table has room for

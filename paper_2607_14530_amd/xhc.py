@@ -137,6 +137,7 @@ _SIGS = {
     "xhc_rotate": (ctypes.c_int, [_D, _H] + [_P] * 3 + [ctypes.c_int64, ctypes.c_int32, _P, _P]),
     "xhc_attn_spans": (ctypes.c_int, [_D, _H, ctypes.c_int32] + [_P] * 4),
     "xhc_attn": (ctypes.c_int, [_D, _H] + [_P] * 6),
+    "xhc_attn_saved_bytes": (ctypes.c_size_t, [_D, _H]),
     "xhc_attn_workspace_bytes": (ctypes.c_size_t, [_D, _H]),
     "xhc_attn_bwd": (ctypes.c_int, [_D, _H] + [_P] * 8 + [ctypes.c_size_t, _P]),
     "xhc_cache_bytes": (ctypes.c_size_t, [_H, _C]),
@@ -375,17 +376,21 @@ def xhc_attn_spans(d, h, n, starts, prefix, span, stream=None):
           _stream(stream))
 
 
-def xhc_attn(d, h, qkv, span, slopes, out, lse, stream=None):
-    _call("xhc_attn", ctypes.byref(d), ctypes.byref(h), _ptr(qkv), _ptr(span), _ptr(slopes), _ptr(out), _ptr(lse),
+def xhc_attn(d, h, qkv, span, slopes, out, saved, stream=None):
+    _call("xhc_attn", ctypes.byref(d), ctypes.byref(h), _ptr(qkv), _ptr(span), _ptr(slopes), _ptr(out), _ptr(saved),
           _stream(stream))
+
+
+def xhc_attn_saved_bytes(d, h):
+    return lib().xhc_attn_saved_bytes(ctypes.byref(d), ctypes.byref(h))
 
 
 def xhc_attn_workspace_bytes(d, h):
     return lib().xhc_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(h))
 
 
-def xhc_attn_bwd(d, h, qkv, span, slopes, out, lse, dout, dqkv, workspace, stream=None):
-    _call("xhc_attn_bwd", ctypes.byref(d), ctypes.byref(h), _ptr(qkv), _ptr(span), _ptr(slopes), _ptr(out), _ptr(lse),
+def xhc_attn_bwd(d, h, qkv, span, slopes, out, saved, dout, dqkv, workspace, stream=None):
+    _call("xhc_attn_bwd", ctypes.byref(d), ctypes.byref(h), _ptr(qkv), _ptr(span), _ptr(slopes), _ptr(out), _ptr(saved),
           _ptr(dout), _ptr(dqkv), _ptr(workspace), _nbytes(workspace), _stream(stream))
 
 
@@ -1011,7 +1016,7 @@ class Attention:
         self.d, self.h, self.device = d, h, _here(device)
         self.slopes = _slopes(h, slopes, self.device)
         self.out = torch.empty(d.T, h.Hq, h.D, dtype=_state_dtype(d), device=self.device)
-        self.lse = None
+        self.saved = None
         self.span = None
 
     def spans(self, starts=None, prefix=None, stream=None):
@@ -1034,7 +1039,7 @@ class Attention:
         _expect(qkv, self.out.dtype, (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D), "qkv")
         _on(qkv, self.device, "qkv")
         _expect_ints(span, (self.d.T, 2), self.device, "span")
-        xhc_attn(self.d, self.h, qkv, span, self.slopes, self.out, self.lse, stream)
+        xhc_attn(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, stream)
         return self.out
 
 
@@ -1044,7 +1049,7 @@ class TrainableAttention(Attention):
 
     def __init__(self, d: Dims, h: Heads, slopes=None, device="cuda"):
         super().__init__(d, h, slopes, device)
-        self.lse = torch.empty(d.T, h.Hq, dtype=torch.float32, device=self.device)
+        self.saved = _bytes(xhc_attn_saved_bytes(d, h), self.device)
         self.dqkv = torch.empty(d.T, h.Hq + 2 * h.Hkv, h.D, dtype=self.out.dtype, device=self.device)
         self.ws = _bytes(xhc_attn_workspace_bytes(d, h), self.device)
         self.seen = None
@@ -1060,7 +1065,7 @@ class TrainableAttention(Attention):
         _expect(dout, self.out.dtype, self.out.shape, "dout")
         _on(dout, self.device, "dout")
         qkv, span = self.seen
-        xhc_attn_bwd(self.d, self.h, qkv, span, self.slopes, self.out, self.lse, dout, self.dqkv, self.ws, stream)
+        xhc_attn_bwd(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, dout, self.dqkv, self.ws, stream)
         return self.dqkv
 
 

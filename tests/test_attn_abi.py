@@ -46,11 +46,11 @@ def spans(d, h, n, p):                                # starts, prefix, span
     return X.lib().xhc_attn_spans(ctypes.byref(d), ctypes.byref(h), n, *p, None)
 
 
-def attn(d, h, p):                                    # qkv, span, slopes, out, lse
+def attn(d, h, p):                                    # qkv, span, slopes, out, saved
     return X.lib().xhc_attn(ctypes.byref(d), ctypes.byref(h), *p, None)
 
 
-def attn_bwd(d, h, p, ws=BIG):                        # qkv, span, slopes, out, lse, dout, dqkv, workspace
+def attn_bwd(d, h, p, ws=BIG):                        # qkv, span, slopes, out, saved, dout, dqkv, workspace
     return X.lib().xhc_attn_bwd(ctypes.byref(d), ctypes.byref(h), *p, ws, None)
 
 
@@ -138,11 +138,13 @@ def test_spans_refusals():
 
 def test_attn_refusals():
     d, h = dims(), heads()
-    refused(lambda p: attn(d, h, p), A[:5], {1, 2, 4}, [16, 8, 4, 16, 4])
-    overlaps(lambda p: attn(d, h, p), A[:5], [QKV, 512, 16, ROWS, 1024], [3, 4])
-    refused(lambda p: attn_bwd(d, h, p), A[:8], {1, 2}, [16, 8, 4, 16, 4, 16, 16, 16])
+    saved = X.xhc_attn_saved_bytes(d, h)
+    assert saved == 64 * 4 * 4 + ROWS and X.xhc_attn_saved_bytes(dims(state="f32"), h) == 64 * 4 * 4
+    refused(lambda p: attn(d, h, p), A[:5], {1, 2, 4}, [16, 8, 4, 16, 16])
+    overlaps(lambda p: attn(d, h, p), A[:5], [QKV, 512, 16, ROWS, saved], [3, 4])
+    refused(lambda p: attn_bwd(d, h, p), A[:8], {1, 2}, [16, 8, 4, 16, 16, 16, 16, 16])
     need = X.xhc_attn_workspace_bytes(d, h)
-    overlaps(lambda p: attn_bwd(d, h, p), A[:8], [QKV, 512, 16, ROWS, 1024, ROWS, QKV, need], [6, 7])
+    overlaps(lambda p: attn_bwd(d, h, p), A[:8], [QKV, 512, 16, ROWS, saved, ROWS, QKV, need], [6, 7])
     assert need > 0 and attn_bwd(d, h, A[:8], need - 1) == X.XHC_EWORKSPACE
     assert X.xhc_attn_workspace_bytes(d, heads(D=160)) == 0
 
