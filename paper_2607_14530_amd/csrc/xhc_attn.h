@@ -49,6 +49,19 @@ __device__ __forceinline__ void sums_frag(const f32x16& x, int s, Frag32& f) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) f.v[j] = x[8 * s + j];
 }
+// l and the sum of a fragment's elements, as they are in it
+__device__ __forceinline__ float add_frag(const uint4& f, float l) {
+  const bf16x2 one = __builtin_bit_cast(bf16x2, 0x3f803f80u);
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, f.x), one, l, false);
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, f.y), one, l, false);
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, f.z), one, l, false);
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, f.w), one, l, false);
+}
+__device__ __forceinline__ float add_frag(const Frag32& f, float l) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) l += f.v[j];
+  return l;
+}
 
 __device__ __forceinline__ void load_frag(const uint16_t* p, uint4& f) { f = *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void load_frag(const float* p, Frag32& f) {
@@ -72,28 +85,58 @@ template <> __device__ __forceinline__ bool not_finite<float>(const uint4& w) {
   return (w.x & e) == e || (w.y & e) == e || (w.z & e) == e || (w.w & e) == e;
 }
 
+// lds_dma16 from a scalar base and an offset for each lane
+__device__ __forceinline__ void lds_dma16_at(const void* base, uint32_t off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(lds_addr)
+               : "memory", "m0");
+}
+
 // A tile of kTile rows of D elements in LDS, in 16-byte pieces.  Piece c of row
-// r lies at place c ^ turn(r), so that eight rows' pieces of one number, which
-// row_frag reads at a time, and four rows' pairs of pieces, which the transposing
-// read takes, meet different banks.  The copy leaves a run of 1 KiB where it
+// r lies at place c ^ turn(r), so that sixteen rows' pieces of one number, which
+// row_frag reads at a time, and four rows' fours of pieces, which the transposing
+// read takes, meet all 64 banks (turned for eight rows and pairs only, half of
+// the LDS cycles were conflicts).  The copy leaves a run of 1 KiB where it
 // puts it, so the pieces are turned on the way: each lane reads the piece that
 // belongs to its place.
 template <typename TS, int D>
 struct Tile {
   static constexpr int kPieces = D * (int)sizeof(TS) / 16, kRowBytes = kPieces * 16, kBytes = kTile * kRowBytes;
   static constexpr int kCopies = kTile * kPieces / 64 / kAttnWaves;
-  static constexpr bool kEight = kPieces % 8 == 0;
   static_assert(kTile * kPieces % (64 * kAttnWaves) == 0, "whole copies for every wave");
   static __device__ __forceinline__ int turn(int r) {
-    return kEight ? 2 * (r % 4) + r / 4 % 2 : 2 * (r / 2 % 2) + r / 4 % 2;
+    if (kPieces % 16 == 0) return 4 * (r % 4) + r / 4 % 4;
+    if (kPieces % 8 == 0) return 4 * (r / 2 % 2) + r / 4 % 4;
+    return r / 4 % 4;
   }
-  // rows row0 .. of a tensor whose rows lie `stride` bytes apart, those behind
-  // `last` as copies of it (what becomes of them is masked)
+  // Rows row0 .. of a tensor whose rows lie `stride` bytes apart, those behind
+  // `last` as copies of it (what becomes of them is masked).  A copy's rows and
+  // pieces follow from the wave's first copy's: by whole rows, which are added
+  // to the scalar base, and by the turn, which changes with the row's number.
   static __device__ __forceinline__ void copy(const unsigned char* base, uint32_t stride, int row0, int last,
                                               uint32_t to, int wave, int lane) {
+    if (row0 + kTile - 1 <= last) {
+      base += (uint64_t)(uint32_t)row0 * stride;
 #pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        const int at = (wave * kCopies + i) * 64;
+        if constexpr (64 % kPieces == 0 && 16 % (64 / kPieces) == 0) {
+          constexpr int R = 64 / kPieces;        // rows of a copy
+          const int r = at / kPieces, x = lane / kPieces;        // (r: a multiple of R)
+          const int c = lane % kPieces ^ turn(x) ^ turn(r % 16);
+          static_assert(R <= 16, "turn(r + x) = turn(r) ^ turn(x) for x below R, r a multiple of it");
+          lds_dma16_at(base + (uint64_t)(uint32_t)r * stride, (uint32_t)x * stride + c * 16, to + at * 16);
+        } else {
+          const int r = (at + lane) / kPieces, c = (at + lane) % kPieces ^ turn(r);
+          lds_dma16_at(base, (uint32_t)r * stride + c * 16, to + at * 16);
+        }
+      }
+      return;
+    }
+#pragma unroll 1
     for (int i = 0; i < kCopies; ++i) {
-      const int at = (wave * kCopies + i) * 64 + lane, r = at / kPieces, c = (at % kPieces) ^ turn(r);
+      const int at = (wave * kCopies + i) * 64 + lane, r = at / kPieces, c = at % kPieces ^ turn(r);
       const int t = row0 + r < last ? row0 + r : last;
       lds_dma16(base + ((uint64_t)(uint32_t)t * stride + c * 16), to + (wave * kCopies + i) * 1024);
     }
@@ -117,10 +160,10 @@ struct Tile {
   static __device__ __forceinline__ void col_frag(const unsigned char* s, int f, int st, int lane, uint4& out) {
     const int r = 4 * (lane / 32) + lane % 16 / 4, q = lane % 4;   // of this lane's read: a row, four channels
     const int c = 4 * f + 2 * (lane / 16 % 2) + q / 2;
-    const unsigned char* p = s + (16 * st + r) * kRowBytes + (c ^ turn(r)) * 16 + q % 2 * 8;
+    const unsigned char* p = s + (16 * st + r) * kRowBytes + q % 2 * 8;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRowBytes));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (c ^ turn(r)) * 16));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRowBytes + (c ^ turn(r + 8)) * 16));
     const uint2 ua = __builtin_bit_cast(uint2, a), ub = __builtin_bit_cast(uint2, b);
     out = make_uint4(ua.x, ua.y, ub.x, ub.y);
   }
@@ -165,6 +208,19 @@ __device__ __forceinline__ int again(int lane) {
   asm volatile("" : "+v"(lane));
   return lane & 63;
 }
+
+// Waits for all copies and loads of this wave.  (By the builtin: the compiler
+// then knows that what it has loaded itself is there.  Not knowing, it waited
+// in every turn of a loop for fragments loaded before it, and so for the copies
+// that had just been sent.)
+__device__ __forceinline__ void wait_loads() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt = 0, expcnt = 7, lgkmcnt = 15 (no wait)
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
+// Stands in a branch that the compiler is not to turn into selections.
+__device__ __forceinline__ void branch_only() { __builtin_amdgcn_sched_barrier(0); }
 
 // What an attention call is about, as its kernels take it.
 struct AttnArgs {

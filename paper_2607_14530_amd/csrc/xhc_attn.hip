@@ -51,7 +51,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     TL::copy(vb, stride, first * kTile, T1, at + TL::kBytes, wave, lane);
     for (int kt = first; kt < end; ++kt) {
       const uint32_t off = (kt - first) % 2 * 2 * TL::kBytes, next = 2 * TL::kBytes - off;
-      wait_vm<0>();
+      wait_loads();
       lds_barrier();
       if (kt + 1 < end) {
         const int ln = again(lane);
@@ -95,6 +95,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
           for (int r = 0; r < 16; ++r) s[rb][r] = fmaf(-sc.slope, fabsf(d0 - (float)(32 * rb + sum_row(r))), s[rb][r]);
       }
       if (cut) {
+        branch_only();
         const int lo = see.x - j0 - 4 * (lane / 32), hi = see.y - j0 - 4 * (lane / 32);
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
@@ -103,6 +104,15 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
             const int j = 32 * rb + sum_row(r);
             if (!(j >= lo && j < hi)) s[rb][r] = kNoKey;
           }
+        if (bad) {
+#pragma unroll
+          for (int rb = 0; rb < 2; ++rb) {
+            const uint32_t keys = (uint32_t)(bad >> (32 * rb)) >> (4 * (lane / 32));
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if ((keys >> sum_row(r) & 1) && s[rb][r] != kNoKey) s[rb][r] = __builtin_nanf("");
+          }
+        }
       }
       float top = s[0][0];
 #pragma unroll
@@ -127,22 +137,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 16; ++r)
           s[rb][r] = __builtin_amdgcn_exp2f(EX ? s[rb][r] - ref : fmaf(s[rb][r], sc.mul, -ref));
-          l += s[rb][r];
-        }
-      if (bad) {
-        const int lo = see.x - j0 - 4 * (lane / 32), hi = see.y - j0 - 4 * (lane / 32);
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          const uint32_t keys = (uint32_t)(bad >> (32 * rb)) >> (4 * (lane / 32));
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = 32 * rb + sum_row(r);
-            if ((keys >> sum_row(r) & 1) && j >= lo && j < hi) s[rb][r] = __builtin_nanf("");
-          }
-        }
-      }
       __builtin_amdgcn_sched_barrier(0);
       const int ln = again(lane);
       Frag<TS> v[2], p;
@@ -150,7 +146,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
       for (int i = 0; i < 4 * F; ++i) {
         const int st = i / F, f = i % F;
-        if (f == 0) sums_frag(s[st / 2], st % 2, p);
+        if (f == 0) {
+          sums_frag(s[st / 2], st % 2, p);
+          l = add_frag(p, l);                    // (the sum of what the values are multiplied with)
+        }
         if (i + 1 < 4 * F) TL::col_frag(V, (i + 1) % F, (i + 1) / F, ln, v[(i + 1) % 2]);
         o[f] = mfma32(v[i % 2], p, o[f]);
         __builtin_amdgcn_sched_barrier(0);

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     TL::copy(vb, stride, first * kTile, T1, at + TL::kBytes, wave, lane);
     for (int kt = first; kt < end; ++kt) {
       const uint32_t off = (kt - first) % 2 * 2 * TL::kBytes, next = 2 * TL::kBytes - off;
-      wait_vm<0>();
+      wait_loads();
       lds_barrier();
       if (kt + 1 < end) {
         const int ln = again(lane);
@@ -166,11 +166,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
             dp[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.mul, -lse)) * (dp[r] - delta);
         }
         if (bad) {
+          branch_only();
           const uint32_t keys = (uint32_t)(bad >> (32 * rb)) >> (4 * (ln / 32));
 #pragma unroll
           for (int r = 0; r < 16; ++r) dp[r] += keys >> sum_row(r) & 1 ? __builtin_nanf("") : 0.f;
         }
         if (cut) {
+          branch_only();
           const int lo = see.x - j1, hi = see.y - j1;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       advance(nhead, nqt, ne);      // (loads of its own stand before the copies, which a wait for them would wait for)
       Score sc;
       sc.init(a, head);
-      wait_vm<0>();
+      wait_loads();
       lds_barrier();
       unsigned char* Q = lds + stage * ST::kBytes;
       unsigned char* G = Q + TL::kBytes;
@@ -348,6 +350,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
           __builtin_amdgcn_sched_barrier(0);
         }
         if (bad) {
+          branch_only();
           const uint32_t rows32 = (uint32_t)(bad >> (32 * rb)) >> (4 * (ln / 32));
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -359,7 +362,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
         if (cut) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
+            branch_only();
             const int4 lo = *reinterpret_cast<const int4*>(rows + 128 + 32 * rb + 8 * i);
             const int4 hi = *reinterpret_cast<const int4*>(rows + 192 + 32 * rb + 8 * i);
             const int L[4] = {lo.x, lo.y, lo.z, lo.w}, U[4] = {hi.x, hi.y, hi.z, hi.w};
