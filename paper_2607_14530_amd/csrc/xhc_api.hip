@@ -1233,7 +1233,7 @@ size_t xhc_attn_saved_bytes(const xhc_dims* d, const xhc_heads* h) {
 }
 
 size_t xhc_attn_workspace_bytes(const xhc_dims* d, const xhc_heads* h) {
-  return check_heads(d, h) == XHC_OK ? attn_bwd_ws_bytes(d->T, h->Hq, h->Hkv, h->D) : 0;
+  return check_heads(d, h) == XHC_OK ? attn_bwd_ws_bytes(d->state_dtype, d->T, h->Hq, h->Hkv, h->D) : 0;
 }
 
 xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
@@ -1246,7 +1246,7 @@ xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, 
   for (const void* p : {qkv, out, saved, dout, (const void*)dqkv, (const void*)workspace})
     if (!aligned16(p)) return XHC_EUNSUPPORTED;
   if (!aligned(span, 8) || !aligned(slopes, 4)) return XHC_EUNSUPPORTED;
-  const size_t need = attn_bwd_ws_bytes(d->T, h->Hq, h->Hkv, h->D);
+  const size_t need = attn_bwd_ws_bytes(d->state_dtype, d->T, h->Hq, h->Hkv, h->D);
   if (workspace_bytes < need) return XHC_EWORKSPACE;
   const size_t all = heads_bytes(d, h, h->Hq + 2 * h->Hkv), rows = heads_bytes(d, h, h->Hq);
   if (!buffers_apart({{qkv, all, false}, {span, (size_t)d->T * 8, false}, {slopes, (size_t)h->Hq * 4, false},

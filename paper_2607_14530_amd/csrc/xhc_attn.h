@@ -100,11 +100,11 @@ __device__ __forceinline__ void lds_dma16_at(const void* base, uint32_t off, uin
 // the LDS cycles were conflicts).  The copy leaves a run of 1 KiB where it
 // puts it, so the pieces are turned on the way: each lane reads the piece that
 // belongs to its place.
-template <typename TS, int D>
+template <typename TS, int D, int NW = kAttnWaves>
 struct Tile {
   static constexpr int kPieces = D * (int)sizeof(TS) / 16, kRowBytes = kPieces * 16, kBytes = kTile * kRowBytes;
-  static constexpr int kCopies = kTile * kPieces / 64 / kAttnWaves;
-  static_assert(kTile * kPieces % (64 * kAttnWaves) == 0, "whole copies for every wave");
+  static constexpr int kCopies = kTile * kPieces / 64 / NW;
+  static_assert(kTile * kPieces % (64 * NW) == 0 && kPieces % NW == 0, "whole copies, and pieces, for every wave");
   static __device__ __forceinline__ int turn(int r) {
     if (kPieces % 16 == 0) return 4 * (r % 4) + r / 4 % 4;
     if (kPieces % 8 == 0) return 4 * (r / 2 % 2) + r / 4 % 4;
@@ -180,25 +180,30 @@ struct Tile {
   // see, which has to be finite: so tiles that a mask cuts are looked over, and
   // for the columns that do see such a row the caller puts a NaN in the row's
   // place.  Called by all waves between barriers of its own.
-  static __device__ __forceinline__ uint64_t clean(unsigned char* s, uint16_t* bits, int wave, int lane) {
-    const int r = wave * 16 + lane / 4;
+  static __device__ __forceinline__ uint64_t clean(unsigned char* s, uint64_t* bits, int wave, int lane) {
+    constexpr int RW = kTile / NW;               // rows of a wave, NW lanes each
+    const int r = wave * RW + lane / NW;
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < kPieces / 4; ++i) bad |= not_finite<TS>(piece(s, r, lane % 4 + 4 * i));
+    for (int i = 0; i < kPieces / NW; ++i) bad |= not_finite<TS>(piece(s, r, lane % NW + NW * i));
     const uint64_t all = __ballot(bad);
+    constexpr uint64_t lanes = (1u << NW) - 1;
     uint32_t rows = 0;
     if (all) {
-      const bool mine = (all >> (lane / 4 * 4)) & 15;
-      rows = 0;
-      for (int i = 0; i < 16; ++i) rows |= (uint32_t)(((all >> (4 * i)) & 15) != 0) << i;
-      if (mine) {
+      for (int i = 0; i < RW; ++i) rows |= (uint32_t)((all >> (NW * i) & lanes) != 0) << i;
+      if (rows >> (lane / NW) & 1) {
 #pragma unroll
-        for (int i = 0; i < kPieces / 4; ++i) piece(s, r, lane % 4 + 4 * i) = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kPieces / NW; ++i) piece(s, r, lane % NW + NW * i) = make_uint4(0, 0, 0, 0);
       }
     }
-    if (lane == 0) bits[wave] = (uint16_t)rows;
+    if (lane == 0) {
+      if constexpr (RW == 16)
+        reinterpret_cast<uint16_t*>(bits)[wave] = (uint16_t)rows;
+      else
+        reinterpret_cast<uint8_t*>(bits)[wave] = (uint8_t)rows;
+    }
     lds_barrier();
-    return *reinterpret_cast<const uint64_t*>(bits);
+    return *bits;
   }
 };
 
@@ -221,6 +226,31 @@ __device__ __forceinline__ void wait_loads() {
 
 // Stands in a branch that the compiler is not to turn into selections.
 __device__ __forceinline__ void branch_only() { __builtin_amdgcn_sched_barrier(0); }
+
+// N products: use(i, fragment i), with the fragments of the next AHEAD on their
+// way from LDS (its latency is that of some three products).  In this order,
+// which the compiler is kept from changing, and before what other waves do.
+template <int N, int AHEAD, typename F, class Read, class Use>
+__device__ __forceinline__ void feed(Read&& read, Use&& use) {
+  F f[AHEAD + 1];
+  __builtin_amdgcn_s_setprio(1);
+  __builtin_amdgcn_sched_barrier(0);
+  unroll<(AHEAD < N ? AHEAD : N)>([&](auto i) { read(i, f[i.value]); });
+  unroll<N>([&](auto i) {
+    if constexpr (i.value + AHEAD < N) read(Int<i.value + AHEAD>{}, f[(i.value + AHEAD) % (AHEAD + 1)]);
+    use(i, f[i.value % (AHEAD + 1)]);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+  __builtin_amdgcn_s_setprio(0);
+}
+
+// Step i's share of N pieces of work among STEPS steps.
+template <int N, int STEPS, class I, class F> __device__ __forceinline__ void share(I, F&& f) {
+  constexpr int each = (N + STEPS - 1) / STEPS, from = I::value * each;
+  unroll<each>([&](auto x) {
+    if constexpr (from + x.value < N) f(Int<from + x.value>{});
+  });
+}
 
 // What an attention call is about, as its kernels take it.
 struct AttnArgs {
@@ -290,8 +320,8 @@ __host__ __device__ __forceinline__ constexpr int sum_row(int r) { return 8 * (r
 
 // The workgroup's extremes of its rows' spans: x min lo, y max hi of the rows
 // that see keys (x >= y where none does), z max lo, w min hi of all.  Rows
-// behind the last are left out.
-__device__ __forceinline__ int4 attn_extremes(int2 s, bool row, int4* red, int wave, int lane) {
+// behind the last are left out.  own: x and y of the wave's rows.
+__device__ __forceinline__ int4 attn_extremes(int2 s, bool row, int4* red, int wave, int lane, int2& own) {
   const bool some = row && s.x < s.y;
   int4 e = make_int4(some ? s.x : INT32_MAX, some ? s.y : 0, row ? (some ? s.x : INT32_MAX) : 0,
                      row ? (some ? s.y : 0) : INT32_MAX);
@@ -302,6 +332,7 @@ __device__ __forceinline__ int4 attn_extremes(int2 s, bool row, int4* red, int w
     e.z = max(e.z, __shfl_xor(e.z, d));
     e.w = min(e.w, __shfl_xor(e.w, d));
   }
+  own = make_int2(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y));
   if (lane == 0) red[wave] = e;
   __syncthreads();
   e = red[0];

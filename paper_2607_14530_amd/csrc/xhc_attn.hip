@@ -17,10 +17,10 @@ constexpr float kNoKey = -__builtin_huge_valf();
 template <typename TS, int D, bool EX>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn(AttnArgs a) {
   using TL = Tile<TS, D>;
-  constexpr int KS = D / 16, F = D / 32;
+  constexpr int KS = D / 16, F = D / 32, AHEAD = sizeof(TS) == 2 ? 4 : 2;
   __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
   __shared__ int4 red[kAttnWaves];
-  __shared__ __align__(8) uint16_t bits[4];
+  __shared__ uint64_t bits;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
   attn_place(a.Hq, (int)((a.T + 127) / 128), head, tile);
@@ -28,7 +28,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   const int t = tile * 128 + wave * 32 + lane % 32, T1 = (int)a.T - 1;
   const bool row = t <= T1;
   const int2 see = span_of(a, t);
-  const int4 ex = attn_extremes(see, row, red, wave, lane);
+  int2 own;
+  const int4 ex = attn_extremes(see, row, red, wave, lane, own);
   const uint32_t stride = (uint32_t)H * D * sizeof(TS);
   const unsigned char* base = reinterpret_cast<const unsigned char*>(a.qkv);
   const unsigned char* kb = base + (size_t)(a.Hq + kvh) * D * sizeof(TS);
@@ -62,19 +63,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       const int j0 = kt * kTile;
       const bool cut = j0 < ex.z || j0 + kTile > ex.w;      // some row does not see all of the tile
       uint64_t bad = 0;
-      if (cut) bad = TL::clean(V, bits, wave, again(lane));
+      if (cut) bad = TL::clean(V, &bits, wave, again(lane));
+      if (j0 >= own.y || j0 + kTile <= own.x) continue;     // no row of this wave sees a key of the tile
       f32x16 s[2] = {f32x16{}, f32x16{}};
-      {
-        const int ln = again(lane);
-        Frag<TS> k[2];
-        TL::row_frag(K, 0, 0, ln, k[0]);
-#pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {       // a fragment is read while the one before is multiplied
-          if (i + 1 < 2 * KS) TL::row_frag(K, (i + 1) / KS, (i + 1) % KS, ln, k[(i + 1) % 2]);
-          s[i / KS] = mfma32(k[i % 2], q[i % KS], s[i / KS]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      int ln = again(lane);
+      feed<2 * KS, AHEAD, Frag<TS>>(
+          [&](auto i, Frag<TS>& k) { TL::row_frag(K, i.value / KS, i.value % KS, ln, k); },
+          [&](auto i, Frag<TS>& k) { s[i.value / KS] = mfma32(k, q[i.value % KS], s[i.value / KS]); });
       // a lane's keys: j0 + 32 rb + sum_row(r) + 4 (lane / 32)
       if (EX && a.cap > 0.f) {
 #pragma unroll
@@ -139,21 +134,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           s[rb][r] = __builtin_amdgcn_exp2f(EX ? s[rb][r] - ref : fmaf(s[rb][r], sc.mul, -ref));
-      __builtin_amdgcn_sched_barrier(0);
-      const int ln = again(lane);
-      Frag<TS> v[2], p;
-      TL::col_frag(V, 0, 0, ln, v[0]);
-#pragma unroll
-      for (int i = 0; i < 4 * F; ++i) {
-        const int st = i / F, f = i % F;
-        if (f == 0) {
-          sums_frag(s[st / 2], st % 2, p);
-          l = add_frag(p, l);                    // (the sum of what the values are multiplied with)
-        }
-        if (i + 1 < 4 * F) TL::col_frag(V, (i + 1) % F, (i + 1) / F, ln, v[(i + 1) % 2]);
-        o[f] = mfma32(v[i % 2], p, o[f]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      ln = again(lane);
+      Frag<TS> p;
+      feed<4 * F, AHEAD, Frag<TS>>(
+          [&](auto i, Frag<TS>& v) { TL::col_frag(V, i.value % F, i.value / F, ln, v); },
+          [&](auto i, Frag<TS>& v) {
+            constexpr int st = i.value / F, f = i.value % F;
+            if constexpr (f == 0) {
+              sums_frag(s[st / 2], st % 2, p);
+              l = add_frag(p, l);                // (the sum of what the values are multiplied with)
+            }
+            o[f] = mfma32(v, p, o[f]);
+          });
     }
   }
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);

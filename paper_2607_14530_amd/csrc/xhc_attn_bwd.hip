@@ -9,6 +9,8 @@
 // fixed and the queries of all heads of the group passing by.  That is seven
 // products in place of five, but no sum is shared between workgroups: no
 // atomics, no fp32 copy of dq, and an order that only the sizes fix.
+#include <float.h>
+
 #include "xhc_attn.h"
 
 namespace xhc {
@@ -85,10 +87,10 @@ __device__ __forceinline__ void reverse_score(float& x, float& dp, const Score& 
 template <typename TS, int D, bool EX>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a) {
   using TL = Tile<TS, D>;
-  constexpr int KS = D / 16, F = D / 32;
+  constexpr int KS = D / 16, F = D / 32, AHEAD = sizeof(TS) == 2 ? 4 : 2;
   __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
   __shared__ int4 red[kAttnWaves];
-  __shared__ __align__(8) uint16_t bits[4];
+  __shared__ uint64_t bits;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
   attn_place(a.Hq, (int)((a.T + 127) / 128), head, tile);
@@ -96,7 +98,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   const int t = tile * 128 + wave * 32 + lane % 32, T1 = (int)a.T - 1;
   const bool row = t <= T1;
   const int2 see = span_of(a, t);
-  const int4 ex = attn_extremes(see, row, red, wave, lane);
+  int2 own;
+  const int4 ex = attn_extremes(see, row, red, wave, lane, own);
   const uint32_t stride = (uint32_t)H * D * sizeof(TS);
   const unsigned char* base = reinterpret_cast<const unsigned char*>(a.qkv);
   const unsigned char* kb = base + (size_t)(a.Hq + kvh) * D * sizeof(TS);
@@ -135,22 +138,20 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       const int j0 = kt * kTile;
       const bool cut = j0 < ex.z || j0 + kTile > ex.w;
       uint64_t bad = 0;
-      if (cut) bad = TL::clean(K, bits, wave, again(lane));
+      if (cut) bad = TL::clean(K, &bits, wave, again(lane));
+      const bool none = j0 >= own.y || j0 + kTile <= own.x;   // no row of this wave sees a key of the tile
 #pragma unroll 1
-      for (int rb = 0; rb < 2; ++rb) {
+      for (int rb = none ? 2 : 0; rb < 2; ++rb) {
         const int ln = again(lane);
         f32x16 s = f32x16{}, dp = f32x16{};
-        Frag<TS> k[2];
-        TL::row_frag(K, rb, 0, ln, k[0]);
-#pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {       // a fragment is read while the one before is multiplied
-          if (i + 1 < 2 * KS) TL::row_frag(i + 1 < KS ? K : V, rb, (i + 1) % KS, ln, k[(i + 1) % 2]);
-          if (i < KS)
-            s = mfma32(k[i % 2], q[i % KS], s);
-          else
-            dp = mfma32(k[i % 2], go[i % KS], dp);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        feed<2 * KS, AHEAD, Frag<TS>>(
+            [&](auto i, Frag<TS>& k) { TL::row_frag(i.value < KS ? K : V, rb, i.value % KS, ln, k); },
+            [&](auto i, Frag<TS>& k) {
+              if constexpr (i.value < KS)
+                s = mfma32(k, q[i.value], s);
+              else
+                dp = mfma32(k, go[i.value - KS], dp);
+            });
         const int j1 = j0 + 32 * rb + 4 * (ln / 32);         // this lane's keys: j1 + sum_row(r)
         if constexpr (EX) {
           const float d0 = (float)(t - j1);
@@ -178,17 +179,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
           for (int r = 0; r < 16; ++r)
             if (!(sum_row(r) >= lo && sum_row(r) < hi)) dp[r] = 0.f;
         }
-        __builtin_amdgcn_sched_barrier(0);
-        Frag<TS> x[2], ds;
-        TL::col_frag(K, 0, 2 * rb, ln, x[0]);
-#pragma unroll
-        for (int i = 0; i < 2 * F; ++i) {
-          const int st = i / F, f = i % F;
-          if (f == 0) sums_frag(dp, st, ds);
-          if (i + 1 < 2 * F) TL::col_frag(K, (i + 1) % F, 2 * rb + (i + 1) / F, ln, x[(i + 1) % 2]);
-          dq[f] = mfma32(x[i % 2], ds, dq[f]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        Frag<TS> ds;
+        feed<2 * F, AHEAD, Frag<TS>>(
+            [&](auto i, Frag<TS>& k) { TL::col_frag(K, i.value % F, 2 * rb + i.value / F, ln, k); },
+            [&](auto i, Frag<TS>& k) {
+              if constexpr (i.value % F == 0) sums_frag(dp, i.value / F, ds);
+              dq[i.value % F] = mfma32(k, ds, dq[i.value % F]);
+            });
       }
     }
   }
@@ -203,27 +200,32 @@ template <typename TL> struct QStage {
   static constexpr int kRows = 2 * TL::kBytes, kBytes = kRows + 1024;
 };
 
+// Waves of a workgroup of k_attn_dkv.  At D = 128, bf16, a wave's sums and the
+// fragments that it keeps do not fit the 256 registers that two waves a SIMD
+// leave it: the values' last PARKED fragments lie in LDS, which one workgroup
+// of eight waves a CU has room for (two of four waves, three parked: 2.33 ms at
+// T = 16384, Hq = 32, Hkv = 8 with its instructions one after another, which
+// those registers asked for).
+constexpr int dkv_waves(bool f32, int D) { return !f32 && D == 128 ? 8 : 4; }
+
 template <typename TS, int D, bool EX>
-__global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dkv(AttnArgs a) {
-  using TL = Tile<TS, D>;
+__global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2 ? 2 : 1) void k_attn_dkv(AttnArgs a) {
+  constexpr int NW = dkv_waves(sizeof(TS) == 4, D), KEYS = 32 * NW;
+  using TL = Tile<TS, D, NW>;
   using ST = QStage<TL>;
-  constexpr int KS = D / 16, F = D / 32;
-  // Of the fragments that a wave keeps, the values' last ones lie in LDS where
-  // the registers do not hold all (D = 128, bf16): two workgroups a CU have 256
-  // registers a lane and 80 KiB each.
-  constexpr int PARKED = sizeof(TS) == 2 && D == 128 ? 3 : 0;
-  __shared__ __align__(1024) unsigned char lds[2 * ST::kBytes + PARKED * kAttnWaves * 1024];
-  __shared__ __align__(8) uint16_t bits[8];
+  constexpr int KS = D / 16, F = D / 32, AHEAD = 2, PARKED = NW == 8 ? 7 : 0;
+  __shared__ __align__(1024) unsigned char lds[2 * ST::kBytes + PARKED * NW * 1024];
+  __shared__ uint64_t bits[2];
   __shared__ int reach[2];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int g = a.Hq / a.Hkv, mine = g / a.parts, H = a.Hq + 2 * a.Hkv;
-  const int tiles = (int)((a.T + 127) / 128), qtiles = (int)(a.Tp / kTile);
+  const int tiles = (int)((a.T + KEYS - 1) / KEYS), qtiles = (int)(a.Tp / kTile);
   int which, tile;
   attn_place(a.Hkv * a.parts, tiles, which, tile);
   tile = tiles - 1 - tile;                       // the first keys are seen by most queries
   const int kvh = which / a.parts, part = which % a.parts;
   const int head0 = kvh * g + part * mine;
-  const int j0 = tile * 128, T1 = (int)a.T - 1;
+  const int j0 = tile * KEYS, T1 = (int)a.T - 1;
   const int key = j0 + wave * 32 + lane % 32;
   const bool row = key <= T1;
   const unsigned char* qb = reinterpret_cast<const unsigned char*>(a.qkv);
@@ -234,9 +236,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   // the first and last tile of queries of which some row sees one of these keys
   if (threadIdx.x < 2) reach[threadIdx.x] = threadIdx.x ? -1 : INT32_MAX;
   __syncthreads();
-  auto sees = [&](const int4& e) { return e.x < j0 + 128 && e.y > j0 && e.x < e.y; };
+  auto sees = [&](const int4& e) { return e.x < j0 + KEYS && e.y > j0 && e.x < e.y; };
   int from = INT32_MAX, upto = -1;
-  for (int i = threadIdx.x; i < qtiles; i += 64 * kAttnWaves)
+  for (int i = threadIdx.x; i < qtiles; i += 64 * NW)
     if (sees(a.range[i])) {
       from = min(from, i);
       upto = max(upto, i);
@@ -268,34 +270,35 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       TL::copy(qb + (size_t)head * D * sizeof(TS), qstride, qt * kTile, T1, to, wave, ln);
       TL::copy(gb + (size_t)head * D * sizeof(TS), gstride, qt * kTile, T1, to + TL::kBytes, wave, ln);
       const int64_t r = (int64_t)qt * kTile + ln;
+      if (wave >= 4) return;
       const void* p = wave == 0   ? (const void*)(a.lse + (int64_t)head * a.Tp + r)
                       : wave == 1 ? (const void*)(a.delta + (int64_t)head * a.Tp + r)
                       : wave == 2 ? (const void*)(a.lo + r)
                                   : (const void*)(a.hi + r);
       lds_dma4(p, to + ST::kRows + wave * 256);
     };
-    auto range_of = [&](int i) {                 // (into scalar registers)
-      const int4 x = a.range[i];
-      return make_int4(__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y),
-                       __builtin_amdgcn_readfirstlane(x.z), __builtin_amdgcn_readfirstlane(x.w));
+    // a tile's range, on its way in one register: four lanes have a part each
+    auto range_at = [&](int i) { return reinterpret_cast<const int*>(a.range + i)[lane % 4]; };
+    auto scalars = [](int x) {
+      return make_int4(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 1),
+                       __builtin_amdgcn_readlane(x, 2), __builtin_amdgcn_readlane(x, 3));
     };
-    // the tile behind (head, qt) that is to be taken; head == head0 + mine: none
-    auto advance = [&](int& head, int& qt, int4& e) {
-      do {
-        if (++qt > upto) {
-          qt = from;
-          ++head;
-        }
-        e = range_of(qt);
-      } while (head < head0 + mine && !sees(e));
+    // the tile behind (head, qt); head == head0 + mine: none
+    auto behind = [&](int& head, int& qt) {
+      if (++qt > upto) {
+        qt = from;
+        ++head;
+      }
     };
+    // What is known of the tile behind the one being copied is loaded with it,
+    // and waited for with it: by itself it kept each turn waiting.
     int head = head0, qt = from, stage = 0;
-    int4 e = range_of(qt);
+    int4 e = scalars(range_at(qt));
     copy(head, qt, at);
+    int nhead = head, nqt = qt;
+    behind(nhead, nqt);
+    int ahead = range_at(nqt);
     while (head < head0 + mine) {
-      int nhead = head, nqt = qt;
-      int4 ne;
-      advance(nhead, nqt, ne);      // (loads of its own stand before the copies, which a wait for them would wait for)
       Score sc;
       sc.init(a, head);
       wait_loads();
@@ -303,99 +306,114 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       unsigned char* Q = lds + stage * ST::kBytes;
       unsigned char* G = Q + TL::kBytes;
       stage ^= 1;
-      if (nhead < head0 + mine) copy(nhead, nqt, at + stage * ST::kBytes);
-      const bool cut = e.z > j0 || e.w < j0 + 128;
+      int4 ne = scalars(ahead);
+      while (nhead < head0 + mine && !sees(ne)) {
+        behind(nhead, nqt);
+        ne = scalars(range_at(nqt));
+      }
+      const int head1 = nhead, qt1 = nqt;
+      if (nhead < head0 + mine) {
+        copy(nhead, nqt, at + stage * ST::kBytes);
+        behind(nhead, nqt);
+        ahead = range_at(nqt);
+      }
+      const bool cut = e.z > j0 || e.w < j0 + KEYS;
       uint64_t bad = 0;
-      if (cut) bad = TL::clean(Q, bits, wave, again(lane)) | TL::clean(G, bits + 4, wave, again(lane));
-#pragma unroll 1
-      for (int rb = 0; rb < 2; ++rb) {
-        const int ln = again(lane);
-        const float* rows = reinterpret_cast<const float*>(Q + ST::kRows) + 4 * (ln / 32);
-        const float d0 = (float)(qt * kTile + 4 * (ln / 32) - key);
-        f32x16 s = f32x16{}, dp = f32x16{};
-        // (one product after the other: few registers are left beside the sums and the keys' and values' fragments)
-        Frag<TS> q[2], v;
-        TL::row_frag(Q, rb, 0, ln, q[0]);
-#pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {
-          if (i + 1 < 2 * KS) TL::row_frag(i + 1 < KS ? Q : G, rb, (i + 1) % KS, ln, q[(i + 1) % 2]);
-          if (i < KS) {
-            s = mfma32(q[i % 2], kf[i % KS], s);
-          } else {
-            if (i - KS < KS - PARKED) v = vf[i - KS];
-            dp = mfma32(q[i % 2], v, dp);
-          }
-          if (i + 1 >= 2 * KS - PARKED && i + 1 < 2 * KS) v = parked[(i + 1 - 2 * KS + PARKED) * 64 + ln];
-          __builtin_amdgcn_sched_barrier(0);
+      if (cut) {
+        bad = TL::clean(Q, bits, wave, again(lane)) | TL::clean(G, bits + 1, wave, again(lane));
+        // rows whose lse or delta is not finite count as such (rows that see nothing are among them)
+        float* r = reinterpret_cast<float*>(Q + ST::kRows);
+        const uint64_t more = __ballot(!(fabsf(r[lane]) <= FLT_MAX && fabsf(r[64 + lane]) <= FLT_MAX));
+        if (more) {
+          bad |= more;
+          lds_barrier();
+          if (wave == 0 && (more >> lane & 1)) r[lane] = r[64 + lane] = 0.f;
+          lds_barrier();
         }
+      }
+      const bool none = e.x >= j0 + 32 * wave + 32 || e.y <= j0 + 32 * wave;     // no row sees a key of this wave
+#pragma unroll 1
+      for (int rb = none ? 2 : 0; rb < 2; ++rb) {
+        const int ln = again(lane);
+        const float* rows = reinterpret_cast<const float*>(Q + ST::kRows) + 32 * rb + 4 * (ln / 32);
+        f32x16 s = f32x16{}, dp = f32x16{};
+        // the scores, then dP with the scores' probabilities beside it
+        feed<KS, AHEAD, Frag<TS>>([&](auto i, Frag<TS>& q) { TL::row_frag(Q, rb, i.value, ln, q); },
+                                  [&](auto i, Frag<TS>& q) { s = mfma32(q, kf[i.value], s); });
+        Frag<TS> v;
+        float4 four;
+        feed<KS, AHEAD, Frag<TS>>(
+            [&](auto i, Frag<TS>& q) { TL::row_frag(G, rb, i.value, ln, q); },
+            [&](auto i, Frag<TS>& q) {
+              if constexpr (i.value < KS - PARKED) v = vf[i.value];
+              dp = mfma32(q, v, dp);
+              if constexpr (i.value + 1 >= KS - PARKED && i.value + 1 < KS)
+                v = parked[(i.value + 1 - KS + PARKED) * 64 + ln];
+              if constexpr (!EX)
+                share<16, KS>(i, [&](auto e) {
+                  if constexpr (e.value % 4 == 0) four = *reinterpret_cast<const float4*>(rows + 2 * e.value);
+                  s[e.value] = __builtin_amdgcn_exp2f(fmaf(s[e.value], sc.mul, -(&four.x)[e.value % 4]));
+                });
+            });
+        if constexpr (EX) {
+          const float d0 = (float)(qt * kTile + 32 * rb + 4 * (ln / 32) - key);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 lse = *reinterpret_cast<const float4*>(rows + 32 * rb + 8 * i);
-          const float4 del = *reinterpret_cast<const float4*>(rows + 64 + 32 * rb + 8 * i);
-          const float L[4] = {lse.x, lse.y, lse.z, lse.w}, E[4] = {del.x, del.y, del.z, del.w};
+          for (int i = 0; i < 4; ++i) {
+            const float4 lse = *reinterpret_cast<const float4*>(rows + 8 * i);
+            const float4 del = *reinterpret_cast<const float4*>(rows + 64 + 8 * i);
 #pragma unroll
-          for (int e4 = 0; e4 < 4; ++e4) {
-            const int r = 4 * i + e4;
-            if constexpr (EX) {
+            for (int r = 4 * i; r < 4 * i + 4; ++r) {
               float x = s[r], y = dp[r];
-              reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 + (float)(32 * rb + sum_row(r))), L[e4],
-                                E[e4]);
+              reverse_score<TS>(x, y, sc, a.cap > 0.f, -sc.slope * fabsf(d0 + (float)sum_row(r)), (&lse.x)[r % 4],
+                                (&del.x)[r % 4]);
               s[r] = x;
               dp[r] = y;
-            } else {
-              s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.mul, -L[e4]));
-              dp[r] = s[r] * (dp[r] - E[e4]);
             }
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if (bad) {
-          branch_only();
-          const uint32_t rows32 = (uint32_t)(bad >> (32 * rb)) >> (4 * (ln / 32));
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float nan = rows32 >> sum_row(r) & 1 ? __builtin_nanf("") : 0.f;
-            s[r] += nan;
-            dp[r] += nan;
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
         if (cut) {
+          branch_only();
+          const uint32_t rows32 = (uint32_t)(bad >> (32 * rb)) >> (4 * (ln / 32));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            branch_only();
-            const int4 lo = *reinterpret_cast<const int4*>(rows + 128 + 32 * rb + 8 * i);
-            const int4 hi = *reinterpret_cast<const int4*>(rows + 192 + 32 * rb + 8 * i);
-            const int L[4] = {lo.x, lo.y, lo.z, lo.w}, U[4] = {hi.x, hi.y, hi.z, hi.w};
+            const int4 lo = *reinterpret_cast<const int4*>(rows + 128 + 8 * i);
+            const int4 hi = *reinterpret_cast<const int4*>(rows + 192 + 8 * i);
+            const float4 del = *reinterpret_cast<const float4*>(rows + 64 + 8 * i);
 #pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-              const int r = 4 * i + e4;
-              const bool seen = key >= L[e4] && key < U[e4];
-              if (!seen) s[r] = dp[r] = 0.f;
+            for (int r = 4 * i; r < 4 * i + 4; ++r) {
+              const bool seen = key >= (&lo.x)[r % 4] && key < (&hi.x)[r % 4];
+              if (rows32 >> sum_row(r) & 1) s[r] = dp[r] = __builtin_nanf("");
+              if (!seen) {
+                s[r] = 0.f;
+                dp[r] = EX ? 0.f : (&del.x)[r % 4];          // p (dP - delta) = 0 below
+              }
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
-        __builtin_amdgcn_sched_barrier(0);
-        Frag<TS> x[2], y[2], p, ds;
-        TL::col_frag(G, 0, 2 * rb, ln, x[0]);
-        TL::col_frag(Q, 0, 2 * rb, ln, y[0]);
-#pragma unroll
-        for (int i = 0; i < 2 * F; ++i) {
-          const int st = i / F, f = i % F;
-          if (f == 0) {
-            sums_frag(s, st, p);
-            sums_frag(dp, st, ds);
-          }
-          if (i + 1 < 2 * F) {
-            TL::col_frag(G, (i + 1) % F, 2 * rb + (i + 1) / F, ln, x[(i + 1) % 2]);
-            TL::col_frag(Q, (i + 1) % F, 2 * rb + (i + 1) / F, ln, y[(i + 1) % 2]);
-          }
-          dv[f] = mfma32(x[i % 2], p, dv[f]);
-          dk[f] = mfma32(y[i % 2], ds, dk[f]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        // dv, with dS = p (dP - delta) beside it, then dk
+        Frag<TS> p;
+        feed<2 * F, AHEAD, Frag<TS>>(
+            [&](auto i, Frag<TS>& x) { TL::col_frag(G, i.value % F, 2 * rb + i.value / F, ln, x); },
+            [&](auto i, Frag<TS>& x) {
+              if constexpr (i.value % F == 0) sums_frag(s, i.value / F, p);
+              dv[i.value % F] = mfma32(x, p, dv[i.value % F]);
+              if constexpr (!EX)
+                share<16, 2 * F>(i, [&](auto e) {
+                  if constexpr (e.value % 4 == 0) four = *reinterpret_cast<const float4*>(rows + 64 + 2 * e.value);
+                  dp[e.value] = s[e.value] * (dp[e.value] - (&four.x)[e.value % 4]);
+                });
+            });
+        feed<2 * F, AHEAD, Frag<TS>>(
+            [&](auto i, Frag<TS>& x) { TL::col_frag(Q, i.value % F, 2 * rb + i.value / F, ln, x); },
+            [&](auto i, Frag<TS>& x) {
+              if constexpr (i.value % F == 0) sums_frag(dp, i.value / F, p);
+              dk[i.value % F] = mfma32(x, p, dk[i.value % F]);
+            });
       }
-      head = nhead;
-      qt = nqt;
+      head = head1;
+      qt = qt1;
       e = ne;
     }
   }
@@ -436,14 +454,14 @@ __global__ __launch_bounds__(256) void k_attn_join(int64_t T, int row, int parts
 
 constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
-// Parts of a group's heads for dk and dv: 512 workgroups fill the chip's 256 CUs
-// twice over; with fewer, a group's heads are divided among several, whose sums
+// Parts of a group's heads for dk and dv: the chip holds 512 workgroups of four
+// waves, of unlike lengths where masks cut; with less than twice as many, a group's heads are divided among several, whose sums
 // are then added.
-int parts_of(int64_t T, int Hq, int Hkv) {
-  const int64_t wg = (T + 127) / 128 * Hkv;
+int parts_of(int64_t T, int Hq, int Hkv, int keys) {
+  const int64_t wg = (T + keys - 1) / keys * Hkv;
   const int g = Hq / Hkv;
   for (int p = 1; p < g; ++p)
-    if (g % p == 0 && wg * p >= 512) return p;
+    if (g % p == 0 && wg * p * keys >= 1024 * 128) return p;
   return g;
 }
 
@@ -456,8 +474,9 @@ template <typename TS, int D, bool EX> hipError_t run_bwd(AttnArgs a, char* ws, 
   a.part = reinterpret_cast<float*>(ws + heads + 2 * rows + up((size_t)a.Tp / kTile * 16));
   k_attn_prep<TS, D><<<dim3((unsigned)(a.Tp / kTile), a.Hq + 1), dim3(256), 0, s>>>(a, delta, lo, hi, range);
   a.delta = delta, a.lo = lo, a.hi = hi, a.range = range;
-  const unsigned tiles = (unsigned)((a.T + 127) / 128);
-  k_attn_dkv<TS, D, EX><<<dim3(tiles * a.Hkv * a.parts), dim3(64 * kAttnWaves), 0, s>>>(a);
+  constexpr int NW = dkv_waves(sizeof(TS) == 4, D);
+  const unsigned tiles = (unsigned)((a.T + 127) / 128), ktiles = (unsigned)((a.T + 32 * NW - 1) / (32 * NW));
+  k_attn_dkv<TS, D, EX><<<dim3(ktiles * a.Hkv * a.parts), dim3(64 * NW), 0, s>>>(a);
   if (a.parts > 1) {
     const int row = 2 * a.Hkv * D;
     k_attn_join<TS><<<dim3((unsigned)((a.T * row / 8 + 255) / 256)), dim3(256), 0, s>>>(
@@ -479,9 +498,9 @@ template <typename TS> hipError_t run_bwd_of(int D, const AttnArgs& a, char* ws,
 
 }  // namespace
 
-size_t attn_bwd_ws_bytes(int64_t T, int Hq, int Hkv, int D) {
+size_t attn_bwd_ws_bytes(int state_dtype, int64_t T, int Hq, int Hkv, int D) {
   const int64_t Tp = (T + kTile - 1) / kTile * kTile;
-  const int parts = parts_of(T, Hq, Hkv);
+  const int parts = parts_of(T, Hq, Hkv, 32 * dkv_waves(state_dtype == XHC_F32, D));
   return up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) +
          (parts > 1 ? (size_t)parts * T * 2 * Hkv * D * 4 : 0);
 }
@@ -500,7 +519,7 @@ hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qk
   a.dqkv = dqkv;
   a.T = d->T, a.S = d->S, a.Tp = (d->T + kTile - 1) / kTile * kTile;
   a.Hq = h->Hq, a.Hkv = h->Hkv, a.window = h->window;
-  a.parts = parts_of(d->T, h->Hq, h->Hkv);
+  a.parts = parts_of(d->T, h->Hq, h->Hkv, 32 * dkv_waves(d->state_dtype == XHC_F32, h->D));
   a.scale = h->scale, a.cap = h->cap;
   return d->state_dtype == XHC_BF16 ? run_bwd_of<uint16_t>(h->D, a, static_cast<char*>(ws), s)
                                     : run_bwd_of<float>(h->D, a, static_cast<char*>(ws), s);

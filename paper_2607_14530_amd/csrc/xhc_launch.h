@@ -335,7 +335,7 @@ hipError_t launch_attn(const xhc_dims* d, const xhc_heads* h, const void* qkv, c
                        const float* slopes, void* out, void* saved, hipStream_t s);
 size_t attn_lse_bytes(int64_t T, int Hq);
 size_t attn_saved_bytes(int state_dtype, int64_t T, int Hq, int D);
-size_t attn_bwd_ws_bytes(int64_t T, int Hq, int Hkv, int D);
+size_t attn_bwd_ws_bytes(int state_dtype, int64_t T, int Hq, int Hkv, int D);
 hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
                            const float* slopes, const void* out, const void* saved, const void* dout, void* dqkv,
                            void* ws, hipStream_t s);
