@@ -305,6 +305,11 @@ __device__ __forceinline__ void pack_frag(const float (&x)[8], Frag32& f) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) f.v[j] = x[j];
 }
+// lane i's value, in scalar registers
+__device__ __forceinline__ int64_t scalar64(int64_t x, int i) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, i);
+  return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 | lo;
+}
 // lane K of this lane's row of 16
 template <int K> __device__ __forceinline__ float row_lane(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + K, 0xF, 0xF, true));
@@ -329,7 +334,7 @@ template <int D> struct Raw {
       for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
     }
   }
-  __device__ __forceinline__ void load(const unsigned char* p, int lane) {
+  __device__ __forceinline__ void load(const unsigned char* p, uint32_t lane) {
     using BL = Block<D>;
 #pragma unroll
     for (int h = 0; h < 2; ++h) words<BL::G>(p + BL::kKeys + (h * 64 + lane) * BL::G * 4, k[h]);
@@ -341,7 +346,7 @@ template <int D> struct Raw {
         words<2>(p + BL::kValues + (at * 64 + lane * 2) * 4, v + at);
     }
     // of a row of 16 lanes the first 4 G have a word each
-    const int s = (lane / 16 * 4 * BL::G + (lane % 16 < 4 * BL::G ? lane % 16 : 0)) * 4;
+    const uint32_t s = (lane / 16 * 4 * BL::G + (lane % 16 < 4 * BL::G ? lane % 16 : 0)) * 4;
     ks = *reinterpret_cast<const uint32_t*>(p + BL::kKeyScales + s);
     vs = *reinterpret_cast<const uint32_t*>(p + BL::kValueScales + s);
   }
@@ -383,7 +388,7 @@ __device__ __forceinline__ Sequence sequence(const CacheArgs& a, int b, int rows
 // group) are the columns of 16x16x32 products.
 constexpr int attend_wgs(bool f32, int rows) { return rows == 16 ? (f32 ? 2 : 3) : (f32 ? 1 : 2); }   // of a CU
 
-template <typename TS, int D, int RT>
+template <typename TS, int D, int RT, bool EX>
 __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_cache_attend(CacheArgs a) {
   using BL = Block<D>;
   constexpr int G = BL::G, W = BL::W, ROWS = 16 * RT, LD = D + 4;
@@ -393,55 +398,80 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = a.Hq / a.Hkv, r16 = lane % 16;
 
-  // units in front of each thread's share of the sequences, and of all
-  const int share = (a.B + 255) / 256, b0 = tid * share, b1 = min(a.B, b0 + share);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Sequence s = sequence(a, b, ROWS);
-    mine += (int64_t)s.tiles * a.Hkv * s.blocks;
-  }
-  scan[tid] = mine;
-  __syncthreads();
-  for (int d = 1; d < 256; d *= 2) {
-    const int64_t x = tid >= d ? scan[tid - d] : 0;
-    __syncthreads();
-    scan[tid] += x;
-    __syncthreads();
-  }
-  const int64_t all = scan[255];
-  // at least four blocks a workgroup, one for each wave
-  int64_t run = (all + gridDim.x - 1) / gridDim.x;
-  if (run < 4) run = 4;
-  if (blockIdx.x == 0) {
-    int64_t at = scan[tid] - mine;
-    for (int b = b0; b < b1; ++b) {
-      const Sequence s = sequence(a, b, ROWS);
-      a.where[2 * b] = at;
-      a.where[2 * b + 1] = s.blocks;
-      at += (int64_t)s.tiles * a.Hkv * s.blocks;
+  // The run's first unit's sequence b, and the units in front of that.
+  int b;
+  int64_t u0, u1, before;
+  auto runs = [&](int64_t all) {
+    // at least four blocks a workgroup, one for each wave
+    int64_t run = (all + gridDim.x - 1) / gridDim.x;
+    if (run < 4) run = 4;
+    if (blockIdx.x == 0 && tid == 0) a.where[2 * (int64_t)a.B] = run;
+    u0 = (int64_t)blockIdx.x * run;
+    u1 = u0 + run < all ? u0 + run : all;
+  };
+  auto units = [&](int i) {
+    const Sequence s = sequence(a, i, ROWS);
+    return (int64_t)s.tiles * a.Hkv * s.blocks;
+  };
+  auto note = [&](int i, int64_t at) {
+    a.where[2 * i] = at;
+    a.where[2 * i + 1] = sequence(a, i, ROWS).blocks;
+  };
+  if (a.B <= 64) {                               // each wave by itself, a lane a sequence
+    const int64_t mine = lane < a.B ? units(lane) : 0;
+    int64_t sum = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t x = __shfl_up((long long)sum, d);
+      if (lane >= d) sum += x;
     }
-    if (tid == 0) a.where[2 * (int64_t)a.B] = run;
+    runs(scalar64(sum, 63));
+    if (blockIdx.x == 0 && wave == 0 && lane < a.B) note(lane, sum - mine);
+    if (u0 >= u1) return;
+    b = __popcll(__ballot(sum <= u0));
+    before = b > 0 ? scalar64(sum, b - 1) : 0;
+  } else {
+    // the workgroup's threads have a share of the sequences each
+    const int share = (a.B + 255) / 256, b0 = tid * share, b1 = min(a.B, b0 + share);
+    int64_t mine = 0;
+    for (int i = b0; i < b1; ++i) mine += units(i);
+    scan[tid] = mine;
+    __syncthreads();
+    for (int d = 1; d < 256; d *= 2) {
+      const int64_t x = tid >= d ? scan[tid - d] : 0;
+      __syncthreads();
+      scan[tid] += x;
+      __syncthreads();
+    }
+    runs(scan[255]);
+    if (blockIdx.x == 0) {
+      int64_t at = scan[tid] - mine;
+      for (int i = b0; i < b1; ++i) {
+        note(i, at);
+        at += units(i);
+      }
+    }
+    if (u0 >= u1) return;
+    int owner = 0;                               // the first thread whose share ends behind u0
+    for (int upto = 255; owner < upto;) {
+      const int c = (owner + upto) / 2;
+      if (scan[c] > u0)
+        upto = c;
+      else
+        owner = c + 1;
+    }
+    before = owner > 0 ? scan[owner - 1] : 0;
+    for (b = owner * share;; ++b) {
+      const int64_t n = units(b);
+      if (before + n > u0) break;
+      before += n;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    before = scalar64(before, 0);
   }
-  const int64_t u0 = (int64_t)blockIdx.x * run, u1 = u0 + run < all ? u0 + run : all;
-  if (u0 >= u1) return;
-  // the sequence of unit u0, and the units in front of it
-  int owner = 0;                                 // the first thread whose share ends behind u0
-  for (int upto = 255; owner < upto;) {
-    const int c = (owner + upto) / 2;
-    if (scan[c] > u0)
-      upto = c;
-    else
-      owner = c + 1;
-  }
-  int64_t before = owner > 0 ? scan[owner - 1] : 0;
-  int b = owner * share;
+  u0 = scalar64(u0, 0);
+  u1 = scalar64(u1, 0);
   Sequence sq = sequence(a, b, ROWS);
-  for (;;) {
-    const int64_t n = (int64_t)sq.tiles * a.Hkv * sq.blocks;
-    if (before + n > u0) break;
-    before += n;
-    sq = sequence(a, ++b, ROWS);
-  }
 
   for (int64_t u = u0; u < u1;) {
     while (u >= before + (int64_t)sq.tiles * a.Hkv * sq.blocks) {
@@ -499,21 +529,31 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
       if (lane < n) mypage = pages[token0(i0 + lane) / a.page];
       // the blocks that are there, one bit each
       uint64_t left = __ballot(mypage >= 0 && mypage < a.npages);
-      Raw<D> raw, nextraw;
-      auto fetch = [&](Raw<D>& r, int i) {
-        const int pg = __builtin_amdgcn_readlane(mypage, i);
-        r.load(block_at<D>(a, pg, head, token0(i0 + i) % a.page), lane);
+      // three of them on their way or worked on, where the registers hold them
+      // (one ahead of the present one does not cover the way from memory)
+      constexpr int RING = RT == 1 && !(EX && D == 128) ? 3 : 2;
+      Raw<D> ring[RING];
+      int in[RING];
+      const unsigned char* from_at = a.pool;
+      auto fetch = [&](Raw<D>& r, int& i) {
+        i = -1;
+        if (left) {
+          i = __builtin_ctzll(left);
+          left &= left - 1;
+          const int pg = __builtin_amdgcn_readlane(mypage, i);
+          from_at = block_at<D>(a, pg, head, token0(i0 + i) % a.page);
+        }
+        // (behind the last block the same once more: with loads that are always
+        // sent the compiler knows how many of them may be on their way)
+        r.load(from_at, (uint32_t)again(lane));
       };
-      if (left) fetch(raw, __builtin_ctzll(left));
-      while (left) {
-        const int i = __builtin_ctzll(left);
-        left &= left - 1;
-        if (left) fetch(nextraw, __builtin_ctzll(left));
+      auto work = [&](const Raw<D>& raw, int i) __attribute__((always_inline)) {
         const int j0 = token0(i0 + i);
         const bool cut = j0 + kBlock > least || j0 < most;   // some row does not see all of the block
         f32x4 s[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{};
+        __builtin_amdgcn_sched_barrier(0);
         const float kl = bf_lo(raw.ks), kh = bf_hi(raw.ks), vl = bf_lo(raw.vs), vh = bf_hi(raw.vs);
         unroll<2 * G>([&](auto hg) {
           constexpr int h = hg.value / G, k = hg.value % G;
@@ -528,20 +568,31 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
             s[rt][h][2] = fmaf(row_lane<W0 + 1>(kl), part[2], s[rt][h][2]);
             s[rt][h][3] = fmaf(row_lane<W0 + 1>(kh), part[3], s[rt][h][3]);
           }
+          if constexpr (hg.value % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         });
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          float top = -__builtin_huge_valf();
+          const int first = j0 + 4 * (again(lane) / 16);     // this lane's tokens: first + 16 (e / 4) + e % 4
+          if constexpr (EX) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float x = s[rt][e / 4][e % 4];
-            x = a.cap > 0.f ? cap * tanh_of<TS>(x * mul) : x * mul;
-            const int j = j0 + 16 * (e / 4) + 4 * (lane / 16) + e % 4;
-            if (a.slopes) x = fmaf(-slope[rt], (float)(see[rt] - 1 - j), x);
-            if (cut && !(j < see[rt] && j >= low[rt])) x = -__builtin_huge_valf();
-            s[rt][e / 4][e % 4] = x;
-            top = fmaxf(top, x);
+            for (int e = 0; e < 8; ++e) {
+              float x = s[rt][e / 4][e % 4];
+              x = a.cap > 0.f ? cap * tanh_of<TS>(x * mul) : x * mul;
+              s[rt][e / 4][e % 4] = fmaf(-slope[rt], (float)(see[rt] - 1 - first - 16 * (e / 4) - e % 4), x);
+            }
           }
+          if (cut) {
+            branch_only();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int j = first + 16 * (e / 4) + e % 4;
+              if (!(j < see[rt] && j >= low[rt])) s[rt][e / 4][e % 4] = -__builtin_huge_valf();
+            }
+          }
+          float top = s[rt][0][0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) top = fmaxf(top, s[rt][e / 4][e % 4]);
+          if constexpr (!EX) top *= mul;         // (the raw products so far; exp takes the factor with it)
           top = max_quarters(top);
           if (__any(top > m[rt] + 8.f)) {        // (as in the attention of token rows)
             const float to = top > m[rt] + 8.f ? top : m[rt];
@@ -556,7 +607,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
           const float ref = m[rt] == -__builtin_huge_valf() ? 0.f : m[rt];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float x = __builtin_amdgcn_exp2f(s[rt][e / 4][e % 4] - ref);
+            const float x = __builtin_amdgcn_exp2f(EX ? s[rt][e / 4][e % 4] - ref : fmaf(s[rt][e / 4][e % 4], mul, -ref));
             s[rt][e / 4][e % 4] = x;
             l[rt] += x;
           }
@@ -577,19 +628,33 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
               p[4 * h + 3] = row_lane<W0 + 1>(vh) * s[rt][h][3];
             });
             if (cut) {                           // what is not seen may have any scale, NaN too
+              branch_only();
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int j = j0 + 16 * (e / 4) + 4 * (lane / 16) + e % 4;
-                if (!(j < see[rt] && j >= low[rt])) p[e] = 0.f;
-              }
+              for (int e = 0; e < 8; ++e)
+                if (s[rt][e / 4][e % 4] == 0.f) p[e] = 0.f;
             }
             Frag<TS> pf;
             pack_frag(p, pf);
             o[rt][2 * k] = mfma16(x0, pf, o[rt][2 * k]);
             o[rt][2 * k + 1] = mfma16(x1, pf, o[rt][2 * k + 1]);
           }
+          __builtin_amdgcn_sched_barrier(0);
         });
-        raw = nextraw;
+      };
+      if (!left) continue;
+      unroll<RING>([&](auto k) { fetch(ring[k.value], in[k.value]); });
+      for (;;) {
+        work(ring[0], in[0]);
+        fetch(ring[0], in[0]);
+        if (in[1] < 0) break;
+        work(ring[1], in[1]);
+        fetch(ring[1], in[1]);
+        if constexpr (RING == 3) {
+          if (in[2] < 0) break;
+          work(ring[2], in[2]);
+          fetch(ring[2], in[2]);
+        }
+        if (in[0] < 0) break;
       }
     }
 
@@ -643,12 +708,12 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
 }
 
 // Rows of the output from the places of their segments' runs, where there are
-// several: a lane has eight channels of one, and its workgroup's four waves
-// share the runs.
-template <typename TS, int D>
-__global__ __launch_bounds__(256) void k_cache_join(CacheArgs a, int ROWS, int64_t wgs) {
+// several: a lane has eight channels of one, and its workgroup's W waves share
+// the runs.
+template <typename TS, int D, int W>
+__global__ __launch_bounds__(64 * W) void k_cache_join(CacheArgs a, int ROWS, int64_t wgs) {
   constexpr int P = D / 8;
-  __shared__ float red[4][10][64];
+  __shared__ float red[W][10][64];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = a.Hq / a.Hkv;
   const int64_t t = blockIdx.x;
   const int b = sequence_of(a.starts, a.B, t, lane);
@@ -675,7 +740,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a, int ROWS, int64
   };
   if (is) {
 #pragma unroll 4
-    for (int64_t w = w0 + wave; w <= w1; w += 4) {
+    for (int64_t w = w0 + wave; w <= w1; w += W) {
       const float2 ml = a.ml[place(w)];
       float y[8];
       Vec8<float>::load(a.part + place(w) * D + c, y);
@@ -688,7 +753,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a, int ROWS, int64
   red[wave][9][lane] = sum;
   __syncthreads();
   if (wave != 0 || !is) return;
-  for (int w = 1; w < 4; ++w) {
+  for (int w = 1; w < W; ++w) {
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = red[w][e][lane];
@@ -798,19 +863,22 @@ hipError_t launch_cache_attend(const xhc_dims* d, const xhc_heads* h, const xhc_
   a.where = reinterpret_cast<int64_t*>(p + up(slots * h->D * 4) + up(slots * 8));
   const dim3 grid((unsigned)wgs), block(256), tokens((unsigned)d->T, (unsigned)((h->Hq * (h->D / 8) + 63) / 64));
   with_width(h->D, [&](auto D) {
-    if (d->state_dtype == XHC_BF16) {
+    auto run = [&](auto type, auto rt, auto ex) {
+      k_cache_attend<decltype(type), D.value, rt.value, ex.value != 0><<<grid, block, 0, s>>>(a);
+    };
+    auto of = [&](auto type) {
+      const bool ex = a.cap > 0.f || slopes;
       if (rows == 16)
-        k_cache_attend<uint16_t, D.value, 1><<<grid, block, 0, s>>>(a);
+        ex ? run(type, Int<1>{}, Int<1>{}) : run(type, Int<1>{}, Int<0>{});
       else
-        k_cache_attend<uint16_t, D.value, 2><<<grid, block, 0, s>>>(a);
-      k_cache_join<uint16_t, D.value><<<tokens, block, 0, s>>>(a, rows, wgs);
-    } else {
-      if (rows == 16)
-        k_cache_attend<float, D.value, 1><<<grid, block, 0, s>>>(a);
+        ex ? run(type, Int<2>{}, Int<1>{}) : run(type, Int<2>{}, Int<0>{});
+      // (few tokens have many runs each: 16 waves take 5 us where four take 13, at one token of 131072)
+      if (d->T <= 16)
+        k_cache_join<decltype(type), D.value, 16><<<tokens, dim3(1024), 0, s>>>(a, rows, wgs);
       else
-        k_cache_attend<float, D.value, 2><<<grid, block, 0, s>>>(a);
-      k_cache_join<float, D.value><<<tokens, block, 0, s>>>(a, rows, wgs);
-    }
+        k_cache_join<decltype(type), D.value, 4><<<tokens, block, 0, s>>>(a, rows, wgs);
+    };
+    d->state_dtype == XHC_BF16 ? of(uint16_t{}) : of(float{});
   });
   return hipGetLastError();
 }
