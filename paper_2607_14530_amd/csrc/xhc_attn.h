@@ -281,7 +281,7 @@ __device__ __forceinline__ int2 span_of(const AttnArgs& a, int t) {
     const int T = (int)a.T;
     return make_int2(min(max(s.x, 0), T), min(max(s.y, 0), T));
   }
-  int lo = t - (int)(t % a.S);
+  int lo = t - (int)((uint32_t)t % (uint32_t)a.S);       // (S <= T where there are tokens)
   if (a.window > 0 && t - a.window + 1 > lo) lo = t - a.window + 1;
   return make_int2(lo, t + 1);
 }
@@ -291,24 +291,27 @@ __device__ __forceinline__ float scalar(float x) {
   return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x)));
 }
 
-// Scores in units of log2 e (their softmax then takes exp2), in place of the
-// raw products of one block of 32 keys x 32 queries or queries x keys:
-// (cap tanh(scale x / cap) - slope |i - j|) log2 e; der: d score / d (scale x),
-// which is 1 without a cap.
-struct Score {
-  float mul, cap, slope;    // mul: scale log2 e, or 2 log2 e scale / cap
+// Scores in units of log2 e (their softmax then takes exp2), of raw products x:
+// (cap tanh(scale x / cap) - slope |i - j|) log2 e, or scale x log2 e for the first.
+template <typename TS> struct Score {
+  float mul, cap, slope;    // without a cap mul is scale log2 e; with one what tanh_of takes x with
   __device__ __forceinline__ void init(const AttnArgs& a, int head) {
     cap = scalar(a.cap * kLog2e);
-    mul = scalar(a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e);
+    mul = scalar(a.cap > 0.f ? a.scale / a.cap * (sizeof(TS) == 2 ? 2.f * kLog2e : 1.f) : a.scale * kLog2e);
     slope = a.slopes ? scalar(a.slopes[head] * kLog2e) : 0.f;
   }
+  // 1 / (1 + exp 2z), z = scale x / cap: tanh z = 1 - 2 of it.  Off by some 2^-23
+  // of 1, where a bf16 product's factors are off by 2^-9 of it.
+  __device__ __forceinline__ float share_of(float x) const {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * mul));
+  }
+  __device__ __forceinline__ float tanh_of(float x) const {
+    if constexpr (sizeof(TS) == 2)
+      return fmaf(-2.f, share_of(x), 1.f);
+    else
+      return tanhf(x * mul);
+  }
 };
-template <typename TS> __device__ __forceinline__ float tanh_of(float x);
-// 1 - 2 / (1 + exp 2x): off by some 2^-23 of 1, where a bf16 product's factors are off by 2^-9 of it
-template <> __device__ __forceinline__ float tanh_of<uint16_t>(float x) {
-  return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
-}
-template <> __device__ __forceinline__ float tanh_of<float>(float x) { return tanhf(x); }
 
 __device__ __forceinline__ float max_halves(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -318,30 +321,47 @@ __device__ __forceinline__ float max_halves(float v) {
 // the row of sum r of a block, less 4 (lane / 32)
 __host__ __device__ __forceinline__ constexpr int sum_row(int r) { return 8 * (r / 4) + r % 4; }
 
-// The workgroup's extremes of its rows' spans: x min lo, y max hi of the rows
-// that see keys (x >= y where none does), z max lo, w min hi of all.  Rows
-// behind the last are left out.  own: x and y of the wave's rows.
-__device__ __forceinline__ int4 attn_extremes(int2 s, bool row, int4* red, int wave, int lane, int2& own) {
-  const bool some = row && s.x < s.y;
-  int4 e = make_int4(some ? s.x : INT32_MAX, some ? s.y : 0, row ? (some ? s.x : INT32_MAX) : 0,
-                     row ? (some ? s.y : 0) : INT32_MAX);
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    e.x = min(e.x, __shfl_xor(e.x, d));
-    e.y = max(e.y, __shfl_xor(e.y, d));
-    e.z = max(e.z, __shfl_xor(e.z, d));
-    e.w = min(e.w, __shfl_xor(e.w, d));
+// NC of k_attn and k_attn_dq: two where there is less than a workgroup a CU
+// (T = 777, Hq = 6, D = 96, fp32: 94 -> 68 us forward; at 512 workgroups, T =
+// 2048, Hq = 32, D = 128, the extra copies cost more, 90 -> 95).
+inline int attn_parts(int64_t T, int Hq) { return (T + 127) / 128 * Hq <= 256 ? 2 : 1; }
+
+// least of the 32 lanes of a half wave, in all of them
+__device__ __forceinline__ int half_min(int v) {
+  v = min(v, __builtin_amdgcn_update_dpp(v, v, 0xB1, 0xF, 0xF, false));    // quad_perm 1,0,3,2
+  v = min(v, __builtin_amdgcn_update_dpp(v, v, 0x4E, 0xF, 0xF, false));    // quad_perm 2,3,0,1
+  v = min(v, __builtin_amdgcn_update_dpp(v, v, 0x141, 0xF, 0xF, false));   // row_half_mirror
+  v = min(v, __builtin_amdgcn_update_dpp(v, v, 0x140, 0xF, 0xF, false));   // row_mirror
+  const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  return min((int)r[0], (int)r[1]);
+}
+
+// The extremes of the spans of the workgroup's rows t0 .. t0 + rows - 1 (a
+// lane's own: s, of row t0 + 32 RW ..): x min lo, y max hi of the rows that see
+// keys (x >= y where none does), z max lo, w min hi of all.  Rows behind the
+// last are left out.  own: x and y of the wave's rows, from row w0 on.
+// Causal spans ascend, so that the first and the last row have all four.
+__device__ __forceinline__ int4 attn_extremes(const AttnArgs& a, int t0, int rows, int w0, int2 s, bool row, int4* red,
+                                              int wave, int lane, int2& own) {
+  if (!a.span) {
+    const int T1 = (int)a.T - 1, t1 = min(t0 + rows - 1, T1), w1 = min(w0 + 31, T1);
+    const int2 first = span_of(a, t0), last = span_of(a, t1);
+    own = w0 <= T1 ? make_int2(span_of(a, w0).x, w1 + 1) : make_int2(INT32_MAX, 0);
+    return make_int4(first.x, last.y, last.x, first.y);
   }
-  own = make_int2(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y));
-  if (lane == 0) red[wave] = e;
+  const bool some = row && s.x < s.y;
+  const int x = half_min(some ? s.x : INT32_MAX), y = -half_min(some ? -s.y : 0),
+            z = -half_min(row ? (some ? -s.x : -INT32_MAX) : 0), w = half_min(row ? (some ? s.y : 0) : INT32_MAX);
+  own = make_int2(__builtin_amdgcn_readfirstlane(x), __builtin_amdgcn_readfirstlane(y));
+  if (lane == 0) red[wave] = make_int4(x, y, z, w);
   __syncthreads();
-  e = red[0];
+  int4 e = red[0];
 #pragma unroll
-  for (int w = 1; w < kAttnWaves; ++w) {
-    e.x = min(e.x, red[w].x);
-    e.y = max(e.y, red[w].y);
-    e.z = max(e.z, red[w].z);
-    e.w = min(e.w, red[w].w);
+  for (int i = 1; i < kAttnWaves; ++i) {
+    e.x = min(e.x, red[i].x);
+    e.y = max(e.y, red[i].y);
+    e.z = max(e.z, red[i].z);
+    e.w = min(e.w, red[i].w);
   }
   return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y),
                    __builtin_amdgcn_readfirstlane(e.z), __builtin_amdgcn_readfirstlane(e.w));

@@ -14,22 +14,29 @@ namespace {
 
 constexpr float kNoKey = -__builtin_huge_valf();
 
-template <typename TS, int D, bool EX>
+// With NC = 2 a workgroup takes 64 queries, and two waves share 32 of them: each
+// has one block of 32 keys of every tile, and their sums are joined at the end.
+// That halves the way through the longest rows' keys, which counts where the
+// chip holds all workgroups at once.
+// MODE: 0 products times a factor, 1 capped, 2 with a bias or (fp32) capped
+template <typename TS, int D, int MODE, int NC>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn(AttnArgs a) {
   using TL = Tile<TS, D>;
   constexpr int KS = D / 16, F = D / 32, AHEAD = sizeof(TS) == 2 ? 4 : 2;
+  constexpr int ROWS = 128 / NC, RW = kAttnWaves / NC, NB = 2 / NC;   // blocks of keys of a wave
   __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
   __shared__ int4 red[kAttnWaves];
   __shared__ uint64_t bits;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
-  attn_place(a.Hq, (int)((a.T + 127) / 128), head, tile);
+  attn_place(a.Hq, (int)((a.T + ROWS - 1) / ROWS), head, tile);
+  const int kc = NC == 1 ? 0 : wave / RW;        // which of the keys' blocks
   const int kvh = head / (a.Hq / a.Hkv), H = a.Hq + 2 * a.Hkv;
-  const int t = tile * 128 + wave * 32 + lane % 32, T1 = (int)a.T - 1;
+  const int t = tile * ROWS + wave % RW * 32 + lane % 32, T1 = (int)a.T - 1;
   const bool row = t <= T1;
   const int2 see = span_of(a, t);
   int2 own;
-  const int4 ex = attn_extremes(see, row, red, wave, lane, own);
+  const int4 ex = attn_extremes(a, tile * ROWS, ROWS, tile * ROWS + wave % RW * 32, see, row, red, wave, lane, own);
   const uint32_t stride = (uint32_t)H * D * sizeof(TS);
   const unsigned char* base = reinterpret_cast<const unsigned char*>(a.qkv);
   const unsigned char* kb = base + (size_t)(a.Hq + kvh) * D * sizeof(TS);
@@ -42,7 +49,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   float m = kNoKey, l = 0.f;
   const int first = ex.x / kTile, end = (ex.y + kTile - 1) / kTile;
   if (ex.x < ex.y) {
-    Score sc;
+    Score<TS> sc;
     sc.init(a, head);
     Frag<TS> q[KS];
     const TS* qp = reinterpret_cast<const TS*>(base) + (int64_t)(row ? t : T1) * H * D + head * D;
@@ -65,35 +72,29 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       uint64_t bad = 0;
       if (cut) bad = TL::clean(V, &bits, wave, again(lane));
       if (j0 >= own.y || j0 + kTile <= own.x) continue;     // no row of this wave sees a key of the tile
-      f32x16 s[2] = {f32x16{}, f32x16{}};
+      f32x16 s[NB];
+#pragma unroll
+      for (int rb = 0; rb < NB; ++rb) s[rb] = f32x16{};
       int ln = again(lane);
-      feed<2 * KS, AHEAD, Frag<TS>>(
-          [&](auto i, Frag<TS>& k) { TL::row_frag(K, i.value / KS, i.value % KS, ln, k); },
+      feed<NB * KS, AHEAD, Frag<TS>>(
+          [&](auto i, Frag<TS>& k) { TL::row_frag(K, kc + i.value / KS, i.value % KS, ln, k); },
           [&](auto i, Frag<TS>& k) { s[i.value / KS] = mfma32(k, q[i.value % KS], s[i.value / KS]); });
-      // a lane's keys: j0 + 32 rb + sum_row(r) + 4 (lane / 32)
-      if (EX && a.cap > 0.f) {
+      const int j1 = j0 + 32 * kc + 4 * (lane / 32);          // a lane's keys: j1 + 32 rb + sum_row(r)
+      if constexpr (MODE == 2) {
+        const float d0 = (float)(t - j1);
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
+        for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[rb][r] = sc.cap * tanh_of<TS>(s[rb][r] * sc.mul);
-      } else if (EX) {
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[rb][r] *= sc.mul;
-      }
-      if (EX && a.slopes) {
-        const float d0 = (float)(t - j0 - 4 * (lane / 32));
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[rb][r] = fmaf(-sc.slope, fabsf(d0 - (float)(32 * rb + sum_row(r))), s[rb][r]);
+          for (int r = 0; r < 16; ++r) {
+            const float x = a.cap > 0.f ? sc.cap * sc.tanh_of(s[rb][r]) : s[rb][r] * sc.mul;
+            s[rb][r] = fmaf(-sc.slope, fabsf(d0 - (float)(32 * rb + sum_row(r))), x);
+          }
       }
       if (cut) {
         branch_only();
-        const int lo = see.x - j0 - 4 * (lane / 32), hi = see.y - j0 - 4 * (lane / 32);
+        const int lo = see.x - j1, hi = see.y - j1;
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
+        for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int j = 32 * rb + sum_row(r);
@@ -101,8 +102,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
           }
         if (bad) {
 #pragma unroll
-          for (int rb = 0; rb < 2; ++rb) {
-            const uint32_t keys = (uint32_t)(bad >> (32 * rb)) >> (4 * (lane / 32));
+          for (int rb = 0; rb < NB; ++rb) {
+            const uint32_t keys = (uint32_t)(bad >> (32 * (kc + rb))) >> (4 * (lane / 32));
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if ((keys >> sum_row(r) & 1) && s[rb][r] != kNoKey) s[rb][r] = __builtin_nanf("");
@@ -111,11 +112,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       }
       float top = s[0][0];
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb)
+      for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[rb][r]);
       top = max_halves(top);
-      if (!EX) top *= sc.mul;                               // (s: still the raw products, mul > 0)
+      // (s: still the raw products where the scores rise with them)
+      if (MODE == 0) top *= sc.mul;
+      if (MODE == 1 && top != kNoKey) top = fmaf(-2.f * sc.cap, sc.share_of(top), sc.cap);
       // The row's reference only follows its maximum when that is 2^8 above it:
       // probabilities up to 256 are as exact, and sums are rarely rescaled.
       if (__any(top > m + 8.f)) {
@@ -130,14 +133,19 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       }
       const float ref = m == kNoKey ? 0.f : m;              // a row that has seen nothing: exp2(-inf) = 0
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb)
+      for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[rb][r] = __builtin_amdgcn_exp2f(EX ? s[rb][r] - ref : fmaf(s[rb][r], sc.mul, -ref));
+        for (int r = 0; r < 16; ++r) {
+          const float x = s[rb][r];
+          s[rb][r] = __builtin_amdgcn_exp2f(MODE == 2   ? x - ref
+                                            : MODE == 0 ? fmaf(x, sc.mul, -ref)
+                                                        : fmaf(-2.f * sc.cap, sc.share_of(x), sc.cap - ref));
+          if (MODE == 1 && cut && x == kNoKey) s[rb][r] = 0.f;           // (the cap has its say there too)
+        }
       ln = again(lane);
       Frag<TS> p;
-      feed<4 * F, AHEAD, Frag<TS>>(
-          [&](auto i, Frag<TS>& v) { TL::col_frag(V, i.value % F, i.value / F, ln, v); },
+      feed<2 * NB * F, AHEAD, Frag<TS>>(
+          [&](auto i, Frag<TS>& v) { TL::col_frag(V, i.value % F, 2 * kc + i.value / F, ln, v); },
           [&](auto i, Frag<TS>& v) {
             constexpr int st = i.value / F, f = i.value % F;
             if constexpr (f == 0) {
@@ -147,6 +155,28 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
             o[f] = mfma32(v, p, o[f]);
           });
     }
+  }
+  if constexpr (NC == 2) {
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(lds) + wave % RW * (F * 16 + 2) * 64 + lane;
+    if (kc == 1) {
+      part[0] = m;
+      part[64] = l;
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[(2 + 16 * f + r) * 64] = o[f][r];
+    }
+    __syncthreads();
+    if (kc == 1) return;
+    const float m1 = part[0], to = fmaxf(m, m1), ref = to == kNoKey ? 0.f : to;
+    const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(m1 - ref);
+    m = to;
+    l = l * c0 + part[64] * c1;
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[f][r] = o[f][r] * c0 + part[(2 + 16 * f + r) * 64] * c1;
   }
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
@@ -237,12 +267,17 @@ __global__ __launch_bounds__(256) void k_rotate(int64_t T, int64_t S, int H, int
 }
 
 template <typename TS, int D> hipError_t run_attn(const AttnArgs& a, hipStream_t s) {
-  const int64_t tiles = (a.T + 127) / 128;
-  const dim3 grid((unsigned)(tiles * a.Hq)), block(64 * kAttnWaves);
-  if (a.cap > 0.f || a.slopes)
-    k_attn<TS, D, true><<<grid, block, 0, s>>>(a);
-  else
-    k_attn<TS, D, false><<<grid, block, 0, s>>>(a);
+  const int nc = attn_parts(a.T, a.Hq);
+  const dim3 grid((unsigned)((a.T + 128 / nc - 1) / (128 / nc) * a.Hq)), block(64 * kAttnWaves);
+  const int mode = a.slopes || (a.cap > 0.f && sizeof(TS) == 4) ? 2 : a.cap > 0.f ? 1 : 0;
+  auto run = [&](auto m, auto n) { k_attn<TS, D, m.value, n.value><<<grid, block, 0, s>>>(a); };
+  auto of = [&](auto n) {
+    if (mode == 2) return run(Int<2>{}, n);
+    if constexpr (sizeof(TS) == 2)
+      if (mode == 1) return run(Int<1>{}, n);
+    run(Int<0>{}, n);
+  };
+  nc == 1 ? of(Int<1>{}) : of(Int<2>{});
   return hipGetLastError();
 }
 

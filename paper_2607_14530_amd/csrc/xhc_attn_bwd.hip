@@ -70,11 +70,11 @@ __global__ __launch_bounds__(256) void k_attn_prep(AttnArgs a, float* delta, int
 
 // p and dS of one pair from the raw product and dP
 template <typename TS>
-__device__ __forceinline__ void reverse_score(float& x, float& dp, const Score& sc, bool capped, float bias, float lse,
+__device__ __forceinline__ void reverse_score(float& x, float& dp, const Score<TS>& sc, bool capped, float bias, float lse,
                                               float delta) {
   float der = 1.f;
   if (capped) {
-    const float t = tanh_of<TS>(x * sc.mul);
+    const float t = sc.tanh_of(x);
     x = sc.cap * t;
     der = 1.f - t * t;
   } else {
@@ -84,22 +84,25 @@ __device__ __forceinline__ void reverse_score(float& x, float& dp, const Score& 
   dp = x * (dp - delta) * der;
 }
 
-template <typename TS, int D, bool EX>
+// (NC as in k_attn)
+template <typename TS, int D, bool EX, int NC>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a) {
   using TL = Tile<TS, D>;
   constexpr int KS = D / 16, F = D / 32, AHEAD = sizeof(TS) == 2 ? 4 : 2;
+  constexpr int ROWS = 128 / NC, RW = kAttnWaves / NC, NB = 2 / NC;
   __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
   __shared__ int4 red[kAttnWaves];
   __shared__ uint64_t bits;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
-  attn_place(a.Hq, (int)((a.T + 127) / 128), head, tile);
+  attn_place(a.Hq, (int)((a.T + ROWS - 1) / ROWS), head, tile);
+  const int kc = NC == 1 ? 0 : wave / RW;
   const int kvh = head / (a.Hq / a.Hkv), H = a.Hq + 2 * a.Hkv;
-  const int t = tile * 128 + wave * 32 + lane % 32, T1 = (int)a.T - 1;
+  const int t = tile * ROWS + wave % RW * 32 + lane % 32, T1 = (int)a.T - 1;
   const bool row = t <= T1;
   const int2 see = span_of(a, t);
   int2 own;
-  const int4 ex = attn_extremes(see, row, red, wave, lane, own);
+  const int4 ex = attn_extremes(a, tile * ROWS, ROWS, tile * ROWS + wave % RW * 32, see, row, red, wave, lane, own);
   const uint32_t stride = (uint32_t)H * D * sizeof(TS);
   const unsigned char* base = reinterpret_cast<const unsigned char*>(a.qkv);
   const unsigned char* kb = base + (size_t)(a.Hq + kvh) * D * sizeof(TS);
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   for (int f = 0; f < F; ++f) dq[f] = f32x16{};
   const int first = ex.x / kTile, end = (ex.y + kTile - 1) / kTile;
   if (ex.x < ex.y) {
-    Score sc;
+    Score<TS> sc;
     sc.init(a, head);
     const int64_t tc = row ? t : T1;
     const float lse = a.lse[(int64_t)head * a.Tp + tc], delta = a.delta[(int64_t)head * a.Tp + tc];
@@ -141,7 +144,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       if (cut) bad = TL::clean(K, &bits, wave, again(lane));
       const bool none = j0 >= own.y || j0 + kTile <= own.x;   // no row of this wave sees a key of the tile
 #pragma unroll 1
-      for (int rb = none ? 2 : 0; rb < 2; ++rb) {
+      for (int rb = none ? 2 : kc; rb < kc + NB; ++rb) {
         const int ln = again(lane);
         f32x16 s = f32x16{}, dp = f32x16{};
         feed<2 * KS, AHEAD, Frag<TS>>(
@@ -188,6 +191,22 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
             });
       }
     }
+  }
+  if constexpr (NC == 2) {
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(lds) + wave % RW * F * 16 * 64 + lane;
+    if (kc == 1) {
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[(16 * f + r) * 64] = dq[f][r];
+    }
+    __syncthreads();
+    if (kc == 1) return;
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[f][r] += part[(16 * f + r) * 64];
   }
   TS* p = reinterpret_cast<TS*>(a.dqkv) + (int64_t)t * H * D + head * D;
 #pragma unroll
@@ -299,7 +318,7 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
     behind(nhead, nqt);
     int ahead = range_at(nqt);
     while (head < head0 + mine) {
-      Score sc;
+      Score<TS> sc;
       sc.init(a, head);
       wait_loads();
       lds_barrier();
@@ -475,14 +494,17 @@ template <typename TS, int D, bool EX> hipError_t run_bwd(AttnArgs a, char* ws, 
   k_attn_prep<TS, D><<<dim3((unsigned)(a.Tp / kTile), a.Hq + 1), dim3(256), 0, s>>>(a, delta, lo, hi, range);
   a.delta = delta, a.lo = lo, a.hi = hi, a.range = range;
   constexpr int NW = dkv_waves(sizeof(TS) == 4, D);
-  const unsigned tiles = (unsigned)((a.T + 127) / 128), ktiles = (unsigned)((a.T + 32 * NW - 1) / (32 * NW));
+  const unsigned ktiles = (unsigned)((a.T + 32 * NW - 1) / (32 * NW));
   k_attn_dkv<TS, D, EX><<<dim3(ktiles * a.Hkv * a.parts), dim3(64 * NW), 0, s>>>(a);
   if (a.parts > 1) {
     const int row = 2 * a.Hkv * D;
     k_attn_join<TS><<<dim3((unsigned)((a.T * row / 8 + 255) / 256)), dim3(256), 0, s>>>(
         a.T, row, a.parts, a.part, a.Hq + 2 * a.Hkv, a.Hq, D, static_cast<TS*>(a.dqkv));
   }
-  k_attn_dq<TS, D, EX><<<dim3(tiles * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
+  if (attn_parts(a.T, a.Hq) == 1)
+    k_attn_dq<TS, D, EX, 1><<<dim3((unsigned)((a.T + 127) / 128) * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
+  else
+    k_attn_dq<TS, D, EX, 2><<<dim3((unsigned)((a.T + 63) / 64) * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
   return hipGetLastError();
 }
 

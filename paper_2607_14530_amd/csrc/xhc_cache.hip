@@ -518,7 +518,9 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
     }
     least = __builtin_amdgcn_readfirstlane(least);
     most = __builtin_amdgcn_readfirstlane(most);
-    const float mul = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e, cap = a.cap * kLog2e;
+    Score<TS> sc;
+    sc.mul = a.cap > 0.f ? a.scale / a.cap * (sizeof(TS) == 2 ? 2.f * kLog2e : 1.f) : a.scale * kLog2e;
+    sc.cap = a.cap * kLog2e;
 
     const int count = (upto - from - wave + 3) / 4;          // this wave's blocks: from + wave + 4 i
     const int* pages = a.pages + (int64_t)b * a.per_seq;
@@ -577,7 +579,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               float x = s[rt][e / 4][e % 4];
-              x = a.cap > 0.f ? cap * tanh_of<TS>(x * mul) : x * mul;
+              x = a.cap > 0.f ? sc.cap * sc.tanh_of(x) : x * sc.mul;
               s[rt][e / 4][e % 4] = fmaf(-slope[rt], (float)(see[rt] - 1 - first - 16 * (e / 4) - e % 4), x);
             }
           }
@@ -592,7 +594,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
           float top = s[rt][0][0];
 #pragma unroll
           for (int e = 1; e < 8; ++e) top = fmaxf(top, s[rt][e / 4][e % 4]);
-          if constexpr (!EX) top *= mul;         // (the raw products so far; exp takes the factor with it)
+          if constexpr (!EX) top *= sc.mul;        // (the raw products so far; exp takes the factor with it)
           top = max_quarters(top);
           if (__any(top > m[rt] + 8.f)) {        // (as in the attention of token rows)
             const float to = top > m[rt] + 8.f ? top : m[rt];
@@ -607,7 +609,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
           const float ref = m[rt] == -__builtin_huge_valf() ? 0.f : m[rt];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float x = __builtin_amdgcn_exp2f(EX ? s[rt][e / 4][e % 4] - ref : fmaf(s[rt][e / 4][e % 4], mul, -ref));
+            const float x = __builtin_amdgcn_exp2f(EX ? s[rt][e / 4][e % 4] - ref : fmaf(s[rt][e / 4][e % 4], sc.mul, -ref));
             s[rt][e / 4][e % 4] = x;
             l[rt] += x;
           }
@@ -661,18 +663,19 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
     // the waves' sums of each 16 rows, added in order
     const bool whole = from == 0 && upto == sq.blocks;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (from == 0 ? 1 : 0);
+    const int ln = again(lane), me = wave * 64 + ln;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[rt]), __float_as_uint(l[rt]), false, false);
       float ls = __uint_as_float(s16[0]) + __uint_as_float(s16[1]);
       ls = swap32_add(ls);
       __syncthreads();
-      if (lane < 16) mls[wave][lane] = make_float2(m[rt], ls);
+      if (ln < 16) mls[wave][ln] = make_float2(m[rt], ls);
 #pragma unroll
       for (int n = 0; n < W; ++n)
-        *reinterpret_cast<f32x4*>(&sums[wave][r16][16 * n + 4 * (lane / 16)]) = o[rt][n];
+        *reinterpret_cast<f32x4*>(&sums[wave][ln % 16][16 * n + 4 * (ln / 16)]) = o[rt][n];
       __syncthreads();
-      for (int i = tid; i < 16 * (D / 8); i += 256) {
+      for (int i = me; i < 16 * (D / 8); i += 256) {
         const int row = i / (D / 8), c = i % (D / 8) * 8;
         const int64_t ri = (int64_t)tile * ROWS + rt * 16 + row, t = sq.first + ri / g, p = sq.len - (sq.after - t);
         if (t >= sq.end || p < 0 || p >= (int64_t)a.per_seq * a.page) continue;

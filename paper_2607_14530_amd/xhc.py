@@ -965,10 +965,12 @@ def _slopes(h, slopes, device):
     return slopes.to(device).contiguous()
 
 
-def _expect_ints(t, shape, dev, name):
-    if t is not None:
-        _expect(t, torch.int32, shape, name)
-        _on(t, dev, name)
+def _take(t, dtype, shape, dev, name):
+    """An argument of a call: of this dtype, shape (a tuple) and device."""
+    if t.dtype is not dtype or t.shape != shape:
+        _expect(t, dtype, shape, name)
+    if t.get_device() != dev.index:
+        raise ValueError(f"{name} is on {t.device}, expected {dev}")
 
 
 class Rotation:
@@ -980,21 +982,21 @@ class Rotation:
     def __init__(self, d: Dims, h: Heads, table, device="cuda"):
         self.d, self.h, self.device = d, h, _here(device)
         self.table, self.positions = _table(h, table, self.device)
+        self.shape, self.dtype = (d.T, h.Hq + 2 * h.Hkv, h.D), _state_dtype(d)
         self.buffers = [None, None]    # of forward, of backward
 
     def _run(self, x, pos, out, inverse, stream):
-        shape = (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D)
-        _expect(x, _state_dtype(self.d), shape, "the heads")
-        _on(x, self.device, "the heads")
-        _expect_ints(pos, (self.d.T,), self.device, "pos")
+        _take(x, self.dtype, self.shape, self.device, "the heads")
+        if pos is not None:
+            _take(pos, torch.int32, (self.d.T,), self.device, "pos")
+        _enqueues(self.device)
         if out is None:
             if self.buffers[inverse] is None:
                 with _within(stream):
-                    self.buffers[inverse] = torch.empty(shape, dtype=x.dtype, device=self.device)
+                    self.buffers[inverse] = torch.empty(self.shape, dtype=self.dtype, device=self.device)
             out = self.buffers[inverse]
         else:
-            _expect(out, x.dtype, shape, "out")
-            _on(out, self.device, "out")
+            _take(out, self.dtype, self.shape, self.device, "out")
         xhc_rotate(self.d, self.h, x, pos, self.table, self.positions, inverse, out, stream)
         return out
 
@@ -1016,6 +1018,7 @@ class Attention:
         self.d, self.h, self.device = d, h, _here(device)
         self.slopes = _slopes(h, slopes, self.device)
         self.out = torch.empty(d.T, h.Hq, h.D, dtype=_state_dtype(d), device=self.device)
+        self.shape = (d.T, h.Hq + 2 * h.Hkv, h.D)
         self.saved = None
         self.span = None
 
@@ -1026,8 +1029,9 @@ class Attention:
         if starts is not None:
             if n < 0:
                 raise ValueError("starts holds one entry more than there are documents")
-            _expect_ints(starts, (n + 1,), self.device, "starts")
-        _expect_ints(prefix, (n,), self.device, "prefix")
+            _take(starts, torch.int32, (n + 1,), self.device, "starts")
+        if prefix is not None:
+            _take(prefix, torch.int32, (n,), self.device, "prefix")
         _enqueues(self.device)
         if self.span is None:
             with _within(stream):
@@ -1036,9 +1040,10 @@ class Attention:
         return self.span
 
     def forward(self, qkv, span=None, stream=None):
-        _expect(qkv, self.out.dtype, (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D), "qkv")
-        _on(qkv, self.device, "qkv")
-        _expect_ints(span, (self.d.T, 2), self.device, "span")
+        _take(qkv, self.out.dtype, self.shape, self.device, "qkv")
+        if span is not None:
+            _take(span, torch.int32, (self.d.T, 2), self.device, "span")
+        _enqueues(self.device)
         xhc_attn(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, stream)
         return self.out
 
@@ -1050,7 +1055,7 @@ class TrainableAttention(Attention):
     def __init__(self, d: Dims, h: Heads, slopes=None, device="cuda"):
         super().__init__(d, h, slopes, device)
         self.saved = _bytes(xhc_attn_saved_bytes(d, h), self.device)
-        self.dqkv = torch.empty(d.T, h.Hq + 2 * h.Hkv, h.D, dtype=self.out.dtype, device=self.device)
+        self.dqkv = torch.empty(self.shape, dtype=self.out.dtype, device=self.device)
         self.ws = _bytes(xhc_attn_workspace_bytes(d, h), self.device)
         self.seen = None
 
@@ -1062,8 +1067,8 @@ class TrainableAttention(Attention):
     def backward(self, dout, stream=None):
         if self.seen is None:
             raise ValueError("backward without a forward")
-        _expect(dout, self.out.dtype, self.out.shape, "dout")
-        _on(dout, self.device, "dout")
+        _take(dout, self.out.dtype, self.out.shape, self.device, "dout")
+        _enqueues(self.device)
         qkv, span = self.seen
         xhc_attn_bwd(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, dout, self.dqkv, self.ws, stream)
         return self.dqkv
@@ -1095,20 +1100,20 @@ class KVCache:
         self.q = torch.empty(d.T, h.Hq, h.D, dtype=sdt, device=self.device)
         self.out = torch.empty_like(self.q)
         self.k = self.v = None
+        self.shape = (d.T, h.Hq + 2 * h.Hkv, h.D)
         self.ws = _bytes(xhc_attn_cache_workspace_bytes(d, h, self.c), self.device)
 
     def _check(self, starts, lens, pages):
-        c = self.c
-        _expect_ints(starts, (c.B + 1,), self.device, "starts")
-        _expect_ints(lens, (c.B,), self.device, "lens")
-        _expect_ints(pages, (c.B, c.per_seq), self.device, "pages")
+        B = self.c.B
+        _take(starts, torch.int32, (B + 1,), self.device, "starts")
+        _take(lens, torch.int32, (B,), self.device, "lens")
+        _take(pages, torch.int32, (B, self.c.per_seq), self.device, "pages")
         _enqueues(self.device)
 
     def append(self, qkv, starts, lens, pages, stream=None):
         """Stores the rotated key heads and the value heads of qkv [T, Hq + 2 Hkv, D]; returns the rotated query heads
         [T, Hq, D]."""
-        _expect(qkv, self.q.dtype, (self.d.T, self.h.Hq + 2 * self.h.Hkv, self.h.D), "qkv")
-        _on(qkv, self.device, "qkv")
+        _take(qkv, self.q.dtype, self.shape, self.device, "qkv")
         self._check(starts, lens, pages)
         xhc_cache_append(self.d, self.h, self.c, qkv, self.table, self.positions, starts, lens, pages, self.pool,
                          self.q, stream)
@@ -1126,8 +1131,7 @@ class KVCache:
 
     def attend(self, q, starts, lens, pages, stream=None):
         """Attention of q [T, Hq, D], the call's tokens (appended before), over their sequences up to themselves."""
-        _expect(q, self.q.dtype, self.q.shape, "q")
-        _on(q, self.device, "q")
+        _take(q, self.q.dtype, self.q.shape, self.device, "q")
         self._check(starts, lens, pages)
         xhc_attn_cache(self.d, self.h, self.c, q, self.slopes, starts, lens, pages, self.pool, self.out, self.ws,
                        stream)
