@@ -477,7 +477,8 @@ xhc_status xhc_ffn_bwd(const xhc_dims* d, int32_t H, int32_t act, const void* in
  * out of range, XHC_EUNSUPPORTED where this library does not take it):
  *   Hkv >= 1, Hq a multiple of it, Hq + 2 Hkv <= 1024;  D 32, 64, 96 or 128;
  *   R from 0 to D, a multiple of 16;  pairs an xhc_pairs;  window >= 0;
- *   scale > 0 and cap >= 0, finite.  T <= 2^23, T (Hq + 2 Hkv) <= 2^29.          */
+ *   scale from 2^-40 to 2^40;  cap 0, or from 2^-20 to 4096.
+ *   T <= 2^23, T (Hq + 2 Hkv) <= 2^29.                                          */
 typedef enum { XHC_PAIRS_HALVES = 0, XHC_PAIRS_NEIGHBOURS = 1 } xhc_pairs;
 typedef struct xhc_heads {
   int32_t Hq;             /* query heads                                         */

@@ -1140,6 +1140,8 @@ static xhc_status check_heads(const xhc_dims* d, const xhc_heads* h) {
     return XHC_EINVAL;
   if (h->pairs != XHC_PAIRS_HALVES && h->pairs != XHC_PAIRS_NEIGHBOURS) return XHC_EINVAL;
   if (!(h->scale > 0.f && h->scale <= FLT_MAX && h->cap >= 0.f && h->cap <= FLT_MAX)) return XHC_EINVAL;
+  if (h->scale < kMinScale || h->scale > kMaxScale || h->cap > kMaxCap || (h->cap > 0.f && h->cap < kMinCap))
+    return XHC_EUNSUPPORTED;
   if (h->D % 32 != 0 || h->D > 128 || h->R % 16 != 0) return XHC_EUNSUPPORTED;
   if (h->Hkv > kMaxHeads || h->Hq > kMaxHeads - 2 * h->Hkv) return XHC_EUNSUPPORTED;
   if (d->T > kMaxAttnT || d->T * (h->Hq + 2 * h->Hkv) > kMaxAttnHeads) return XHC_EUNSUPPORTED;

@@ -396,7 +396,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
   __shared__ float2 mls[4][16];
   __shared__ int64_t scan[256];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int g = a.Hq / a.Hkv, r16 = lane % 16;
+  const int g = a.Hq / a.Hkv;
 
   // The run's first unit's sequence b, and the units in front of that.
   int b;
@@ -479,11 +479,15 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
       sq = sequence(a, ++b, ROWS);
     }
     const int64_t seg = (u - before) / sq.blocks, seg0 = before + seg * sq.blocks;
-    const int head = (int)(seg % a.Hkv), tile = (int)(seg / a.Hkv);
+    int heads = a.Hkv;
+    const float* slopes = a.slopes;
+    asm volatile("" : "+s"(heads), "+s"(slopes));      // (what follows from them is not kept in registers over the loop)
+    const int head = (int)(seg % heads), tile = (int)(seg / heads);
     const int from = (int)(u - seg0);
     const int64_t last = u1 < seg0 + sq.blocks ? u1 : seg0 + sq.blocks;
     const int upto = (int)(last - seg0);         // blocks from .. upto - 1 of the segment are taken here
 
+    const int r16 = again(lane) % 16, quarter = again(lane) / 16;
     // this lane's rows: row r16 of each of the RT tiles
     Frag<TS> q[RT][G];
     int see[RT], low[RT];                        // the row sees low .. see - 1
@@ -498,12 +502,12 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
       const int qh = head * g + (int)(row % g);
       see[rt] = is ? (int)p + 1 : 0;
       low[rt] = is && a.window > 0 && p - a.window + 1 > 0 ? (int)(p - a.window + 1) : 0;
-      slope[rt] = a.slopes ? a.slopes[qh] * kLog2e : 0.f;
+      slope[rt] = slopes ? slopes[qh] * kLog2e : 0.f;
       if (is) {                                  // (what the other rows give is not used)
         least = min(least, see[rt]);
         most = max(most, low[rt]);
       }
-      const TS* qp = static_cast<const TS*>(a.q) + ((is ? t : sq.first) * a.Hq + qh) * D + 8 * (lane / 16);
+      const TS* qp = static_cast<const TS*>(a.q) + ((is ? t : sq.first) * a.Hq + qh) * D + 8 * quarter;
 #pragma unroll
       for (int k = 0; k < G; ++k) load_frag(qp + 32 * k, q[rt][k]);
       m[rt] = -__builtin_huge_valf();
@@ -511,13 +515,8 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
 #pragma unroll
       for (int n = 0; n < W; ++n) o[rt][n] = f32x4{};
     }
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) {
-      least = min(least, __shfl_xor(least, d));
-      most = max(most, __shfl_xor(most, d));
-    }
-    least = __builtin_amdgcn_readfirstlane(least);
-    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(half_min(least));
+    most = -__builtin_amdgcn_readfirstlane(half_min(-most));
     Score<TS> sc;
     sc.mul = a.cap > 0.f ? a.scale / a.cap * (sizeof(TS) == 2 ? 2.f * kLog2e : 1.f) : a.scale * kLog2e;
     sc.cap = a.cap * kLog2e;
@@ -527,10 +526,19 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
     auto token0 = [&](int i) { return (sq.block0 + from + wave + 4 * i) * kBlock; };
     for (int i0 = 0; i0 < count; i0 += 64) {
       const int n = min(64, count - i0);
-      int mypage = -1;
-      if (lane < n) mypage = pages[token0(i0 + lane) / a.page];
+      // a lane finds a block's place: its number in the pool
+      int64_t place = 0;
+      bool there = false;
+      int page = a.page;
+      asm volatile("" : "+s"(page));             // (nor the reciprocal for the division by it)
+      if (lane < n) {
+        const uint32_t tok = (uint32_t)token0(i0 + lane);
+        const int pg = pages[tok / (uint32_t)page];
+        there = pg >= 0 && pg < a.npages;
+        place = ((int64_t)pg * a.Hkv + head) * (page / kBlock) + tok % (uint32_t)page / kBlock;
+      }
       // the blocks that are there, one bit each
-      uint64_t left = __ballot(mypage >= 0 && mypage < a.npages);
+      uint64_t left = __ballot(there);
       // three of them on their way or worked on, where the registers hold them
       // (one ahead of the present one does not cover the way from memory)
       constexpr int RING = RT == 1 && !(EX && D == 128) ? 3 : 2;
@@ -542,8 +550,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
         if (left) {
           i = __builtin_ctzll(left);
           left &= left - 1;
-          const int pg = __builtin_amdgcn_readlane(mypage, i);
-          from_at = block_at<D>(a, pg, head, token0(i0 + i) % a.page);
+          from_at = a.pool + scalar64(place, i) * Block<D>::kBytes;
         }
         // (behind the last block the same once more: with loads that are always
         // sent the compiler knows how many of them may be on their way)
@@ -574,6 +581,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
         });
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+          __builtin_amdgcn_sched_barrier(0);
           const int first = j0 + 4 * (again(lane) / 16);     // this lane's tokens: first + 16 (e / 4) + e % 4
           if constexpr (EX) {
 #pragma unroll

@@ -327,6 +327,10 @@ hipError_t launch_grad_clip(int n, const void* const* grads, const int64_t* coun
 constexpr int64_t kMaxAttnT = (int64_t)1 << 23;      // tokens, and heads of all of them: a launch's threads stay
 constexpr int64_t kMaxAttnHeads = (int64_t)1 << 29;  // below 2^32
 constexpr int kMaxHeads = 1024;                      // of a token
+// A capped score is off by some 2^-22 of the cap (bf16 state), and the factors
+// formed of scale and cap stay within fp32.
+constexpr float kMinScale = 1.f / (1ll << 40), kMaxScale = (float)(1ll << 40);
+constexpr float kMinCap = 1.f / (1 << 20), kMaxCap = 4096.f;
 hipError_t launch_rotate(const xhc_dims* d, const xhc_heads* h, const void* src, const int32_t* pos,
                          const float* table, int64_t positions, bool inverse, void* dst, hipStream_t s);
 hipError_t launch_attn_spans(int64_t T, int64_t S, int window, int n, const int32_t* starts, const int32_t* prefix,

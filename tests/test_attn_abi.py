@@ -78,6 +78,8 @@ CALLS = [(lambda d, h: rotate(d, h, A[:4])), (lambda d, h: spans(d, h, 3, A[:3])
     (dict(window=-1), X.XHC_EINVAL), (dict(scale=0.0), X.XHC_EINVAL), (dict(scale=float("nan")), X.XHC_EINVAL),
     (dict(scale=float("inf")), X.XHC_EINVAL), (dict(cap=-1.0), X.XHC_EINVAL), (dict(cap=float("inf")), X.XHC_EINVAL),
     (dict(D=48, R=48), X.XHC_EUNSUPPORTED), (dict(D=160), X.XHC_EUNSUPPORTED), (dict(R=24), X.XHC_EUNSUPPORTED),
+    (dict(cap=4097.0), X.XHC_EUNSUPPORTED), (dict(cap=2.0 ** -21), X.XHC_EUNSUPPORTED),
+    (dict(scale=2.0 ** 41), X.XHC_EUNSUPPORTED), (dict(scale=2.0 ** -41), X.XHC_EUNSUPPORTED),
     (dict(Hq=1024), X.XHC_EUNSUPPORTED), (dict(Hq=1024, Hkv=1024), X.XHC_EUNSUPPORTED),
 ])
 def test_heads_refused(call, kw, status):

@@ -213,3 +213,41 @@ def test_held_values_at_the_borders():
         z = z.cpu()[:, 0].to(U.F64)
         assert torch.equal(torch.isnan(z), torch.isnan(ref))
         assert torch.equal(torch.nan_to_num(z), torch.nan_to_num(ref))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_later_tokens_that_are_not_finite(dtype):
+    """A token whose key or value is not finite makes the rows that see it NaN, and leaves the others' bits."""
+    m = Model(2, 4, 32, 4, 2, 64, dtype, seed=12)
+    m.append([70, 40])
+    outs = []
+    for bad in (False, True):
+        d = X.make_dims(8, 1, 1, 1, 32, S=1, state=NAME[dtype])
+        c = X.KVCache(d, m.h, m.table, 2, 4, page=32, npages=m.npages, pool=m.pool.clone())
+        x = torch.randn(8, 8, 64, generator=torch.Generator().manual_seed(1)).to(dtype)
+        if bad:
+            x[3, 5] = float("nan")               # a key of sequence 0's fourth token, a value of sequence 1's last
+            x[7, 6, 9] = float("inf")
+        args = (i32([0, 5, 8]), i32([75, 43]), m.pages.int().cuda())
+        c.append(x.cuda(), *args)
+        q = torch.randn(8, 4, 64, generator=torch.Generator().manual_seed(2)).to(dtype).cuda()
+        outs.append(c.attend(q, *args).clone())
+    good, got = outs
+    same = [0, 1, 2, 5, 6]
+    assert torch.equal(got[same], good[same])
+    assert torch.equal(got[3:5, :2], good[3:5, :2]) and bool(torch.isnan(got[3:5, 2:]).any(-1).all())
+    assert torch.equal(got[7, 2:], good[7, 2:]) and bool(torch.isnan(got[7, :2]).any(-1).all())
+
+
+def test_append_without_queries():
+    m = Model(2, 2, 32, 4, 2, 64, BF, seed=13)
+    m.append([20, 30])
+    x = torch.randn(2, 8, 64).bfloat16()
+    pools = []
+    for q in (True, False):
+        d = X.make_dims(2, 1, 1, 1, 32, S=1)
+        c = X.KVCache(d, m.h, m.table, 2, 2, page=32, npages=m.npages, pool=m.pool.clone())
+        args = (i32([0, 1, 2]), i32([21, 31]), m.pages.int().cuda())
+        X.xhc_cache_append(d, m.h, c.c, x.cuda(), c.table, c.positions, *args, c.pool, c.q if q else None)
+        pools.append(c.pool)
+    assert torch.equal(*pools) and not torch.equal(pools[0], m.pool)
