@@ -269,7 +269,7 @@ struct AttnArgs {
   float* part;              // dk, dv of parts of a group's heads
   int64_t T, S, Tp;
   int Hq, Hkv, window;
-  int parts;                // of a group's query heads, each one workgroup's (dk, dv)
+  int parts, slices;        // of dk and dv: shares of a group's heads times slices of the queries
   float scale, cap;
 };
 

@@ -237,13 +237,13 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
   __shared__ uint64_t bits[2];
   __shared__ int reach[2];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int g = a.Hq / a.Hkv, mine = g / a.parts, H = a.Hq + 2 * a.Hkv;
+  const int g = a.Hq / a.Hkv, shares = a.parts / a.slices, mine = g / shares, H = a.Hq + 2 * a.Hkv;
   const int tiles = (int)((a.T + KEYS - 1) / KEYS), qtiles = (int)(a.Tp / kTile);
   int which, tile;
   attn_place(a.Hkv * a.parts, tiles, which, tile);
   tile = tiles - 1 - tile;                       // the first keys are seen by most queries
   const int kvh = which / a.parts, part = which % a.parts;
-  const int head0 = kvh * g + part * mine;
+  const int head0 = kvh * g + part % shares * mine, slice = part / shares;
   const int j0 = tile * KEYS, T1 = (int)a.T - 1;
   const int key = j0 + wave * 32 + lane % 32;
   const bool row = key <= T1;
@@ -269,6 +269,11 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
   __syncthreads();
   from = __builtin_amdgcn_readfirstlane(reach[0]);
   upto = __builtin_amdgcn_readfirstlane(reach[1]);
+  if (a.slices > 1 && from <= upto) {            // the queries of this slice
+    const int n = upto - from + 1, of = from;
+    from = of + n * slice / a.slices;
+    upto = of + n * (slice + 1) / a.slices - 1;
+  }
 
   f32x16 dk[F], dv[F];
 #pragma unroll
@@ -473,15 +478,25 @@ __global__ __launch_bounds__(256) void k_attn_join(int64_t T, int row, int parts
 
 constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
-// Parts of a group's heads for dk and dv: the chip holds 512 workgroups of four
-// waves, of unlike lengths where masks cut; with less than twice as many, a group's heads are divided among several, whose sums
-// are then added.
-int parts_of(int64_t T, int Hq, int Hkv, int keys) {
-  const int64_t wg = (T + keys - 1) / keys * Hkv;
+// Parts of the sums of dk and dv, which are added afterwards: the chip holds
+// 512 workgroups of four waves, of unlike lengths where masks cut; with less
+// than twice as many, a group's heads are divided among several.  Where those
+// do not give each CU a workgroup, so are the tiles of queries that see a
+// workgroup's keys (T = 777, Hq = 6, Hkv = 2, D = 96, fp32: 42 workgroups
+// without, 146 us).
+struct Parts {
+  int parts, slices;                             // parts = shares of a group's heads times slices of the queries
+};
+Parts parts_of(int64_t T, int Hq, int Hkv, int keys) {
+  const int64_t wg = (T + keys - 1) / keys * Hkv, tiles = (T + kTile - 1) / kTile;
   const int g = Hq / Hkv;
+  if (T == 0) return {1, 1};
   for (int p = 1; p < g; ++p)
-    if (g % p == 0 && wg * p * keys >= 1024 * 128) return p;
-  return g;
+    if (g % p == 0 && wg * p * keys >= 1024 * 128) return {p, 1};
+  int64_t n = 256 * 128 / (wg * g * keys);
+  n = n < 1 ? 1 : n < 8 ? n : 8;
+  n = n < tiles ? n : tiles;
+  return {g * (int)n, (int)n};
 }
 
 template <typename TS, int D, bool EX> hipError_t run_bwd(AttnArgs a, char* ws, hipStream_t s) {
@@ -522,7 +537,7 @@ template <typename TS> hipError_t run_bwd_of(int D, const AttnArgs& a, char* ws,
 
 size_t attn_bwd_ws_bytes(int state_dtype, int64_t T, int Hq, int Hkv, int D) {
   const int64_t Tp = (T + kTile - 1) / kTile * kTile;
-  const int parts = parts_of(T, Hq, Hkv, 32 * dkv_waves(state_dtype == XHC_F32, D));
+  const int parts = parts_of(T, Hq, Hkv, 32 * dkv_waves(state_dtype == XHC_F32, D)).parts;
   return up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) +
          (parts > 1 ? (size_t)parts * T * 2 * Hkv * D * 4 : 0);
 }
@@ -541,7 +556,8 @@ hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qk
   a.dqkv = dqkv;
   a.T = d->T, a.S = d->S, a.Tp = (d->T + kTile - 1) / kTile * kTile;
   a.Hq = h->Hq, a.Hkv = h->Hkv, a.window = h->window;
-  a.parts = parts_of(d->T, h->Hq, h->Hkv, 32 * dkv_waves(d->state_dtype == XHC_F32, h->D));
+  const Parts parts = parts_of(d->T, h->Hq, h->Hkv, 32 * dkv_waves(d->state_dtype == XHC_F32, h->D));
+  a.parts = parts.parts, a.slices = parts.slices;
   a.scale = h->scale, a.cap = h->cap;
   return d->state_dtype == XHC_BF16 ? run_bwd_of<uint16_t>(h->D, a, static_cast<char*>(ws), s)
                                     : run_bwd_of<float>(h->D, a, static_cast<char*>(ws), s);

@@ -34,8 +34,8 @@ struct CacheArgs {
   int64_t T;
   int Hq, Hkv, R, pairs, window, page, npages, B, per_seq;
   int rows;               // append: tokens that a workgroup looks after
-  int tokens;             // append: of which it rotates the queries
-  unsigned qblocks;       // append: workgroups that rotate queries
+  int tokens;             // append: of which a workgroup behind those rotates the queries
+  unsigned blocks;        // append: workgroups that look after keys and values
   float scale, cap;
   // attend
   float* part;            // [2 grid][16 RT][D]
@@ -112,7 +112,14 @@ __device__ __forceinline__ void rotated8(const TS* head, int c, const float* cs,
 
 // Codes of eight channels of a group that four neighbouring lanes share, and
 // its scale (bf16 bits): the largest magnitude / 6, rounded; divisions rounded
-// to the nearest, so that the codes are the definition's to the bit.
+// to the nearest, so that the codes are the definition's to the bit.  The
+// quotients by one scale share its reciprocal r: with r rounded to the nearest
+// and q within one step of x / s, q + (x - q s) r in fused products is x / s
+// rounded to the nearest (Markstein's theorem); x r may be two steps off, so
+// the correction is made twice.  Nothing underflows where it matters: s is
+// 2^-103 or more, and quotients far below 1/4 may have any last bits.  (IEEE
+// divisions and seven comparisons an element instead: 55 us for 8192 tokens of
+// Hq = 32, Hkv = 8, D = 128.)
 __device__ __forceinline__ uint32_t hold8(const float (&x)[8], uint32_t& bits) {
   uint32_t top = 0;                              // magnitudes order as their bits do, NaN above all
 #pragma unroll
@@ -125,19 +132,24 @@ __device__ __forceinline__ uint32_t hold8(const float (&x)[8], uint32_t& bits) {
   const float s = __uint_as_float(bits << 16);
   uint32_t w = 0;
   if (bits != 0 && bits != 0x7fc0u) {
+    const float r = 1.f / s;
+    float m[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float m = fabsf(x[i]) / s;
-      uint32_t c = (m > 0.25f) + (m >= 0.75f) + (m > 1.25f) + (m >= 1.75f) + (m > 2.5f) + (m >= 3.5f) + (m > 5.f);
-      c |= __float_as_uint(x[i]) >> 31 << 3;
-      w |= c << (4 * i);
+      m[i] = x[i] * r;
+      m[i] = fmaf(fmaf(-m[i], s, x[i]), r, m[i]);
+      m[i] = fmaf(fmaf(-m[i], s, x[i]), r, m[i]);
     }
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, m[0], m[1], 1.f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, m[2], m[3], 1.f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, m[4], m[5], 1.f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, m[6], m[7], 1.f, 3);
   }
   return w;
 }
 
-// The first workgroups rotate the queries, a few tokens each.  Each of the
-// others looks after `rows` tokens for one head: it stores the block of each
+// The last workgroups rotate the queries, a few tokens each.  Each of the
+// `blocks` in front of them, which take longer, looks after `rows` tokens for one head: it stores the block of each
 // token that is the call's first in its block, which may go on behind them;
 // so no two workgroups write to a block.  Tokens that were there before keep
 // their bits.
@@ -150,8 +162,8 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
   const int tid = threadIdx.x, lane = tid % 64, H = a.Hq + 2 * a.Hkv;
   const int64_t cap = (int64_t)a.per_seq * a.page;
   const TS* qkv = static_cast<const TS*>(a.qkv);
-  if (blockIdx.x < a.qblocks) {
-    const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
+  if (blockIdx.x >= a.blocks) {
+    const int64_t t0 = (int64_t)(blockIdx.x - a.blocks) * a.tokens;
     for (int i = tid / 64; i < a.tokens; i += 4) {
       const int64_t t = t0 + i;
       const int b = t < a.T ? sequence_of(a.starts, a.B, t, lane) : -1;
@@ -162,16 +174,23 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
     __syncthreads();
     TS* q = static_cast<TS*>(a.q);
     const int all = a.tokens * a.Hq * P;
-    for (int u = tid; u < all; u += 256) {
-      const int c = u % P * 8, hd = u / P % a.Hq, i = u / P / a.Hq;
-      if (pos[i] < 0) continue;
-      float x[8];
-      rotated8<TS>(qkv + ((t0 + i) * H + hd) * D, c, a.table + pos[i] * a.R, a.R, a.pairs, x);
-      Vec8<TS>::store(q + ((t0 + i) * a.Hq + hd) * D + c, x);
+    for (int u0 = tid; u0 < all; u0 += 512) {    // two at a time, their loads first (of the first token where one is none)
+      float x[2][8];
+      TS* to[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int u = u0 + 256 * k, c = u % P * 8, hd = u / P % a.Hq, i = u / P / a.Hq;
+        const int64_t p = u < all ? pos[i] : -1, t = p < 0 ? t0 : t0 + i;
+        to[k] = p < 0 ? nullptr : q + (t * a.Hq + hd) * D + c;
+        rotated8<TS>(qkv + (t * H + hd) * D, c, a.table + (p < 0 ? 0 : p) * a.R, a.R, a.pairs, x[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (to[k]) Vec8<TS>::store(to[k], x[k]);
     }
     return;
   }
-  const unsigned mine = blockIdx.x - a.qblocks;
+  const unsigned mine = blockIdx.x;
   const int head = mine % a.Hkv;
   int64_t t = (int64_t)(mine / a.Hkv) * a.rows;
   const int64_t behind = t + a.rows < a.T ? t + a.rows : a.T;
@@ -196,24 +215,29 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
     if ((p % kBlock == 0 || t == first) && idx >= 0 && idx < a.npages) {
       unsigned char* to = block_at<D>(a, idx, head, (int)(p % a.page));
       const int at = (int)(p % kBlock), n = (int)(next - t);     // tokens at .. at + n - 1 of the block are new
-      for (int u = tid; u < n * P * 2; u += 256) {
-        const int c = u % P, i = u / P % n, val = u / P / n, tok = at + i;
-        const TS* src = qkv + ((t + i) * H + a.Hq + (val ? a.Hkv : 0) + head) * D;
-        float x[8];
-        if (val)
-          Vec8<TS>::load(src + 8 * c, x);
-        else
-          rotated8<TS>(src, 8 * c, a.table + (p + i) * a.R, a.R, a.pairs, x);
-        uint32_t bits;
-        const uint32_t w = hold8(x, bits);
-        if (c % 4 == 0)
-          *reinterpret_cast<uint16_t*>(to + (val ? BL::kValueScales : BL::kKeyScales) + BL::scale_at(tok, c / 4)) =
-              (uint16_t)bits;
-        if (val) {
+      // all loads of a thread's two tokens before the first use
+      for (int u0 = tid; u0 < n * P; u0 += 512) {
+        float x[2][8], y[2][8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) codes[tok][8 * c + e] = (uint8_t)(w >> (4 * e) & 15);
-        } else {
+        for (int k = 0; k < 2; ++k) {
+          const int u = min(u0 + 256 * k, n * P - 1), c = u % P, i = u / P;
+          const TS* src = qkv + ((t + i) * H + a.Hq + head) * D;
+          Vec8<TS>::load(src + (int64_t)a.Hkv * D + 8 * c, y[k]);
+          rotated8<TS>(src, 8 * c, a.table + (p + i) * a.R, a.R, a.pairs, x[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int u = u0 + 256 * k, c = u % P, tok = at + u / P;
+          if (u >= n * P) break;
+          uint32_t bits, vbits;
+          const uint32_t w = hold8(x[k], bits), v = hold8(y[k], vbits);
+          if (c % 4 == 0) {
+            *reinterpret_cast<uint16_t*>(to + BL::kKeyScales + BL::scale_at(tok, c / 4)) = (uint16_t)bits;
+            *reinterpret_cast<uint16_t*>(to + BL::kValueScales + BL::scale_at(tok, c / 4)) = (uint16_t)vbits;
+          }
           *reinterpret_cast<uint32_t*>(to + BL::key_word(tok, c)) = w;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) codes[tok][8 * c + e] = (uint8_t)(v >> (4 * e) & 15);
         }
       }
       __syncthreads();
@@ -834,8 +858,9 @@ hipError_t launch_cache_append(const xhc_dims* d, const xhc_heads* h, const xhc_
   a.rows = (int)(mean < 1 ? 1 : mean > kBlock ? kBlock : mean);
   while ((d->T + a.rows - 1) / a.rows * h->Hkv > (1 << 22)) a.rows *= 2;   // (a launch's threads stay below 2^32)
   a.tokens = per >= 256 ? 1 : (int)(256 / per);
-  a.qblocks = q ? (unsigned)((d->T + a.tokens - 1) / a.tokens) : 0;
-  const dim3 grid((unsigned)(a.qblocks + (d->T + a.rows - 1) / a.rows * h->Hkv)), block(256);
+  while (a.tokens < 64 && d->T > 4096 * (int64_t)a.tokens) a.tokens *= 2;
+  a.blocks = (unsigned)((d->T + a.rows - 1) / a.rows * h->Hkv);
+  const dim3 grid(a.blocks + (q ? (unsigned)((d->T + a.tokens - 1) / a.tokens) : 0)), block(256);
   with_width(h->D, [&](auto D) {
     if (d->state_dtype == XHC_BF16)
       k_cache_append<uint16_t, D.value><<<grid, block, 0, s>>>(a);

@@ -149,6 +149,9 @@ def test_attn_refusals():
     overlaps(lambda p: attn_bwd(d, h, p), A[:8], [QKV, 512, 16, ROWS, saved, ROWS, QKV, need], [6, 7])
     assert need > 0 and attn_bwd(d, h, A[:8], need - 1) == X.XHC_EWORKSPACE
     assert X.xhc_attn_workspace_bytes(d, heads(D=160)) == 0
+    for state in ("bf16", "f32"):                  # no token, one, and few of few heads
+        none, one = (X.xhc_attn_workspace_bytes(dims(T=t, state=state), heads(Hq=1, Hkv=1)) for t in (0, 1))
+        assert none <= one < 1 << 20
 
 
 def test_cache_refusals():
