@@ -267,40 +267,52 @@ __device__ __forceinline__ float held_value(uint32_t code) {
   return code & 8 ? -m : m;
 }
 
+// A few tokens a workgroup, as with the queries above: their places first, which
+// three loads one after another find.
 template <typename TS, int D>
 __global__ __launch_bounds__(256) void k_cache_read(CacheArgs a) {
   using BL = Block<D>;
   constexpr int P = D / 8;
-  const int64_t t = blockIdx.x;
-  const int lane = threadIdx.x % 64;
-  const int b = sequence_of(a.starts, a.B, t, lane);
-  if (b < 0 || t >= a.starts[b + 1]) return;
-  const int64_t p = a.lens[b] - (a.starts[b + 1] - t), cap = (int64_t)a.per_seq * a.page;
-  if (p < 0 || p >= cap) return;
-  const int idx = a.pages[(int64_t)b * a.per_seq + p / a.page];
-  if (idx < 0 || idx >= a.npages) return;
-  const int tok = (int)(p % kBlock);
-  for (int u = threadIdx.x; u < a.Hkv * P * 2; u += 256) {
-    const int c = u % P, head = u / P % a.Hkv, val = u / P / a.Hkv;
-    const unsigned char* from = block_at<D>(a, idx, head, (int)(p % a.page));
-    const uint16_t bits = *reinterpret_cast<const uint16_t*>(from + (val ? BL::kValueScales : BL::kKeyScales) +
-                                                             BL::scale_at(tok, c / 4));
-    uint32_t w = 0;
-    if (val) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int ch = 8 * c + e;
-        const uint32_t word = *reinterpret_cast<const uint32_t*>(from + BL::value_word(BL::value_lane(tok, ch), ch / 16));
-        w |= (word >> (4 * BL::value_slot(tok)) & 15) << (4 * e);
-      }
-    } else {
-      w = *reinterpret_cast<const uint32_t*>(from + BL::key_word(tok, c));
+  __shared__ int2 place[256];                    // a token's page (-1: none) and place in it
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int64_t t0 = (int64_t)blockIdx.x * a.tokens, cap = (int64_t)a.per_seq * a.page;
+  for (int i = tid / 64; i < a.tokens; i += 4) {
+    const int64_t t = t0 + i;
+    const int b = t < a.T ? sequence_of(a.starts, a.B, t, lane) : -1;
+    int2 at = make_int2(-1, 0);
+    if (b >= 0 && t < a.starts[b + 1]) {
+      const int64_t p = a.lens[b] - (a.starts[b + 1] - t);
+      if (p >= 0 && p < cap) at = make_int2(a.pages[(int64_t)b * a.per_seq + p / a.page], (int)(p % a.page));
     }
-    const float s = __uint_as_float((uint32_t)bits << 16);
-    float x[8];
+    if (lane == 0) place[i] = at;
+  }
+  __syncthreads();
+  const int all = a.tokens * a.Hkv * P;
+  for (int u = tid; u < all; u += 256) {
+    const int c = u % P, head = u / P % a.Hkv, i = u / P / a.Hkv;
+    const int2 at = place[i];
+    if (at.x < 0 || at.x >= a.npages) continue;
+    const unsigned char* from = block_at<D>(a, at.x, head, at.y);
+    const int tok = at.y % kBlock;
+    const uint32_t ks = *reinterpret_cast<const uint16_t*>(from + BL::kKeyScales + BL::scale_at(tok, c / 4));
+    const uint32_t vs = *reinterpret_cast<const uint16_t*>(from + BL::kValueScales + BL::scale_at(tok, c / 4));
+    const uint32_t k = *reinterpret_cast<const uint32_t*>(from + BL::key_word(tok, c));
+    uint32_t v = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = held_value(w >> (4 * e) & 15) * s;
-    Vec8<TS>::store(static_cast<TS*>(val ? a.v : a.k) + (t * a.Hkv + head) * D + 8 * c, x);
+    for (int e = 0; e < 8; ++e) {
+      const int ch = 8 * c + e;
+      const uint32_t word = *reinterpret_cast<const uint32_t*>(from + BL::value_word(BL::value_lane(tok, ch), ch / 16));
+      v |= (word >> (4 * BL::value_slot(tok)) & 15) << (4 * e);
+    }
+    float x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = held_value(k >> (4 * e) & 15) * __uint_as_float(ks << 16);
+      y[e] = held_value(v >> (4 * e) & 15) * __uint_as_float(vs << 16);
+    }
+    const int64_t to = ((t0 + i) * a.Hkv + head) * D + 8 * c;
+    Vec8<TS>::store(static_cast<TS*>(a.k) + to, x);
+    Vec8<TS>::store(static_cast<TS*>(a.v) + to, y);
   }
 }
 
@@ -821,6 +833,15 @@ template <class F> void with_width(int D, F&& f) {
   }
 }
 
+// tokens of a workgroup that has `per` threads' work with each: all its threads
+// work, and where there are many tokens it has enough of them that finding
+// their places is a small part
+int tokens_of(int64_t T, int per) {
+  int n = per >= 256 ? 1 : 256 / per;
+  while (n < 64 && T > 2048 * (int64_t)n) n *= 2;
+  return n;
+}
+
 // rows of a tile: 32 where the sequences have more than 16 on average
 int tile_rows(int64_t T, int B, int g) { return T * g > 16 * (int64_t)B ? 32 : 16; }
 
@@ -854,11 +875,10 @@ hipError_t launch_cache_append(const xhc_dims* d, const xhc_heads* h, const xhc_
                                void* pool, void* q, hipStream_t s) {
   CacheArgs a = args_of(d, h, c, starts, lens, pages, pool);
   a.qkv = qkv, a.table = table, a.q = q;
-  const int64_t mean = d->T / c->B, per = h->Hq * (h->D / 8);
+  const int64_t mean = d->T / c->B;
   a.rows = (int)(mean < 1 ? 1 : mean > kBlock ? kBlock : mean);
   while ((d->T + a.rows - 1) / a.rows * h->Hkv > (1 << 22)) a.rows *= 2;   // (a launch's threads stay below 2^32)
-  a.tokens = per >= 256 ? 1 : (int)(256 / per);
-  while (a.tokens < 64 && d->T > 4096 * (int64_t)a.tokens) a.tokens *= 2;
+  a.tokens = tokens_of(d->T, h->Hq * (h->D / 8));
   a.blocks = (unsigned)((d->T + a.rows - 1) / a.rows * h->Hkv);
   const dim3 grid(a.blocks + (q ? (unsigned)((d->T + a.tokens - 1) / a.tokens) : 0)), block(256);
   with_width(h->D, [&](auto D) {
@@ -875,7 +895,8 @@ hipError_t launch_cache_read(const xhc_dims* d, const xhc_heads* h, const xhc_ca
                              hipStream_t s) {
   CacheArgs a = args_of(d, h, c, starts, lens, pages, pool);
   a.k = k, a.v = v;
-  const dim3 grid((unsigned)d->T), block(256);
+  a.tokens = tokens_of(d->T, h->Hkv * (h->D / 8));
+  const dim3 grid((unsigned)((d->T + a.tokens - 1) / a.tokens)), block(256);
   with_width(h->D, [&](auto D) {
     if (d->state_dtype == XHC_BF16)
       k_cache_read<uint16_t, D.value><<<grid, block, 0, s>>>(a);

@@ -190,7 +190,7 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream   # an index: looked up fastest
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # (current_stream makes an object first)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -966,11 +966,14 @@ def _slopes(h, slopes, device):
 
 
 def _take(t, dtype, shape, dev, name):
-    """An argument of a call: of this dtype, shape (a tuple) and device."""
+    """The address of an argument of a call: of this dtype, shape (a tuple) and device."""
     if t.dtype is not dtype or t.shape != shape:
         _expect(t, dtype, shape, name)
     if t.get_device() != dev.index:
         raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 class Rotation:
@@ -986,9 +989,9 @@ class Rotation:
         self.buffers = [None, None]    # of forward, of backward
 
     def _run(self, x, pos, out, inverse, stream):
-        _take(x, self.dtype, self.shape, self.device, "the heads")
+        at = _take(x, self.dtype, self.shape, self.device, "the heads")
         if pos is not None:
-            _take(pos, torch.int32, (self.d.T,), self.device, "pos")
+            pos = _take(pos, torch.int32, (self.d.T,), self.device, "pos")
         _enqueues(self.device)
         if out is None:
             if self.buffers[inverse] is None:
@@ -997,7 +1000,7 @@ class Rotation:
             out = self.buffers[inverse]
         else:
             _take(out, self.dtype, self.shape, self.device, "out")
-        xhc_rotate(self.d, self.h, x, pos, self.table, self.positions, inverse, out, stream)
+        xhc_rotate(self.d, self.h, at, pos, self.table, self.positions, inverse, out, stream)
         return out
 
     def forward(self, qkv, pos=None, out=None, stream=None):
@@ -1029,9 +1032,9 @@ class Attention:
         if starts is not None:
             if n < 0:
                 raise ValueError("starts holds one entry more than there are documents")
-            _take(starts, torch.int32, (n + 1,), self.device, "starts")
+            starts = _take(starts, torch.int32, (n + 1,), self.device, "starts")
         if prefix is not None:
-            _take(prefix, torch.int32, (n,), self.device, "prefix")
+            prefix = _take(prefix, torch.int32, (n,), self.device, "prefix")
         _enqueues(self.device)
         if self.span is None:
             with _within(stream):
@@ -1040,9 +1043,9 @@ class Attention:
         return self.span
 
     def forward(self, qkv, span=None, stream=None):
-        _take(qkv, self.out.dtype, self.shape, self.device, "qkv")
+        qkv = _take(qkv, self.out.dtype, self.shape, self.device, "qkv")
         if span is not None:
-            _take(span, torch.int32, (self.d.T, 2), self.device, "span")
+            span = _take(span, torch.int32, (self.d.T, 2), self.device, "span")
         _enqueues(self.device)
         xhc_attn(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, stream)
         return self.out
@@ -1067,7 +1070,7 @@ class TrainableAttention(Attention):
     def backward(self, dout, stream=None):
         if self.seen is None:
             raise ValueError("backward without a forward")
-        _take(dout, self.out.dtype, self.out.shape, self.device, "dout")
+        dout = _take(dout, self.out.dtype, self.out.shape, self.device, "dout")
         _enqueues(self.device)
         qkv, span = self.seen
         xhc_attn_bwd(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, dout, self.dqkv, self.ws, stream)
@@ -1105,36 +1108,35 @@ class KVCache:
 
     def _check(self, starts, lens, pages):
         B = self.c.B
-        _take(starts, torch.int32, (B + 1,), self.device, "starts")
-        _take(lens, torch.int32, (B,), self.device, "lens")
-        _take(pages, torch.int32, (B, self.c.per_seq), self.device, "pages")
+        at = (_take(starts, torch.int32, (B + 1,), self.device, "starts"),
+              _take(lens, torch.int32, (B,), self.device, "lens"),
+              _take(pages, torch.int32, (B, self.c.per_seq), self.device, "pages"))
         _enqueues(self.device)
+        return at
 
     def append(self, qkv, starts, lens, pages, stream=None):
         """Stores the rotated key heads and the value heads of qkv [T, Hq + 2 Hkv, D]; returns the rotated query heads
         [T, Hq, D]."""
-        _take(qkv, self.q.dtype, self.shape, self.device, "qkv")
-        self._check(starts, lens, pages)
-        xhc_cache_append(self.d, self.h, self.c, qkv, self.table, self.positions, starts, lens, pages, self.pool,
-                         self.q, stream)
+        qkv = _take(qkv, self.q.dtype, self.shape, self.device, "qkv")
+        xhc_cache_append(self.d, self.h, self.c, qkv, self.table, self.positions,
+                         *self._check(starts, lens, pages), self.pool, self.q, stream)
         return self.q
 
     def read(self, starts, lens, pages, stream=None):
         """The keys and values [T, Hkv, D] held for the call's tokens (zeros until a token's have been read)."""
-        self._check(starts, lens, pages)
+        at = self._check(starts, lens, pages)
         if self.k is None:
             with _within(stream):
                 self.k, self.v = (torch.zeros(self.d.T, self.h.Hkv, self.h.D, dtype=self.q.dtype, device=self.device)
                                   for _ in range(2))
-        xhc_cache_read(self.d, self.h, self.c, starts, lens, pages, self.pool, self.k, self.v, stream)
+        xhc_cache_read(self.d, self.h, self.c, *at, self.pool, self.k, self.v, stream)
         return self.k, self.v
 
     def attend(self, q, starts, lens, pages, stream=None):
         """Attention of q [T, Hq, D], the call's tokens (appended before), over their sequences up to themselves."""
-        _take(q, self.q.dtype, self.q.shape, self.device, "q")
-        self._check(starts, lens, pages)
-        xhc_attn_cache(self.d, self.h, self.c, q, self.slopes, starts, lens, pages, self.pool, self.out, self.ws,
-                       stream)
+        q = _take(q, self.q.dtype, self.q.shape, self.device, "q")
+        xhc_attn_cache(self.d, self.h, self.c, q, self.slopes, *self._check(starts, lens, pages), self.pool, self.out,
+                       self.ws, stream)
         return self.out
 
 
