@@ -82,6 +82,16 @@ __device__ __forceinline__ int sequence_of(const int* starts, int B, int64_t t, 
   return __builtin_amdgcn_readfirstlane(first);
 }
 
+// four pairs of neighbours by w (cosine, sine of each)
+__device__ __forceinline__ void turn_pairs(float (&x)[8], const float* w) {
+  float a[4], b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = x[2 * i], b[i] = x[2 * i + 1];
+  turn<4>(a, b, w, 1.f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = a[i], x[2 * i + 1] = b[i];
+}
+
 // Eight consecutive channels from channel c of a head, rotated at the position
 // whose table row is cs.
 template <typename TS>
@@ -89,13 +99,9 @@ __device__ __forceinline__ void rotated8(const TS* head, int c, const float* cs,
   Vec8<TS>::load(head + c, x);
   if (c >= R) return;
   if (pairs) {
-    float w[8], a[4], b[4];
+    float w[8];
     Vec8<float>::load(cs + c, w);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = x[2 * i], b[i] = x[2 * i + 1];
-    turn<4>(a, b, w, 1.f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = a[i], x[2 * i + 1] = b[i];
+    turn_pairs(x, w);
   } else {
     const bool low = c < R / 2;
     float w[16], y[8];
@@ -148,8 +154,8 @@ __device__ __forceinline__ uint32_t hold8(const float (&x)[8], uint32_t& bits) {
   return w;
 }
 
-// The last workgroups rotate the queries, a few tokens each.  Each of the
-// `blocks` in front of them, which take longer, looks after `rows` tokens for one head: it stores the block of each
+// Some workgroups rotate the queries, a few tokens each.  Each of the `blocks`
+// others, which wait for more and move less, looks after `rows` tokens for one head: it stores the block of each
 // token that is the call's first in its block, which may go on behind them;
 // so no two workgroups write to a block.  Tokens that were there before keep
 // their bits.
@@ -162,8 +168,14 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
   const int tid = threadIdx.x, lane = tid % 64, H = a.Hq + 2 * a.Hkv;
   const int64_t cap = (int64_t)a.per_seq * a.page;
   const TS* qkv = static_cast<const TS*>(a.qkv);
-  if (blockIdx.x >= a.blocks) {
-    const int64_t t0 = (int64_t)(blockIdx.x - a.blocks) * a.tokens;
+  // eights of both kinds in turn, which go to the eight XCDs, then what is left of one
+  const unsigned eights = (a.blocks < gridDim.x - a.blocks ? a.blocks : gridDim.x - a.blocks) / 8;
+  const bool turns = blockIdx.x < 16 * eights;
+  const unsigned left = a.blocks - 8 * eights;
+  const bool queries = turns ? blockIdx.x % 16 >= 8 : blockIdx.x - 16 * eights >= left;
+  const unsigned mine = turns ? blockIdx.x / 16 * 8 + blockIdx.x % 8 : blockIdx.x - 8 * eights - (queries ? left : 0);
+  if (queries) {
+    const int64_t t0 = (int64_t)mine * a.tokens;
     for (int i = tid / 64; i < a.tokens; i += 4) {
       const int64_t t = t0 + i;
       const int b = t < a.T ? sequence_of(a.starts, a.B, t, lane) : -1;
@@ -172,25 +184,48 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
       if (lane == 0) pos[i] = p < cap ? p : -1;
     }
     __syncthreads();
-    TS* q = static_cast<TS*>(a.q);
-    const int all = a.tokens * a.Hq * P;
-    for (int u0 = tid; u0 < all; u0 += 512) {    // two at a time, their loads first (of the first token where one is none)
-      float x[2][8];
-      TS* to[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int u = u0 + 256 * k, c = u % P * 8, hd = u / P % a.Hq, i = u / P / a.Hq;
-        const int64_t p = u < all ? pos[i] : -1, t = p < 0 ? t0 : t0 + i;
-        to[k] = p < 0 ? nullptr : q + (t * a.Hq + hd) * D + c;
-        rotated8<TS>(qkv + (t * H + hd) * D, c, a.table + (p < 0 ? 0 : p) * a.R, a.R, a.pairs, x[k]);
+    // a thread has 16 channels (rotated ones with their partners) of some heads
+    // of a token, which share a table's row; two heads' loads first
+    constexpr int per = D / 16, slots = 256 / per;
+    const int heads = min(a.Hq, max(1, slots / a.tokens)), n = slots / heads, j = tid % per, slot = tid / per;
+    if (slot >= n * heads) return;
+    for (int i = slot / heads; i < a.tokens; i += n) {
+      const int64_t p = pos[i];
+      if (p < 0) continue;
+      const bool turned = 16 * j < a.R, split = turned && !a.pairs;
+      float cs[16];
+      if (turned) {
+        Vec8<float>::load(a.table + p * a.R + 16 * j, *reinterpret_cast<float(*)[8]>(cs));
+        Vec8<float>::load(a.table + p * a.R + 16 * j + 8, *reinterpret_cast<float(*)[8]>(cs + 8));
       }
+      const int ca = split ? 8 * j : 16 * j, cb = split ? 8 * j + a.R / 2 : 16 * j + 8;
+      const TS* src = qkv + (t0 + i) * H * D;
+      TS* q = static_cast<TS*>(a.q) + (t0 + i) * a.Hq * D;
+      for (int h0 = slot % heads; h0 < a.Hq; h0 += 2 * heads) {
+        float x[2][8], y[2][8];
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (to[k]) Vec8<TS>::store(to[k], x[k]);
+        for (int k = 0; k < 2; ++k) {
+          const int h = min(h0 + k * heads, a.Hq - 1);
+          Vec8<TS>::load(src + h * D + ca, x[k]);
+          Vec8<TS>::load(src + h * D + cb, y[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int h = h0 + k * heads;
+          if (h >= a.Hq) break;
+          if (split) {
+            turn<8>(x[k], y[k], cs, 1.f);
+          } else if (turned) {
+            turn_pairs(x[k], cs);
+            turn_pairs(y[k], cs + 8);
+          }
+          Vec8<TS>::store(q + h * D + ca, x[k]);
+          Vec8<TS>::store(q + h * D + cb, y[k]);
+        }
+      }
     }
     return;
   }
-  const unsigned mine = blockIdx.x;
   const int head = mine % a.Hkv;
   int64_t t = (int64_t)(mine / a.Hkv) * a.rows;
   const int64_t behind = t + a.rows < a.T ? t + a.rows : a.T;
