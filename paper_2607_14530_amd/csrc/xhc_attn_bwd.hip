@@ -344,13 +344,13 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
       const bool cut = e.z > j0 || e.w < j0 + KEYS;
       uint64_t bad = 0;
       if (cut) {
-        bad = TL::clean(Q, bits, wave, again(lane)) | TL::clean(G, bits + 1, wave, again(lane));
-        // rows whose lse or delta is not finite count as such (rows that see nothing are among them)
+        // rows whose lse or delta is not finite count as such (rows that see nothing are among them);
+        // all others are finite: an infinity or NaN of a query makes its lse one, unless a cap
+        // bounds the scores, and one of do its delta (0 times it is NaN)
         float* r = reinterpret_cast<float*>(Q + ST::kRows);
         const uint64_t more = __ballot(!(fabsf(r[lane]) <= FLT_MAX && fabsf(r[64 + lane]) <= FLT_MAX));
-        if (more) {
-          bad |= more;
-          lds_barrier();
+        if (more || (EX && a.cap > 0.f)) {
+          bad = more | TL::clean(Q, bits, wave, again(lane)) | TL::clean(G, bits + 1, wave, again(lane));
           if (wave == 0 && (more >> lane & 1)) r[lane] = r[64 + lane] = 0.f;
           lds_barrier();
         }
