@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   constexpr int ROWS = 128 / NC, RW = kAttnWaves / NC, NB = 2 / NC;   // blocks of keys of a wave
   __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
   __shared__ int4 red[kAttnWaves];
-  __shared__ uint64_t bits;
+  __shared__ uint64_t bits[2];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
   attn_place(a.Hq, (int)((a.T + ROWS - 1) / ROWS), head, tile);
@@ -59,18 +59,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     TL::copy(vb, stride, first * kTile, T1, at + TL::kBytes, wave, lane);
     for (int kt = first; kt < end; ++kt) {
       const uint32_t off = (kt - first) % 2 * 2 * TL::kBytes, next = 2 * TL::kBytes - off;
+      unsigned char *K = lds + off, *V = K + TL::kBytes;
+      const int j0 = kt * kTile;
+      const bool cut = j0 < ex.z || j0 + kTile > ex.w;      // some row does not see all of the tile
       wait_loads();
+      if (cut) TL::clean(V, bits + (kt - first) % 2, wave, again(lane));
       lds_barrier();
       if (kt + 1 < end) {
         const int ln = again(lane);
         TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, ln);
         TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, ln);
       }
-      unsigned char *K = lds + off, *V = K + TL::kBytes;
-      const int j0 = kt * kTile;
-      const bool cut = j0 < ex.z || j0 + kTile > ex.w;      // some row does not see all of the tile
-      uint64_t bad = 0;
-      if (cut) bad = TL::clean(V, &bits, wave, again(lane));
+      const uint64_t bad = cut ? bits[(kt - first) % 2] : 0;
       if (j0 >= own.y || j0 + kTile <= own.x) continue;     // no row of this wave sees a key of the tile
       f32x16 s[NB];
 #pragma unroll

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   constexpr int ROWS = 128 / NC, RW = kAttnWaves / NC, NB = 2 / NC;
   __shared__ __align__(1024) unsigned char lds[4 * TL::kBytes];
   __shared__ int4 red[kAttnWaves];
-  __shared__ uint64_t bits;
+  __shared__ uint64_t bits[2];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
   attn_place(a.Hq, (int)((a.T + ROWS - 1) / ROWS), head, tile);
@@ -130,18 +130,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     TL::copy(vb, stride, first * kTile, T1, at + TL::kBytes, wave, lane);
     for (int kt = first; kt < end; ++kt) {
       const uint32_t off = (kt - first) % 2 * 2 * TL::kBytes, next = 2 * TL::kBytes - off;
+      unsigned char *K = lds + off, *V = K + TL::kBytes;
+      const int j0 = kt * kTile;
+      const bool cut = j0 < ex.z || j0 + kTile > ex.w;
       wait_loads();
+      if (cut) TL::clean(K, bits + (kt - first) % 2, wave, again(lane));
       lds_barrier();
       if (kt + 1 < end) {
         const int ln = again(lane);
         TL::copy(kb, stride, (kt + 1) * kTile, T1, at + next, wave, ln);
         TL::copy(vb, stride, (kt + 1) * kTile, T1, at + next + TL::kBytes, wave, ln);
       }
-      unsigned char *K = lds + off, *V = K + TL::kBytes;
-      const int j0 = kt * kTile;
-      const bool cut = j0 < ex.z || j0 + kTile > ex.w;
-      uint64_t bad = 0;
-      if (cut) bad = TL::clean(K, &bits, wave, again(lane));
+      const uint64_t bad = cut ? bits[(kt - first) % 2] : 0;
       const bool none = j0 >= own.y || j0 + kTile <= own.x;   // no row of this wave sees a key of the tile
 #pragma unroll 1
       for (int rb = none ? 2 : kc; rb < kc + NB; ++rb) {
@@ -350,7 +350,10 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
         float* r = reinterpret_cast<float*>(Q + ST::kRows);
         const uint64_t more = __ballot(!(fabsf(r[lane]) <= FLT_MAX && fabsf(r[64 + lane]) <= FLT_MAX));
         if (more || (EX && a.cap > 0.f)) {
-          bad = more | TL::clean(Q, bits, wave, again(lane)) | TL::clean(G, bits + 1, wave, again(lane));
+          TL::clean(Q, bits, wave, again(lane));
+          TL::clean(G, bits + 1, wave, again(lane));
+          lds_barrier();
+          bad = more | bits[0] | bits[1];
           if (wave == 0 && (more >> lane & 1)) r[lane] = r[64 + lane] = 0.f;
           lds_barrier();
         }
