@@ -521,8 +521,9 @@ xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, cons
  *   slopes  [Hq] fp32 or NULL
  *   saved   NULL, or xhc_attn_saved_bytes(d, h) bytes that receive the rows'
  *           sums, and what rounding out has left, for xhc_attn_bwd
- * A token that sees nothing gets zeros.  Tokens that are not seen do not matter, whatever they hold; where a token that is seen
- * holds infinities or NaN, all of a row that sees it may become NaN.
+ * A token that sees nothing gets zeros.  Tokens that are not seen do not matter,
+ * whatever they hold; where a token that is seen holds infinities or NaN, all
+ * of a row that sees it may become NaN.
  * xhc_attn_bwd - dqkv [T, Hq + 2 Hkv, D] from qkv, span, slopes as in the
  *   forward, its out and saved, and dout [T,Hq,D]; slopes get no gradient.
  *   workspace: xhc_attn_workspace_bytes(d, h) bytes.

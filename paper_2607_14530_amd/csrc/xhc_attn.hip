@@ -6,6 +6,8 @@
 // Forward (k_attn): a workgroup takes 128 queries of a head, a wave 32 of them,
 // and goes once over the keys that its rows see, 64 at a time, with the running
 // maximum and sum of each row.
+#include <float.h>
+
 #include "xhc_attn.h"
 
 namespace xhc {
@@ -98,6 +100,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int j = 32 * rb + sum_row(r);
+            if (MODE == 1 && s[rb][r] == kNoKey) s[rb][r] = -FLT_MAX;      // seen, with a score of -cap
             if (!(j >= lo && j < hi)) s[rb][r] = kNoKey;
           }
         if (bad) {
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       top = max_halves(top);
       // (s: still the raw products where the scores rise with them)
       if (MODE == 0) top *= sc.mul;
-      if (MODE == 1 && top != kNoKey) top = fmaf(-2.f * sc.cap, sc.share_of(top), sc.cap);
+      if (MODE == 1 && (!cut || top != kNoKey)) top = fmaf(-2.f * sc.cap, sc.share_of(top), sc.cap);
       // The row's reference only follows its maximum when that is 2^8 above it:
       // probabilities up to 256 are as exact, and sums are rarely rescaled.
       if (__any(top > m + 8.f)) {

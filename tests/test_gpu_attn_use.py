@@ -63,6 +63,45 @@ def test_what_is_not_seen_does_not_matter(bad, dtype):
     assert bool((out[180:] == 0).all()) and bool((grad[180:] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_one_bad_channel_of_a_query_or_its_gradient(bad, cap, dtype):
+    """A query, or a row of dout, with one channel that is not finite only changes its own row and the gradients of keys
+    that it sees (a cap bounds the scores of an infinite query, whose sums are then finite)."""
+    T, Hq, Hkv, D = 330, 6, 2, 64
+    starts = i32([0, 100, 300])
+    qkv, dout = inputs(T, Hq, Hkv, D, dtype, 2)
+    att = bundle(T, T, Hq, Hkv, D, dtype, cap=cap)
+    span = att.spans(starts)
+    out, grad = att.forward(qkv, span).clone(), att.backward(dout).clone()
+    for t in (0, 63, 99, 130, 255, 299):
+        first, end = (0, 100) if t < 100 else (100, 300)
+        for of_query in (True, False):
+            q2, d2 = qkv.clone(), dout.clone()
+            (q2 if of_query else d2)[t, 4, 37] = bad             # query head 4: of key and value head 1
+            out2, grad2 = att.forward(q2, span).clone(), att.backward(d2).clone()
+            same = torch.ones(T, Hq, dtype=torch.bool, device="cuda")
+            same[t, 4] = not of_query
+            assert torch.equal(out2[same], out[same]), (t, of_query)
+            same = torch.ones(T, Hq + 2 * Hkv, dtype=torch.bool, device="cuda")
+            same[t, 4] = False
+            same[first:t + 1, Hq + 1] = same[first:t + 1, Hq + Hkv + 1] = False
+            assert torch.equal(grad2[same], grad[same]), (t, of_query)
+            row = grad2[t, 4].float()
+            if of_query and cap and bad == bad:  # scores of an infinite query are cap or -cap, where tanh' = 0
+                assert bool((row == 0).all()), t
+                k, v = (qkv[first:t + 1, h].double() for h in (Hq + 1, Hq + Hkv + 1))
+                p = torch.softmax(cap * torch.sign(bad * k[:, 37]), 0)
+                # the row's own values are among those; p is rounded, and so is what it is divided by, and the result
+                bound = 3 * torch.finfo(dtype).eps / 2 if dtype is BF else 2.0 ** -16
+                err = (out2[t, 4].double() - (p[:, None] * v).sum(0)).abs().max()
+                assert float(err) <= bound * float(v.abs().max()), (t, float(err))
+            else:
+                assert not bool(torch.isfinite(row).all()), (t, of_query)
+            assert bool(torch.isfinite(grad2[t + 1:end].float()).all()), (t, of_query)
+
+
 def test_the_same_twice():
     """The same bits from call to call, whatever the buffers held."""
     T, Hq, Hkv, D = 700, 8, 2, 128
