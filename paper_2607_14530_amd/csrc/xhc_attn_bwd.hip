@@ -483,10 +483,12 @@ constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 // Parts of the sums of dk and dv, which are added afterwards: the chip holds
 // 512 workgroups of four waves, of unlike lengths where masks cut; with less
-// than twice as many, a group's heads are divided among several.  Where those
-// do not give each CU a workgroup, so are the tiles of queries that see a
-// workgroup's keys (T = 777, Hq = 6, Hkv = 2, D = 96, fp32: 42 workgroups
-// without, 146 us).
+// than twice as many, a group's heads are divided among several (8190 tokens in
+// documents, Hq = 16, Hkv = 4, D = 64: backward 157 us in four parts, 189 in
+// two).  Where those leave room, so are the tiles of queries that see a
+// workgroup's keys, in up to eight slices (backward of T = 815, Hq = 14, Hkv =
+// 2, D = 128: 122 us without slices, 95 with a workgroup of four waves for each
+// CU, 86 with two; T = 777, Hq = 6, Hkv = 2, D = 96, fp32: 209, 128, 121).
 struct Parts {
   int parts, slices;                             // parts = shares of a group's heads times slices of the queries
 };
@@ -496,7 +498,7 @@ Parts parts_of(int64_t T, int Hq, int Hkv, int keys) {
   if (T == 0) return {1, 1};
   for (int p = 1; p < g; ++p)
     if (g % p == 0 && wg * p * keys >= 1024 * 128) return {p, 1};
-  int64_t n = 256 * 128 / (wg * g * keys);
+  int64_t n = 512 * 128 / (wg * g * keys);
   n = n < 1 ? 1 : n < 8 ? n : 8;
   n = n < tiles ? n : tiles;
   return {g * (int)n, (int)n};
