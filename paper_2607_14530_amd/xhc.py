@@ -11,6 +11,9 @@ for convenience; they add no arithmetic.  ``RMSNorm`` and ``FeedForward`` (and
 their trainable forms, whose forward and backward ``Stack`` takes as a
 sublayer's functions) do the same for an MLP-type sublayer's own function, and
 ``clip_grad_norm`` for the clip of the gradients that a backward has given.
+``Rotation``, ``Attention`` and ``TrainableAttention`` are an attention-type
+sublayer's own function between its projections, ``KVCache`` its serving form:
+a paged cache in 4 bits and the attention over it.
 """
 
 from __future__ import annotations
