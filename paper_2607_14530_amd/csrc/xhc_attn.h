@@ -272,6 +272,7 @@ struct AttnArgs {
   int64_t T, S, Tp;
   int Hq, Hkv, window;
   int parts, slices;        // of dk and dv: shares of a group's heads times slices of the queries
+  int qslices;              // of dq: slices of the keys
   float scale, cap;
 };
 

@@ -98,7 +98,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   __shared__ uint64_t bits[2];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int head, tile;
-  attn_place(a.Hq, (int)((a.T + ROWS - 1) / ROWS), head, tile);
+  attn_place(a.Hq * a.qslices, (int)((a.T + ROWS - 1) / ROWS), head, tile);
+  const int slice = head % a.qslices;
+  head /= a.qslices;
   const int kc = NC == 1 ? 0 : wave / RW;
   const int kvh = head / (a.Hq / a.Hkv), H = a.Hq + 2 * a.Hkv;
   const int t = tile * ROWS + wave % RW * 32 + lane % 32, T1 = (int)a.T - 1;
@@ -115,8 +117,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   f32x16 dq[F];
 #pragma unroll
   for (int f = 0; f < F; ++f) dq[f] = f32x16{};
-  const int first = ex.x / kTile, end = (ex.y + kTile - 1) / kTile;
-  if (ex.x < ex.y) {
+  int first = ex.x / kTile, end = (ex.y + kTile - 1) / kTile;
+  if (a.qslices > 1) {                           // the keys of this slice
+    const int n = end - first, of = first;
+    first = of + n * slice / a.qslices;
+    end = of + n * (slice + 1) / a.qslices;
+  }
+  if (ex.x < ex.y && first < end) {
     Score<TS> sc;
     sc.init(a, head);
     const int64_t tc = row ? t : T1;
@@ -210,6 +217,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     for (int f = 0; f < F; ++f)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[f][r] += part[(16 * f + r) * 64];
+  }
+  if (a.qslices > 1) {
+    float* p = a.part + (((int64_t)slice * a.T + t) * a.Hq + head) * D;
+#pragma unroll
+    for (int f = 0; f < F; ++f) store_sums<float>(dq[f], a.scale, p + 32 * f, row, lane);
+    return;
   }
   TS* p = reinterpret_cast<TS*>(a.dqkv) + (int64_t)t * H * D + head * D;
 #pragma unroll
@@ -464,7 +477,8 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
   }
 }
 
-// dk and dv from the parts, added in order; `row` = 2 Hkv D elements a token
+// Sums of a token's `row` elements from their parts, added in order: dk and dv,
+// or dq (Hq = 0: what lies in front of them)
 template <typename TS>
 __global__ __launch_bounds__(256) void k_attn_join(int64_t T, int row, int parts, const float* part, int H, int Hq, int D,
                                                    TS* dqkv) {
@@ -507,6 +521,18 @@ Parts parts_of(int64_t T, int Hq, int Hkv, int keys) {
   return {g * (int)n, (int)n};
 }
 
+// Slices of the keys for dq, added afterwards, where the rows are few and the keys
+// many: until the chip has two workgroups a CU (fp32: one), with four tiles each
+// (backward of T = 777, Hq = 6, Hkv = 2, D = 96, fp32: 121 -> 85 us in three; T =
+// 763, Hq = 4, Hkv = 4, D = 64, bf16: 45 -> 43 in two).
+int dq_slices(bool f32, int64_t T, int Hq) {
+  if (T == 0 || attn_parts(T, Hq) == 1) return 1;
+  const int64_t wg = (T + 63) / 64 * Hq, tiles = (T + kTile - 1) / kTile;
+  int64_t n = (f32 ? 256 : 512) / wg;
+  n = n < tiles / 4 ? n : tiles / 4;
+  return n < 1 ? 1 : n < 4 ? (int)n : 4;
+}
+
 template <typename TS, int D, bool EX> hipError_t run_bwd(AttnArgs a, char* ws, hipStream_t s) {
   const size_t heads = up((size_t)a.Tp * a.Hq * 4), rows = up((size_t)a.Tp * 4);
   float* delta = reinterpret_cast<float*>(ws);
@@ -527,7 +553,12 @@ template <typename TS, int D, bool EX> hipError_t run_bwd(AttnArgs a, char* ws, 
   if (attn_parts(a.T, a.Hq) == 1)
     k_attn_dq<TS, D, EX, 1><<<dim3((unsigned)((a.T + 127) / 128) * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
   else
-    k_attn_dq<TS, D, EX, 2><<<dim3((unsigned)((a.T + 63) / 64) * a.Hq), dim3(64 * kAttnWaves), 0, s>>>(a);
+    k_attn_dq<TS, D, EX, 2><<<dim3((unsigned)((a.T + 63) / 64) * a.Hq * a.qslices), dim3(64 * kAttnWaves), 0, s>>>(a);
+  if (a.qslices > 1) {
+    const int row = a.Hq * D;
+    k_attn_join<TS><<<dim3((unsigned)((a.T * row / 8 + 255) / 256)), dim3(256), 0, s>>>(
+        a.T, row, a.qslices, a.part, a.Hq + 2 * a.Hkv, 0, D, static_cast<TS*>(a.dqkv));
+  }
   return hipGetLastError();
 }
 
@@ -546,8 +577,10 @@ template <typename TS> hipError_t run_bwd_of(int D, const AttnArgs& a, char* ws,
 size_t attn_bwd_ws_bytes(int state_dtype, int64_t T, int Hq, int Hkv, int D) {
   const int64_t Tp = (T + kTile - 1) / kTile * kTile;
   const int parts = parts_of(T, Hq, Hkv, 32 * dkv_waves(state_dtype == XHC_F32, D)).parts;
-  return up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) +
-         (parts > 1 ? (size_t)parts * T * 2 * Hkv * D * 4 : 0);
+  const int slices = dq_slices(state_dtype == XHC_F32, T, Hq);
+  const size_t kv = parts > 1 ? (size_t)parts * T * 2 * Hkv * D * 4 : 0, q = slices > 1 ? (size_t)slices * T * Hq * D * 4 : 0;
+  // (the parts of dk and dv are added before dq begins: one place for both)
+  return up((size_t)Tp * Hq * 4) + 2 * up((size_t)Tp * 4) + up((size_t)Tp / kTile * 16) + (kv > q ? kv : q);
 }
 
 hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, const int32_t* span,
@@ -566,6 +599,7 @@ hipError_t launch_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qk
   a.Hq = h->Hq, a.Hkv = h->Hkv, a.window = h->window;
   const Parts parts = parts_of(d->T, h->Hq, h->Hkv, 32 * dkv_waves(d->state_dtype == XHC_F32, h->D));
   a.parts = parts.parts, a.slices = parts.slices;
+  a.qslices = dq_slices(d->state_dtype == XHC_F32, d->T, h->Hq);
   a.scale = h->scale, a.cap = h->cap;
   return d->state_dtype == XHC_BF16 ? run_bwd_of<uint16_t>(h->D, a, static_cast<char*>(ws), s)
                                     : run_bwd_of<float>(h->D, a, static_cast<char*>(ws), s);

@@ -53,6 +53,15 @@ def test_causal(T, S, Hq, Hkv, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,Hq,Hkv,D,kw", [
+    (513, 1, 1, 96, {}), (900, 2, 1, 64, dict(cap=15.0)), (1100, 3, 3, 128, dict(window=300)),
+    (777, 4, 2, 32, dict(slopes=[0.5, 0.1, 0.02, 0.0], starts=[0, 3, 600, 770], prefix=[1, 400, 0]))])
+def test_few_heads_of_many_tokens(T, Hq, Hkv, D, kw, dtype):
+    """Sums of dq, dk and dv in slices of the keys and queries, some of which have none."""
+    run(T, T, Hq, Hkv, D, dtype, seed=T, **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("cap,slopes,window", [(2.0, None, 0), (0.0, [0.25, 0.01, 0.5, 1.0], 0), (20.0, [0.1, 0.2, 0.0, 0.4], 70),
                                                (0.0, None, 1), (0.0, None, 64)])
 def test_cap_bias_window(cap, slopes, window, dtype):
