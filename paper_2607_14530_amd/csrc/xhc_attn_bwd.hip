@@ -524,7 +524,7 @@ Parts parts_of(int64_t T, int Hq, int Hkv, int keys) {
 // Slices of the keys for dq, added afterwards, where the rows are few and the keys
 // many: until the chip has two workgroups a CU (fp32: one), with four tiles each
 // (backward of T = 777, Hq = 6, Hkv = 2, D = 96, fp32: 121 -> 85 us in three; T =
-// 763, Hq = 4, Hkv = 4, D = 64, bf16: 45 -> 43 in two).
+// 763, Hq = 4, Hkv = 4, D = 64, bf16: 45 -> 43 in three).
 int dq_slices(bool f32, int64_t T, int Hq) {
   if (T == 0 || attn_parts(T, Hq) == 1) return 1;
   const int64_t wg = (T + 63) / 64 * Hq, tiles = (T + kTile - 1) / kTile;
