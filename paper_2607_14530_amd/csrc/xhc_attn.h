@@ -314,6 +314,23 @@ template <typename TS> struct Score {
     else
       return tanhf(x * mul);
   }
+  // tanh z and its derivative 1 - tanh^2 z = 4 e / (1 + e)^2, e = exp(-2 |z|), or
+  // 4 r (1 - r) with r = 1 / (1 + exp 2 |z|).  Relative to itself either is as exact
+  // next to the cap as elsewhere; 1 less the square of a rounded tanh is off by a
+  // third of it at z = 8.5, and 0 from 9 on.  (Backward of T = 8192 in one
+  // sequence, Hq = 32, Hkv = 8, D = 128, bf16, cap 30: 2490 us, 2460 with that
+  // square; T = 777, Hq = 6, Hkv = 2, D = 96, fp32: 113 and 106.)
+  __device__ __forceinline__ float tanh_of(float x, float& der) const {
+    if constexpr (sizeof(TS) == 2) {
+      const float r = share_of(fabsf(x));
+      der = 4.f * fmaf(-r, r, r);
+      return copysignf(fmaf(-2.f, r, 1.f), x);
+    } else {
+      const float e = expf(-2.f * fabsf(x * mul));
+      der = 4.f * e / ((1.f + e) * (1.f + e));
+      return tanhf(x * mul);
+    }
+  }
 };
 
 __device__ __forceinline__ float max_halves(float v) {
