@@ -1,0 +1,127 @@
+"""Attention at more workgroups than the chip has CUs, the form of calls with many
+rows: a workgroup takes 128 rows of a head, and the sums of dk and dv are those of a
+group's heads together, of some of them, or of each.  Against the formulas in 64
+bits for some of the heads, value by value within bounds that count the roundings."""
+
+import pytest
+import torch
+
+from paper_2607_14530_amd import xhc as X
+from tests import attn_util as U
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+NAME = {BF: "bf16", F32: "f32"}
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def some_heads(Hq, Hkv, groups):
+    """Rows of qkv [T, Hq + 2 Hkv, D] of these key and value heads with their query heads, and the query heads."""
+    g = Hq // Hkv
+    q = [h * g + i for h in groups for i in range(g)]
+    return q + [Hq + h for h in groups] + [Hq + Hkv + h for h in groups], q
+
+
+def compare(att, qkv, dout, lo, hi, span, Hq, Hkv, groups, cap=0.0, slopes=None):
+    D = qkv.shape[2]
+    out = att.forward(qkv.cuda(), span)
+    dqkv = att.backward(dout.cuda())
+    assert bool(torch.isfinite(out.float()).all()) and bool(torch.isfinite(dqkv.float()).all())
+    every, q = some_heads(Hq, Hkv, groups)
+    ref, dref = U.all_heads(qkv[:, every], lo, hi, len(q), len(groups), D ** -0.5, cap,
+                            None if slopes is None else [slopes[i] for i in q], dout[:, q])
+    U.assert_within(out[:, q], ref, "out")
+    got, n, m = dqkv[:, every], len(q), len(groups)
+    for name, a, b in (("dq", 0, n), ("dk", n, n + m), ("dv", n + m, n + 2 * m)):
+        U.assert_within(got[:, a:b], (dref[0][:, a:b], dref[1][:, a:b]), name)
+
+
+KINDS = {
+    "causal": dict(),
+    "window": dict(window=150),
+    "cap": dict(cap=10.0),
+    "slopes": dict(slopes=True),
+    "cap_slopes_window": dict(cap=4.0, slopes=True, window=90),
+    "documents": dict(starts=[0, 1, 130, 130, 600, 640, 1070]),
+    "prefixes_cap": dict(starts=[3, 256, 700, 1090], prefix=[100, 444, 30], cap=15.0),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows(kind, D, dtype):
+    k = KINDS[kind]
+    T, Hq, Hkv = 1100, 30, 6                     # nine workgroups for each of 30 heads
+    window, cap, starts, prefix = k.get("window", 0), k.get("cap", 0.0), k.get("starts"), k.get("prefix")
+    slopes = [0.5 ** (1 + i % 9) for i in range(Hq)] if "slopes" in k else None
+    S = 550 if kind in ("causal", "cap") else T
+    d = X.make_dims(T, 1, 1, 1, 32, S=S, state=NAME[dtype])
+    h = X.make_heads(Hq, Hkv, D, window=window, cap=cap)
+    att = X.TrainableAttention(d, h, slopes=None if slopes is None else torch.tensor(slopes, device="cuda"))
+    span = None if starts is None else att.spans(i32(starts), None if prefix is None else i32(prefix))
+    qkv, dout = U.inputs(T, Hq, Hkv, D, dtype, D + len(kind))
+    compare(att, qkv, dout, *U.spans(T, S, window, starts, prefix), span, Hq, Hkv, [0, 5], cap, slopes)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hq,Hkv,D,kw", [
+    (228, 114, 32, {}),                          # a workgroup has both heads of its group: no sums in parts
+    (206, 103, 128, dict(cap=10.0)),
+    (256, 64, 32, {}),                           # two shares of two heads
+    (240, 40, 64, dict(slopes=True)),            # three shares of two
+    (180, 30, 96, dict(window=200)),             # six of one
+])
+def test_shares_of_a_group(Hq, Hkv, D, kw, dtype):
+    T = 1100
+    slopes = [0.5 ** (1 + i % 7) for i in range(Hq)] if "slopes" in kw else None
+    d = X.make_dims(T, 1, 1, 1, 32, S=T, state=NAME[dtype])
+    h = X.make_heads(Hq, Hkv, D, window=kw.get("window", 0), cap=kw.get("cap", 0.0))
+    att = X.TrainableAttention(d, h, slopes=None if slopes is None else torch.tensor(slopes, device="cuda"))
+    qkv, dout = U.inputs(T, Hq, Hkv, D, dtype, Hq)
+    compare(att, qkv, dout, *U.spans(T, T, kw.get("window", 0)), None, Hq, Hkv, [1, Hkv - 1], kw.get("cap", 0.0), slopes)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cap,D", [(0.0, 64), (30.0, 64), (0.0, 128), (30.0, 32), (0.0, 96)])
+def test_bad_values_that_are_not_seen(cap, D, dtype):
+    """NaN and infinities in a token: what does not see it keeps its bits, forward and backward."""
+    T, Hq, Hkv = 1100, 32, 4
+    d = X.make_dims(T, 1, 1, 1, 32, S=T, state=NAME[dtype])
+    att = X.TrainableAttention(d, X.make_heads(Hq, Hkv, D, cap=cap))
+    span = att.spans(i32([0, 500, 1080]), i32([40, 0]))
+    qkv, dout = (z.cuda() for z in U.inputs(T, Hq, Hkv, D, dtype, 3))
+    dout[1080:] = 0
+    out, grad = att.forward(qkv, span).clone(), att.backward(dout).clone()
+    for t, bad in ((30, float("nan")), (333, float("inf")), (499, float("-inf")), (777, float("nan")), (1090, float("inf"))):
+        q2, d2 = qkv.clone(), dout.clone()
+        q2[t] = bad
+        d2[t] = bad
+        out2, grad2 = att.forward(q2, span).clone(), att.backward(d2).clone()
+        same = torch.ones(T, dtype=torch.bool, device="cuda")
+        gsame = same.clone()
+        first, end = (0, 500) if t < 500 else (500, 1080) if t < 1080 else (t, t + 1)
+        same[0 if t < 40 else t:end] = False     # who sees it
+        gsame[first:end] = False
+        if t < 1080:
+            assert not bool(torch.isfinite(out2[t:end].float()).all(-1).any())
+        assert torch.equal(out2[same], out[same]), t
+        assert torch.equal(grad2[gsame], grad[gsame]), t
+
+
+def test_the_same_twice():
+    """The same bits from call to call, whatever the buffers held."""
+    T, Hq, Hkv, D = 1100, 32, 8, 64
+    qkv, dout = (z.cuda() for z in U.inputs(T, Hq, Hkv, D, BF, 4))
+    att = X.TrainableAttention(X.make_dims(T, 1, 1, 1, 32, S=T), X.make_heads(Hq, Hkv, D))
+    a, b = att.forward(qkv).clone(), att.backward(dout).clone()
+    for fill in (0, 255):
+        for t in (att.ws, att.saved):
+            t.fill_(fill)
+        att.out.fill_(float("nan"))
+        att.dqkv.fill_(float("nan"))
+        assert torch.equal(att.forward(qkv), a) and torch.equal(att.backward(dout), b)
