@@ -14,6 +14,7 @@
 #include <float.h>
 
 #include "xhc_attn.h"
+#include "xhc_spans.h"
 
 namespace xhc {
 
@@ -207,11 +208,7 @@ __global__ __launch_bounds__(256) void k_attn_spans(int64_t T, int64_t S, int wi
   const int t = (int)t64;
   int from = t - (int)(t % S), hi = t + 1;
   if (starts) {
-    int a = 0, b = n;                       // the last i in [0, n] with starts[i] <= t, if starts[0] is
-    while (a < b) {
-      const int c = (a + b + 1) / 2;
-      if (starts[c] <= t) a = c; else b = c - 1;
-    }
+    const int a = last_start(starts, n, t);
     if (starts[0] > t || a == n) {
       span[t] = make_int2(0, 0);
       return;
