@@ -954,18 +954,33 @@ def rotation_table(positions, R, base=10000.0, device="cuda"):
     return torch.stack([torch.cos(a), torch.sin(a)], -1).float()
 
 
+def _settle():
+    """Waits for what a bundle's constructor has enqueued: its first call may then go to any stream.  (Where the
+    constructor itself is captured there is nothing to wait for before the replay.)"""
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream().synchronize()
+
+
+def _laid_out(t, device):
+    """The tensor itself where it is contiguous on the device, else a copy that is."""
+    c = t.to(device).contiguous()
+    if c is not t:
+        _settle()
+    return c
+
+
 def _table(h, table, device):
     if h.R == 0:
         return None, 0
     _expect(table, torch.float32, (table.shape[0], h.R // 2, 2), "table")
-    return table.to(device).contiguous(), table.shape[0]
+    return _laid_out(table, device), table.shape[0]
 
 
 def _slopes(h, slopes, device):
     if slopes is None:
         return None
     _expect(slopes, torch.float32, (h.Hq,), "slopes")
-    return slopes.to(device).contiguous()
+    return _laid_out(slopes, device)
 
 
 def _take(t, dtype, shape, dev, name):
@@ -1086,7 +1101,9 @@ class KVCache:
     (-1) is one that is not there.  Each call takes starts [sequences + 1], lens [sequences] and pages [sequences,
     per_sequence], int32 on the device: sequence b's newest tokens are starts[b] .. starts[b + 1] - 1 of the call's,
     the last of its lens[b].  ``pool``: that of another KVCache with the same heads, page and npages, for calls of
-    another number of tokens.  Outputs go to buffers of this object, overwritten by its next call."""
+    another number of tokens.  Outputs go to buffers of this object, overwritten by its next call but for the rows of
+    tokens that no sequence has or that lie outside its row of the page table (as in a padded batch), and in read() of
+    tokens that are not stored: those keep what an earlier call left there, zeros at first."""
 
     def __init__(self, d: Dims, h: Heads, table, sequences, per_sequence, page=64, npages=None, slopes=None,
                  pool=None, device="cuda"):
@@ -1103,11 +1120,12 @@ class KVCache:
         _on(pool, self.device, "pool")
         self.pool = pool
         sdt = _state_dtype(d)
-        self.q = torch.empty(d.T, h.Hq, h.D, dtype=sdt, device=self.device)
-        self.out = torch.empty_like(self.q)
-        self.k = self.v = None
+        # (k and v now and not by the first read: in a captured one the zeros would be part of every replay)
+        self.q, self.out = (torch.zeros(d.T, h.Hq, h.D, dtype=sdt, device=self.device) for _ in range(2))
+        self.k, self.v = (torch.zeros(d.T, h.Hkv, h.D, dtype=sdt, device=self.device) for _ in range(2))
         self.shape = (d.T, h.Hq + 2 * h.Hkv, h.D)
         self.ws = _bytes(xhc_attn_cache_workspace_bytes(d, h, self.c), self.device)
+        _settle()
 
     def _check(self, starts, lens, pages):
         B = self.c.B
@@ -1126,13 +1144,8 @@ class KVCache:
         return self.q
 
     def read(self, starts, lens, pages, stream=None):
-        """The keys and values [T, Hkv, D] held for the call's tokens (zeros until a token's have been read)."""
-        at = self._check(starts, lens, pages)
-        if self.k is None:
-            with _within(stream):
-                self.k, self.v = (torch.zeros(self.d.T, self.h.Hkv, self.h.D, dtype=self.q.dtype, device=self.device)
-                                  for _ in range(2))
-        xhc_cache_read(self.d, self.h, self.c, *at, self.pool, self.k, self.v, stream)
+        """The keys and values [T, Hkv, D] held for the call's tokens."""
+        xhc_cache_read(self.d, self.h, self.c, *self._check(starts, lens, pages), self.pool, self.k, self.v, stream)
         return self.k, self.v
 
     def attend(self, q, starts, lens, pages, stream=None):
