@@ -994,6 +994,11 @@ def _take(t, dtype, shape, dev, name):
     return t.data_ptr()
 
 
+def _version(t):
+    """How often torch has changed t in place; None where it does not count."""
+    return None if t.is_inference() else t._version
+
+
 class Rotation:
     """Position rotation of the query and key heads of qkv [T, Hq + 2 Hkv, D] by a table of cosines and sines
     (rotation_table).  Positions are t % d.S unless given (pos [T] int32).  Forward and backward each have a buffer
@@ -1071,7 +1076,8 @@ class Attention:
 
 class TrainableAttention(Attention):
     """An Attention that keeps what the backward needs and runs it: backward(dout) returns dL/dqkv of the last
-    forward's qkv and span (read again: they must still hold their values)."""
+    forward's qkv and span.  It reads them again, and the output that forward returned: they must still hold their
+    values.  An output that torch has changed in place since then is refused."""
 
     def __init__(self, d: Dims, h: Heads, slopes=None, device="cuda"):
         super().__init__(d, h, slopes, device)
@@ -1082,15 +1088,17 @@ class TrainableAttention(Attention):
 
     def forward(self, qkv, span=None, stream=None):
         out = super().forward(qkv, span, stream)
-        self.seen = (qkv, span)        # (of a forward that ran: a refused one changes nothing)
+        self.seen = (qkv, span, _version(out))       # (of a forward that ran: a refused one changes nothing)
         return out
 
     def backward(self, dout, stream=None):
         if self.seen is None:
             raise ValueError("backward without a forward")
+        qkv, span, version = self.seen
+        if _version(self.out) != version:
+            raise ValueError("the forward's output was changed in place: backward reads it again")
         dout = _take(dout, self.out.dtype, self.out.shape, self.device, "dout")
         _enqueues(self.device)
-        qkv, span = self.seen
         xhc_attn_bwd(self.d, self.h, qkv, span, self.slopes, self.out, self.saved, dout, self.dqkv, self.ws, stream)
         return self.dqkv
 
