@@ -72,3 +72,14 @@ def test_a_refused_forward_leaves_the_last_ones_input(calls):
             att.forward(bad)
         att.backward(torch.zeros(T, Hq, D, dtype=BF))
         assert calls[-1][1][2] is x
+
+
+def test_the_current_stream_by_public_names(monkeypatch):
+    """A torch without the short way to a stream's handle has the documented one."""
+    class Stream:
+        cuda_stream = 1234
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream)
+    assert X._stream(None) == 1234
+    assert X._stream(Stream) == 1234 and X._stream(77) == 77
