@@ -74,6 +74,13 @@ def make_dims(T, N, k, m, C, Kr=1, S=None, kappa=(4, 8, 12), sinkhorn_iters=20, 
     return d
 
 
+def _int32(**values):
+    """Refuses what a 32-bit field would cut to other values (ctypes does so without a word)."""
+    for name, v in values.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{name} does not fit 32 bits: {v}")
+
+
 class Heads(ctypes.Structure):
     _fields_ = [
         ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("R", ctypes.c_int32),
@@ -86,8 +93,9 @@ def make_heads(Hq, Hkv, D, rotary=None, pairing="halves", window=0, scale=None, 
     given), pairing "halves" or "neighbours", scale D^-1/2 unless given; window and cap 0 for none."""
     if pairing not in ("halves", "neighbours"):
         raise ValueError(f"pairing is 'halves' or 'neighbours', got {pairing!r}")
-    return Heads(Hq, Hkv, D, D if rotary is None else rotary,
-                 XHC_PAIRS_HALVES if pairing == "halves" else XHC_PAIRS_NEIGHBOURS, window,
+    rotary = D if rotary is None else rotary
+    _int32(Hq=Hq, Hkv=Hkv, D=D, rotary=rotary, window=window)
+    return Heads(Hq, Hkv, D, rotary, XHC_PAIRS_HALVES if pairing == "halves" else XHC_PAIRS_NEIGHBOURS, window,
                  D ** -0.5 if scale is None else scale, cap)
 
 
@@ -1059,6 +1067,7 @@ class Attention:
         if starts is not None:
             if n < 0:
                 raise ValueError("starts holds one entry more than there are documents")
+            _int32(documents=n)
             starts = _take(starts, torch.int32, (n + 1,), self.device, "starts")
         if prefix is not None:
             prefix = _take(prefix, torch.int32, (n,), self.device, "prefix")
@@ -1120,7 +1129,9 @@ class KVCache:
     def __init__(self, d: Dims, h: Heads, table, sequences, per_sequence, page=64, npages=None, slopes=None,
                  pool=None, device="cuda"):
         self.d, self.h, self.device = d, h, _here(device)
-        self.c = Cache(page, sequences * per_sequence if npages is None else npages, sequences, per_sequence)
+        npages = sequences * per_sequence if npages is None else npages
+        _int32(page=page, npages=npages, sequences=sequences, per_sequence=per_sequence)
+        self.c = Cache(page, npages, sequences, per_sequence)
         self.table, self.positions = _table(h, table, self.device)
         self.slopes = _slopes(h, slopes, self.device)
         n = xhc_cache_bytes(h, self.c)

@@ -83,3 +83,38 @@ def test_the_current_stream_by_public_names(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream)
     assert X._stream(None) == 1234
     assert X._stream(Stream) == 1234 and X._stream(77) == 77
+
+
+BIG = [2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 31 - 1, -2 ** 32 + 64]
+
+
+@pytest.mark.parametrize("v", BIG)
+def test_heads_that_do_not_fit_their_fields_are_refused(v):
+    """A field keeps 32 bits: a window of 2^32 + 5 would be one of 5."""
+    for kw in (dict(Hq=v), dict(Hkv=v), dict(D=v), dict(rotary=v), dict(window=v)):
+        with pytest.raises(ValueError):
+            X.make_heads(**{**dict(Hq=4, Hkv=2, D=64, scale=0.125), **kw})
+    assert X.make_heads(4, 2, 64, window=2 ** 31 - 1).window == 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("kw", [dict(sequences=65536, per_sequence=65537), dict(npages=2 ** 32 + 8), dict(page=2 ** 32 + 64),
+                                dict(sequences=2 ** 32 + 2), dict(per_sequence=2 ** 32 + 2, npages=8)])
+def test_caches_that_do_not_fit_their_fields_are_refused(calls, kw, monkeypatch):
+    """A pool of 2^32 + 65536 pages would be one of 65536, and what lies in the others lost."""
+    monkeypatch.setattr(X, "_settle", lambda: None, raising=False)
+    made = []
+    monkeypatch.setattr(torch, "zeros", lambda *a, **k: made.append(a))
+    h = X.make_heads(Hq, Hkv, D, rotary=0)
+    with pytest.raises(ValueError):
+        X.KVCache(X.make_dims(T, 1, 1, 1, 32), h, None, device="cpu", **{**dict(sequences=2, per_sequence=2, page=32), **kw})
+    assert not made
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32 + 1])
+def test_more_documents_than_their_number_holds_are_refused(calls, n):
+    class Starts:
+        dtype, shape = torch.int32, (n + 1,)
+        numel = staticmethod(lambda: n + 1)
+    with pytest.raises(ValueError):
+        attention().spans(Starts)
+    assert not calls
