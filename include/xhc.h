@@ -547,7 +547,8 @@ xhc_status xhc_attn_bwd(const xhc_dims* d, const xhc_heads* h, const void* qkv, 
  * position lens[b] - (starts[b+1] - t).  Tokens of no sequence are left alone,
  * as are those whose position is not in 0 .. per_seq page - 1.  A page that
  * several sequences hold must not be appended to.
- *   starts [B + 1], lens [B], pages [B, per_seq] int32, device
+ *   starts [B + 1] (ascending; the outputs are undefined where they are not),
+ *           lens [B], pages [B, per_seq] int32, device
  *   pool    xhc_cache_bytes(h, c) bytes, 256-byte aligned
  * Keys and values are held as 4-bit floats (sign, 2 exponent, 1 fraction bits:
  * 0, 1/2, 1, 3/2, 2, 3, 4, 6; nearest, ties to even) times a bf16 scale for 32

@@ -806,7 +806,8 @@ __global__ __launch_bounds__(64 * W) void k_cache_join(CacheArgs a, int ROWS, in
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = a.Hq / a.Hkv;
   const int64_t t = blockIdx.x;
   const int b = sequence_of(a.starts, a.B, t, lane);
-  if (b < 0 || t >= a.starts[b + 1]) return;
+  // (t in front of the start: only where starts do not ascend; its row would lie in front of the places)
+  if (b < 0 || t < a.starts[b] || t >= a.starts[b + 1]) return;
   const int64_t first = a.starts[b] > 0 ? a.starts[b] : 0;
   const int64_t p = a.lens[b] - (a.starts[b + 1] - t);
   if (p < 0 || p >= (int64_t)a.per_seq * a.page) return;

@@ -96,3 +96,25 @@ def test_a_new_bundle_is_ready_for_any_stream():
     out = c.attend(q, *args, stream=s)
     torch.cuda.synchronize()
     assert torch.equal(q, q0) and torch.equal(out, out0)
+
+
+@pytest.mark.parametrize("B", [3, 70])
+def test_starts_that_do_not_ascend_stay_within_the_buffers(B):
+    """Undefined outputs, but of the call's tokens only, and nothing of its workspace's surroundings is read as a sum
+    of theirs: a token in front of the start of the sequence that the search finds is left to others."""
+    T, per = 8, 64
+    c = cache(T, B, per)
+    n = c.ws.numel()
+    around = torch.full((n + 8192,), 255, dtype=torch.uint8, device="cuda")
+    assert around.data_ptr() % 16 == 0
+    c.ws = around[4096:4096 + n]
+    out = torch.full((T + 64, Hq, D), 7.0, dtype=BF, device="cuda")
+    c.out = out[32:32 + T]
+    starts, lens = [5, 6, 2] + [8] * (B - 2), [per * PAGE] * B
+    pages = torch.arange(B * per, device="cuda").int().view(B, per)
+    q = torch.randn(T, Hq, D, device="cuda").to(BF)
+    c.attend(q, i32(starts), i32(lens), pages)
+    torch.cuda.synchronize()
+    assert bool((around[:4096] == 255).all()) and bool((around[4096 + n:] == 255).all())
+    assert bool((out[:32] == 7).all()) and bool((out[32 + T:] == 7).all())
+    assert bool(torch.isfinite(c.out.float()).all())           # (the pool holds zeros)
