@@ -527,7 +527,9 @@ xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, cons
  * xhc_attn_bwd - dqkv [T, Hq + 2 Hkv, D] from qkv, span, slopes as in the
  *   forward, its out and saved, and dout [T,Hq,D]; slopes get no gradient.
  *   workspace: xhc_attn_workspace_bytes(d, h) bytes.
- * Sums and softmax are fp32, in an order that the sizes fix.  bf16 state:
+ * Scores are rounded to fp32: one of size s is off by 2^-24 s, and its weight by
+ * a factor of exp of that.  Sums and softmax are fp32, in an order that the
+ * sizes fix.  bf16 state:
  * probabilities and the gradients of scores are rounded to bf16 as operands of
  * the next product; fp32 state: products are those of fp32 values in full.     */
 size_t xhc_attn_saved_bytes(const xhc_dims* d, const xhc_heads* h);

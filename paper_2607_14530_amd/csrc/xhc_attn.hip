@@ -59,6 +59,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
   if (ex.x < ex.y) {
     Score<TS> sc;
     sc.init(a, head);
+    bool far = false;                            // some row's m is above kFar
     Frag<TS> q[KS];
     const TS* qp = reinterpret_cast<const TS*>(base) + (int64_t)(row ? t : T1) * H * D + head * D;
 #pragma unroll
@@ -130,24 +131,41 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
       if (MODE == 1 && (!cut || top != kNoKey)) top = fmaf(-2.f * sc.cap, sc.share_of(top), sc.cap);
       // The row's reference only follows its maximum when that is 2^8 above it:
       // probabilities up to 256 are as exact, and sums are rarely rescaled.
-      if (__any(top > m + 8.f)) {
-        const float to = top > m + 8.f ? top : m;           // (from -inf: the first maximum)
-        const float c = m == kNoKey ? 0.f : __builtin_amdgcn_exp2f(m - to);
-        m = to;
-        l *= c;
+      // Far scores: the exponents are formed in the branch, and 1 times them less 0
+      // is what exp2 then takes (so that the way of all others stays as it is).
+      float ref = m == kNoKey ? 0.f : m, mul = sc.mul;      // (a row that has seen nothing: exp2(-inf) = 0)
+      const bool rise = __any(top > m + 8.f);
+      if (rise || (MODE == 0 && far)) {
+        if (rise) {
+          const float to = top > m + 8.f ? top : m;           // (from -inf: the first maximum)
+          const float c = m == kNoKey ? 0.f : __builtin_amdgcn_exp2f(m - to);
+          m = to;
+          l *= c;
 #pragma unroll
-        for (int f = 0; f < F; ++f)
+          for (int f = 0; f < F; ++f)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[f][r] *= c;
+            for (int r = 0; r < 16; ++r) o[f][r] *= c;
+          if (MODE == 0) far = __any(m != kNoKey && fabsf(m) > kFar);
+        }
+        ref = m == kNoKey ? 0.f : m;
+        if (MODE == 0 && far) {
+          const bool mine = fabsf(m) > kFar;
+#pragma unroll
+          for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              s[rb][r] = mine ? rounded_diff(s[rb][r], sc.mul, ref) : fmaf(s[rb][r], sc.mul, -ref);
+          mul = scalar(1.f);
+          ref = 0.f;
+        }
       }
-      const float ref = m == kNoKey ? 0.f : m;              // a row that has seen nothing: exp2(-inf) = 0
 #pragma unroll
       for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float x = s[rb][r];
           s[rb][r] = __builtin_amdgcn_exp2f(MODE == 2   ? x - ref
-                                            : MODE == 0 ? fmaf(x, sc.mul, -ref)
+                                            : MODE == 0 ? fmaf(x, mul, -ref)
                                                         : fmaf(-2.f * sc.cap, sc.share_of(x), sc.cap - ref));
           if (MODE == 1 && cut && x == kNoKey) s[rb][r] = 0.f;           // (the cap has its say there too)
         }

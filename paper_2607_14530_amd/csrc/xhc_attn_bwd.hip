@@ -71,13 +71,14 @@ __global__ __launch_bounds__(256) void k_attn_prep(AttnArgs a, float* delta, int
   }
 }
 
-// p and dS of N pairs from the raw products and dP; bias, lse, delta: of pair r.
+// p and dS of N pairs from the raw products and dP; dist, lse, delta: of pair r.
+// The score is rounded as the forward rounds it (and a far one's largest is then lse).
 // A cap is asked for once for them all: asked for with each pair, its two ways
 // kept more than the registers hold, and at D = 128 k_attn_dkv went through
 // scratch memory (backward of T = 8192, Hq = 32, Hkv = 8, cap 30: 2960 us instead
 // of 2490; with a bias at D = 64, Hq = 16, Hkv = 4: 970 instead of 664).
-template <typename TS, int N, class B, class L, class E>
-__device__ __forceinline__ void reverse_scores(float* x, float* dp, const Score<TS>& sc, bool capped, B&& bias, L&& lse,
+template <typename TS, int N, class I, class L, class E>
+__device__ __forceinline__ void reverse_scores(float* x, float* dp, const Score<TS>& sc, bool capped, I&& dist, L&& lse,
                                                E&& delta) {
   if (capped) {
     branch_only();
@@ -97,7 +98,7 @@ __device__ __forceinline__ void reverse_scores(float* x, float* dp, const Score<
   }
 #pragma unroll
   for (int r = 0; r < N; ++r) {
-    x[r] = __builtin_amdgcn_exp2f(x[r] + bias(r) - lse(r));
+    x[r] = __builtin_amdgcn_exp2f(fmaf(-sc.slope, dist(r), x[r]) - lse(r));
     dp[r] *= x[r];
   }
 }
@@ -142,7 +143,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
     Score<TS> sc;
     sc.init(a, head);
     const int64_t tc = row ? t : T1;
-    const float lse = a.lse[(int64_t)head * a.Tp + tc], delta = a.delta[(int64_t)head * a.Tp + tc];
+    float lse = a.lse[(int64_t)head * a.Tp + tc];
+    const float delta = a.delta[(int64_t)head * a.Tp + tc];
+    // where scores are far: the exponents are formed in a branch, and 1 times them
+    // less 0 is what exp2 then takes
+    const bool far = !EX && __any(fabsf(lse) > kFar && fabsf(lse) <= FLT_MAX);
+    const float mul = scalar(far ? 1.f : sc.mul);
+    if (far) lse = 0.f;
     Frag<TS> q[KS], go[KS];
     const TS* qp = reinterpret_cast<const TS*>(base) + tc * H * D + head * D;
     const TS* gp = reinterpret_cast<const TS*>(a.dout) + (tc * a.Hq + head) * D;
@@ -189,15 +196,22 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(TS) == 2 ? 2 : 1) void k_at
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = s[4 * i + r], y[r] = dp[4 * i + r];
             reverse_scores<TS, 4>(x, y, sc, a.cap > 0.f,
-                                  [&](int r) { return -sc.slope * fabsf(d0 - (float)sum_row(4 * i + r)); },
+                                  [&](int r) { return fabsf(d0 - (float)sum_row(4 * i + r)); },
                                   [&](int) { return lse; }, [&](int) { return delta; });
 #pragma unroll
             for (int r = 0; r < 4; ++r) dp[4 * i + r] = y[r];
           }
         } else {
+          if (far) {
+            branch_only();
+            const float of = a.lse[(int64_t)head * a.Tp + (row ? t : T1)];
+            const bool mine = fabsf(of) > kFar;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = mine ? rounded_diff(s[r], sc.mul, of) : fmaf(s[r], sc.mul, -of);
+          }
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            dp[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.mul, -lse)) * (dp[r] - delta);
+            dp[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, -lse)) * (dp[r] - delta);
         }
         if (bad) {
           branch_only();
@@ -415,7 +429,7 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
               if constexpr (!EX)
                 share<16, KS>(i, [&](auto e) {
                   if constexpr (e.value % 4 == 0) four = *reinterpret_cast<const float4*>(rows + 2 * e.value);
-                  s[e.value] = __builtin_amdgcn_exp2f(fmaf(s[e.value], sc.mul, -(&four.x)[e.value % 4]));
+                  s[e.value] = __builtin_amdgcn_exp2f(rounded_diff(s[e.value], sc.mul, (&four.x)[e.value % 4]));
                 });
             });
         if constexpr (EX) {
@@ -428,7 +442,7 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = s[4 * i + r], y[r] = dp[4 * i + r];
             reverse_scores<TS, 4>(x, y, sc, a.cap > 0.f,
-                                  [&](int r) { return -sc.slope * fabsf(d0 + (float)sum_row(4 * i + r)); },
+                                  [&](int r) { return fabsf(d0 + (float)sum_row(4 * i + r)); },
                                   [&](int r) { return (&lse.x)[r]; }, [&](int r) { return (&del.x)[r]; });
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[4 * i + r] = x[r], dp[4 * i + r] = y[r];

@@ -470,6 +470,7 @@ template <typename TS, int D, int RT, bool EX>
 __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_cache_attend(CacheArgs a) {
   using BL = Block<D>;
   constexpr int G = BL::G, W = BL::W, ROWS = 16 * RT, LD = D + 4;
+  constexpr bool ROUND = RT == 2;                // scores always rounded before their difference (see kFar)
   __shared__ __align__(16) float sums[4][16][LD];
   __shared__ float2 mls[4][16];
   __shared__ int64_t scan[256];
@@ -598,6 +599,7 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
     Score<TS> sc;
     sc.mul = a.cap > 0.f ? a.scale / a.cap * (sizeof(TS) == 2 ? 2.f * kLog2e : 1.f) : a.scale * kLog2e;
     sc.cap = a.cap * kLog2e;
+    bool far = false;                            // some row's m is above kFar
 
     const int count = (upto - from - wave + 3) / 4;          // this wave's blocks: from + wave + 4 i
     const int* pages = a.pages + (int64_t)b * a.per_seq;
@@ -682,20 +684,37 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
           for (int e = 1; e < 8; ++e) top = fmaxf(top, s[rt][e / 4][e % 4]);
           if constexpr (!EX) top *= sc.mul;        // (the raw products so far; exp takes the factor with it)
           top = max_quarters(top);
-          if (__any(top > m[rt] + 8.f)) {        // (as in the attention of token rows)
-            const float to = top > m[rt] + 8.f ? top : m[rt];
-            const float c = m[rt] == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(m[rt] - to);
-            m[rt] = to;
-            l[rt] *= c;
+          // (reference and far scores as in the attention of token rows)
+          float mul = sc.mul;
+          const bool rise = __any(top > m[rt] + 8.f);
+          if (rise || far) {
+            if (rise) {
+              const float to = top > m[rt] + 8.f ? top : m[rt];
+              const float c = m[rt] == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(m[rt] - to);
+              m[rt] = to;
+              l[rt] *= c;
 #pragma unroll
-            for (int n2 = 0; n2 < W; ++n2)
+              for (int n2 = 0; n2 < W; ++n2)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[rt][n2][e] *= c;
+                for (int e = 0; e < 4; ++e) o[rt][n2][e] *= c;
+              if (!EX && !ROUND) far = __any(m[rt] != -__builtin_huge_valf() && fabsf(m[rt]) > kFar);
+            }
+            if (far) {
+              const float ref = m[rt] == -__builtin_huge_valf() ? 0.f : m[rt];
+              const bool mine = fabsf(ref) > kFar;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float y = s[rt][e / 4][e % 4];
+                s[rt][e / 4][e % 4] = mine ? rounded_diff(y, sc.mul, ref) : fmaf(y, sc.mul, -ref);
+              }
+              mul = scalar(1.f);
+            }
           }
-          const float ref = m[rt] == -__builtin_huge_valf() ? 0.f : m[rt];
+          const float ref = far || m[rt] == -__builtin_huge_valf() ? 0.f : m[rt];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float x = __builtin_amdgcn_exp2f(EX ? s[rt][e / 4][e % 4] - ref : fmaf(s[rt][e / 4][e % 4], sc.mul, -ref));
+            const float y = s[rt][e / 4][e % 4];
+            const float x = __builtin_amdgcn_exp2f(EX ? y - ref : ROUND ? rounded_diff(y, sc.mul, ref) : fmaf(y, mul, -ref));
             s[rt][e / 4][e % 4] = x;
             l[rt] += x;
           }
