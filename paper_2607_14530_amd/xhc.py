@@ -967,8 +967,9 @@ def rotation_table(positions, R, base=10000.0, device="cuda"):
 
 
 def _settle():
-    """Waits for what a bundle's constructor has enqueued: its first call may then go to any stream.  (Where the
-    constructor itself is captured there is nothing to wait for before the replay.)"""
+    """Waits for what a bundle's constructor has enqueued, and for earlier work in memory that it was given: its first
+    call may then go to any stream.  (Where the constructor itself is captured there is nothing to wait for before the
+    replay.)"""
     if not torch.cuda.is_current_stream_capturing():
         torch.cuda.current_stream().synchronize()
 
@@ -1059,6 +1060,7 @@ class Attention:
         self.shape = (d.T, h.Hq + 2 * h.Hkv, h.D)
         self.saved = None
         self.span = None
+        _settle()
 
     def spans(self, starts=None, prefix=None, stream=None):
         """span [T, 2] of documents: document i has the tokens starts[i] .. starts[i + 1] - 1 (int32 [n + 1]), its
@@ -1098,6 +1100,7 @@ class TrainableAttention(Attention):
         self.dqkv = torch.empty(self.shape, dtype=self.out.dtype, device=self.device)
         self.ws = _bytes(xhc_attn_workspace_bytes(d, h), self.device)
         self.seen = None
+        _settle()
 
     def forward(self, qkv, span=None, stream=None):
         out = super().forward(qkv, span, stream)

@@ -21,6 +21,7 @@ def calls(monkeypatch):
         return t
     monkeypatch.setattr(X, "_take", take)
     monkeypatch.setattr(X, "_here", lambda device: torch.device("cpu"))
+    monkeypatch.setattr(X, "_settle", lambda: None)
     return made
 
 
@@ -101,7 +102,6 @@ def test_heads_that_do_not_fit_their_fields_are_refused(v):
                                 dict(sequences=2 ** 32 + 2), dict(per_sequence=2 ** 32 + 2, npages=8)])
 def test_caches_that_do_not_fit_their_fields_are_refused(calls, kw, monkeypatch):
     """A pool of 2^32 + 65536 pages would be one of 65536, and what lies in the others lost."""
-    monkeypatch.setattr(X, "_settle", lambda: None, raising=False)
     made = []
     monkeypatch.setattr(torch, "zeros", lambda *a, **k: made.append(a))
     h = X.make_heads(Hq, Hkv, D, rotary=0)
