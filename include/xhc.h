@@ -509,8 +509,9 @@ xhc_status xhc_rotate(const xhc_dims* d, const xhc_heads* h, const void* in, con
  * attention stays within it; tokens of none see nothing.  prefix [n] int32 or
  * NULL: the first prefix[i] tokens of document i are seen by all of it (cut at
  * its end).  Without starts (NULL, n = 0, prefix NULL) a document is a sequence
- * of S tokens.  Otherwise token t sees up to t, of the last h->window positions
- * where that is not 0.                                                        */
+ * of S tokens.  Otherwise token t sees up to t.  h->window, where that is not 0,
+ * cuts what lies in front of a token, its prefix too: it sees from t - window + 1
+ * on (and a prefix that reaches behind it to its end).                        */
 xhc_status xhc_attn_spans(const xhc_dims* d, const xhc_heads* h, int32_t n, const int32_t* starts,
                           const int32_t* prefix, int32_t* span, void* stream);
 

@@ -1064,7 +1064,8 @@ class Attention:
 
     def spans(self, starts=None, prefix=None, stream=None):
         """span [T, 2] of documents: document i has the tokens starts[i] .. starts[i + 1] - 1 (int32 [n + 1]), its
-        first prefix[i] (int32 [n]) seen by all of it; without starts, of sequences."""
+        first prefix[i] (int32 [n]) seen by all of it, as far as a window reaches back; without starts, of
+        sequences."""
         n = 0 if starts is None else starts.numel() - 1
         if starts is not None:
             if n < 0:
