@@ -13,6 +13,11 @@
 //              so that those, rounded, are the other operand as they lie: the
 //              probabilities never leave their lane's registers
 //
+// With a bf16 state probabilities and the gradients of scores are rounded to bf16
+// there, as the instructions take operands of one type: held in two halves each
+// product of theirs would be two.  Outputs and gradients are then off by 0.0024 of
+// their norm; their own rounding alone makes 0.0017.
+//
 // fp32 tensors use the 32x32x2 instruction eight times on the same eight
 // elements, which takes their products in full at a sixteenth of the rate.
 #pragma once

@@ -6,10 +6,10 @@
 // Forward (k_attn): a workgroup takes 128 queries of a head, a wave 32 of them,
 // and goes once over the keys that its rows see, 64 at a time, with the running
 // maximum and sum of each row.  T = 16384 in two sequences, Hq = 32, Hkv = 8,
-// D = 128, bf16: 1.17 ms, 0.94 PFLOP/s of the pairs that are seen, with the
-// matrix cores busy for 48 % of the cycles, the vector ones for 64 %, at a clock
-// that power holds near 1.9 GHz; no bank conflicts.  8190 tokens in 23
-// documents, Hq = 16, D = 64: 43 us, where the matrix cores are busy for 9 % and
+// D = 128, bf16: 1.11 to 1.17 ms, 0.94 to 0.99 PFLOP/s of the pairs that are seen,
+// with the matrix cores busy for 47 % of the cycles, the vector ones for 63 %, at a
+// clock that power holds near 1.9 GHz; no bank conflicts.  8190 tokens in 23
+// documents, Hq = 16, D = 64: 44 us, where the matrix cores are busy for 9 % and
 // a workgroup's start, with its first copies, and the longest documents count.
 #include <float.h>
 

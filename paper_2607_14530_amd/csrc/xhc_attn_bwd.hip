@@ -10,8 +10,8 @@
 // products in place of five, but no sum is shared between workgroups: no
 // atomics, no fp32 copy of dq, and an order that only the sizes fix.  T = 16384
 // in two sequences, Hq = 32, Hkv = 8, D = 128, bf16: k_attn_prep 73 us (5.5
-// TB/s), k_attn_dkv 2.2 ms and k_attn_dq 1.55 ms (1.0 PFLOP/s of their products,
-// the matrix cores busy for 46 and 53 % of the cycles; the clock as forward).
+// TB/s), k_attn_dkv 2.2 ms and k_attn_dq 1.5 ms (1.0 PFLOP/s of their products,
+// the matrix cores busy for 45 and 55 % of the cycles; the clock as forward).
 #include <float.h>
 
 #include "xhc_attn.h"
@@ -302,7 +302,10 @@ __global__ __launch_bounds__(64 * dkv_waves(sizeof(TS) == 4, D), sizeof(TS) == 2
   const uint32_t qstride = (uint32_t)H * D * sizeof(TS), gstride = (uint32_t)a.Hq * D * sizeof(TS);
   const uint32_t at = lds_offset(lds);
 
-  // the first and last tile of queries of which some row sees one of these keys
+  // The first and last tile of queries of which some row sees one of these keys.
+  // Each workgroup reads the ranges of all tiles, out of its XCD's L2 (in sequences
+  // of 512, Hq = 16, Hkv = 4, D = 64, where the work itself grows with T alone, a backward
+  // takes 168 us for 16384 of T = 2^17 tokens and 164 for as many of 2^19).
   if (threadIdx.x < 2) reach[threadIdx.x] = threadIdx.x ? -1 : INT32_MAX;
   __syncthreads();
   auto sees = [&](const int4& e) { return e.x < j0 + KEYS && e.y > j0 && e.x < e.y; };

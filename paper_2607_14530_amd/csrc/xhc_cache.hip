@@ -15,7 +15,8 @@
 //           broadcast within the row, part of the instruction that multiplies)
 //
 // A group's scale is a factor of its share of a score, and of a probability
-// before it is rounded as an operand of the product with the values.
+// before it is rounded (bf16 state) as an operand of the product with the values.
+// The row's sum is of the unrounded ones: a rounded one goes with its group's scale.
 //
 // Measured at Hq = 32, Hkv = 8, D = 128, bf16: a token's attention over 131072
 // keys 34 us (151 MB, 4.4 TB/s) and the join 8; over 64 sequences of 2048 to
@@ -714,7 +715,9 @@ __global__ __launch_bounds__(256, attend_wgs(sizeof(TS) == 4, 16 * RT)) void k_c
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float y = s[rt][e / 4][e % 4];
-            const float x = __builtin_amdgcn_exp2f(EX ? y - ref : ROUND ? rounded_diff(y, sc.mul, ref) : fmaf(y, mul, -ref));
+            const float x = __builtin_amdgcn_exp2f(EX      ? y - ref
+                                                   : ROUND ? rounded_diff(y, sc.mul, ref)
+                                                           : fmaf(y, mul, -ref));
             s[rt][e / 4][e % 4] = x;
             l[rt] += x;
           }
