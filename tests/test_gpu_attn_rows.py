@@ -87,12 +87,14 @@ def test_shares_of_a_group(Hq, Hkv, D, kw, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("cap,D", [(0.0, 64), (30.0, 64), (0.0, 128), (30.0, 32), (0.0, 96)])
-def test_bad_values_that_are_not_seen(cap, D, dtype):
+@pytest.mark.parametrize("cap,D,biased", [(0.0, 64, False), (30.0, 64, False), (0.0, 128, False), (30.0, 32, False),
+                                          (0.0, 96, False), (0.0, 64, True), (30.0, 128, True)])
+def test_bad_values_that_are_not_seen(cap, D, biased, dtype):
     """NaN and infinities in a token: what does not see it keeps its bits, forward and backward."""
     T, Hq, Hkv = 1100, 32, 4
     d = X.make_dims(T, 1, 1, 1, 32, S=T, state=NAME[dtype])
-    att = X.TrainableAttention(d, X.make_heads(Hq, Hkv, D, cap=cap))
+    slopes = 0.5 ** torch.arange(1, Hq + 1, device="cuda").float() if biased else None
+    att = X.TrainableAttention(d, X.make_heads(Hq, Hkv, D, cap=cap), slopes=slopes)
     span = att.spans(i32([0, 500, 1080]), i32([40, 0]))
     qkv, dout = (z.cuda() for z in U.inputs(T, Hq, Hkv, D, dtype, 3))
     dout[1080:] = 0
